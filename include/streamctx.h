@@ -380,6 +380,73 @@ int sc_stack_forward(const sc_block_weights* layers, int32_t n_layers, sc_cache*
                      const sc_plan* plan, void* x, const sc_rope* rope, void* ws, size_t ws_bytes,
                      sc_stream stream);
 
+/* ---- A bounded, shared history -------------------------------------------
+ * What leaves the history window can live on in a bounded form: the attention
+ * weighs the cached keys, the heaviest tokens of several states are folded into
+ * one state, and every node of a pack reads that state beside its own.
+ *
+ * Weights of a cache: a caller-owned device array of
+ * sc_cache_weights_bytes() bytes, fp32
+ *   weights[layer][slot][head][token]
+ * with the pool's slot numbering.  Slots are used again after a release, so a
+ * state's weights are cleared (every layer) when it is new to the array;
+ * nothing else clears them.  Calls that write one array are ordered on one
+ * stream. */
+size_t sc_cache_weights_bytes(const sc_cache* cache);
+/* Zeroes the weights of one cached state in every layer.  SC_ENOTFOUND. */
+int sc_cache_weights_clear(const sc_cache* cache, sc_node state, float* weights, sc_stream stream);
+
+/* sc_attention that also adds to every cached key the weight it received:
+ *   weights[layer][slot][head][token] += sum over the plan's nodes that read
+ *     the slot, and over their query rows, of softmax(Q K^T * scale)
+ * bf16 and fp32 caches; the weights of slots that the plan does not read stay as
+ * they are.  Sums are fp32 in a fixed order: equal calls give equal bits.  The
+ * logits are products of q and k as they are stored, scaled in fp32, and o
+ * follows from the same (sc_attention rounds a bf16 q times the scale): both
+ * calls agree within bf16 rounding, not in bits.  Limits, arguments and errors
+ * as sc_attention (layer, plan and workspace among them), and SC_EINVAL for
+ * a scale that is not finite or a null array.  ws: 16-byte aligned, of
+ * sc_attention_weigh_workspace_bytes(plan, cache) bytes. */
+size_t sc_attention_weigh_workspace_bytes(const sc_plan* plan, const sc_cache* cache);
+int sc_attention_weigh(const sc_plan* plan, const sc_cache* cache, int32_t layer, const void* q,
+                       void* o, float scale, float* weights, void* ws, size_t ws_bytes,
+                       sc_stream stream);
+
+/* Folds n cached states into one, in layers [layer, layer + n_layers): with the
+ * sources' tokens numbered in the order of `sources` (frames ascending), each
+ * head keeps its T = pages_per_chunk * tokens_per_page tokens of the largest
+ * weights, of equal weights the lowest numbers (a NaN counts as lighter than any
+ * number), and the new state `into` holds their keys, values and weights in
+ * the order of their numbers.  Keys stay as they were cached (rotated at their
+ * own positions), so attention over the fold needs nothing else.  kept: device
+ * int32 [n_layers][n_heads][T], the numbers kept.  `into` gets slots as by
+ * sc_cache_append; the sources stay cached until they are released.  At most 800
+ * pages in all.  Errors: SC_EINVAL (null argument, layers out of range, a state
+ * named twice), SC_ENOTFOUND, SC_EUNAVAILABLE (a source not written at one of
+ * the layers), SC_EEXIST (`into` written at one of them), SC_ECAPACITY,
+ * SC_EUNSUPPORTED, SC_EDEVICE. */
+int sc_cache_condense(sc_cache* cache, int32_t layer, int32_t n_layers, const sc_node* sources,
+                      int32_t n, sc_node into, float* weights, int32_t* kept, sc_stream stream);
+
+/* A plan whose nodes read the n given cached states first, all of them, and then
+ * what `plan` has them read: a memory beside a pack's windows, one prompt
+ * before many continuations (sc_plan_condition with an nq of 1 makes nodes of
+ * single tokens), one history before many candidates.  The new plan stands by
+ * itself (`plan` may be freed) and goes wherever a plan of `plan`'s kind goes:
+ * sc_attention, sc_attention_noalloc, sc_attention_weigh, and as the plan of a
+ * block or stack or of its cross-attention.  The attention reads the prefix once
+ * for the rows of all nodes where that pays.  Limits: at most 64 nodes and 800
+ * pages with the prefix counted once; at least 32 tokens per page for bf16; and
+ * where the nodes' lists hold more than 800 pages together, or pages of fewer
+ * than 64 tokens are read by more than 64 queries a node, no more rows than
+ * 136 MB of partials hold (two of head_dim + 2 fp32 values per row and head);
+ * else SC_EUNSUPPORTED when the plan is used (SC_ECAPACITY if it is the
+ * smaller scratch of sc_attention_noalloc that does not hold them).
+ * A plan that shares a prefix already gets the new states before it.
+ * Errors: SC_EINVAL (null argument, n < 1, a state that would be read twice:
+ * named twice, or read by a node of `plan`), SC_ENOTFOUND, SC_EUNSUPPORTED. */
+int sc_plan_share(const sc_plan* plan, const sc_node* states, int32_t n, sc_plan** out);
+
 /* Measurement support (kernel timer, matrix-core probe): streamctx_measure.h */
 
 #ifdef __cplusplus

@@ -27,6 +27,7 @@ __all__ = [
     "sc_pipeline_rounds", "sc_pipeline_round_nodes", "sc_cache_release_unread", "sc_stack_forward",
     "sc_serial_steps", "sc_serial_step_node", "sc_block_workspace_views",
     "sc_attention_noalloc", "sc_attention_noalloc_scratch_bytes",
+    "sc_cache_weights_bytes", "sc_attention_weigh_workspace_bytes", "sc_attention_weigh", "sc_plan_share",
 ]
 
 SC_OK, SC_EINVAL, SC_EUNAVAILABLE, SC_ECAPACITY = 0, -1, -2, -3
@@ -51,6 +52,8 @@ EXPORTED_SYMBOLS = [
     "sc_pipeline_rounds", "sc_pipeline_round_nodes", "sc_cache_release_unread", "sc_stack_forward",
     "sc_serial_steps", "sc_serial_step_node", "sc_block_workspace_views",
     "sc_attention_noalloc", "sc_attention_noalloc_scratch_bytes",
+    "sc_cache_weights_bytes", "sc_cache_weights_clear", "sc_attention_weigh_workspace_bytes",
+    "sc_attention_weigh", "sc_cache_condense", "sc_plan_share",
 ]
 
 # The library and PyTorch must share one HIP runtime: torch ships its own
@@ -168,6 +171,12 @@ _SIG = {
     "sc_serial_step_node": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.POINTER(sc_node)]),
     "sc_block_workspace_views": (C.c_int, [C.POINTER(sc_block_weights), C.c_int32, C.POINTER(C.c_size_t),
                                            C.POINTER(C.c_size_t)]),
+    "sc_cache_weights_bytes": (C.c_size_t, [_P]),
+    "sc_cache_weights_clear": (C.c_int, [_P, sc_node, _P, _P]),
+    "sc_attention_weigh_workspace_bytes": (C.c_size_t, [_P, _P]),
+    "sc_attention_weigh": (C.c_int, [_P, _P, C.c_int32, _P, _P, C.c_float, _P, _P, C.c_size_t, _P]),
+    "sc_cache_condense": (C.c_int, [_P, C.c_int32, C.c_int32, C.POINTER(sc_node), C.c_int32, sc_node, _P, _P, _P]),
+    "sc_plan_share": (C.c_int, [_P, C.POINTER(sc_node), C.c_int32, C.POINTER(_P)]),
 }
 # ABI version this binding marshals for (SC_ABI_VERSION of the header)
 ABI_VERSION = 7
@@ -329,6 +338,19 @@ class Cache:
         _check(lib.sc_cache_append(self._h, layer, sc_node(*state), _ptr(k), _ptr(v), rp,
                                    _stream(stream)))
 
+    def weights_clear(self, state, weights, stream=None) -> None:
+        """Zero the accumulated weights of one cached state, every layer."""
+        _check(lib.sc_cache_weights_clear(self._h, sc_node(*state), _ptr(weights), _stream(stream)))
+
+    def condense(self, layer: int, n_layers: int, sources, into, weights, kept, stream=None) -> None:
+        """Fold the cached states ``sources`` into the new state ``into`` in layers
+        [layer, layer + n_layers): each head keeps its heaviest tokens (``weights``:
+        fp32 [n_layers][n_slots][heads][tokens] of the whole cache).  ``kept``
+        (device int32 [n_layers, heads, tokens of a state]) receives their numbers."""
+        arr = (sc_node * max(1, len(sources)))(*[sc_node(int(c), int(j)) for c, j in sources])
+        _check(lib.sc_cache_condense(self._h, layer, n_layers, arr, len(sources), sc_node(*into),
+                                     _ptr(weights), _ptr(kept), _stream(stream)))
+
 
 def sc_cache_create(pool, n_layers, n_heads, head_dim, tokens_per_page, pages_per_chunk, n_slots,
                     dtype=SC_DTYPE_BF16) -> Cache:
@@ -399,6 +421,14 @@ def sc_plan_condition(cache: Cache, conditions, nq: int) -> Plan:
     return Plan(out.value, cache)
 
 
+def sc_plan_share(plan: Plan, states) -> Plan:
+    """Plan whose nodes all read the cached ``states`` before what ``plan`` has them read."""
+    arr = (sc_node * max(1, len(states)))(*[sc_node(int(c), int(j)) for c, j in states])
+    out = C.c_void_p()
+    _check(lib.sc_plan_share(plan.handle, arr, len(states), C.byref(out)))
+    return Plan(out.value, plan.cache)
+
+
 def sc_condition_workspace_bytes(cache: Cache) -> int:
     return lib.sc_condition_workspace_bytes(cache.handle)
 
@@ -417,6 +447,22 @@ def sc_attention(plan: Plan, cache: Cache, layer: int, q, o, scale: float, ws=No
                  ws_bytes: int = 0, stream=None) -> None:
     _check(lib.sc_attention(plan.handle, cache.handle, layer, _ptr(q), _ptr(o), scale, _ptr(ws),
                             ws_bytes, _stream(stream)))
+
+
+def sc_cache_weights_bytes(cache: Cache) -> int:
+    return lib.sc_cache_weights_bytes(cache.handle)
+
+
+def sc_attention_weigh_workspace_bytes(plan: Plan, cache: Cache) -> int:
+    return lib.sc_attention_weigh_workspace_bytes(plan.handle, cache.handle)
+
+
+def sc_attention_weigh(plan: Plan, cache: Cache, layer: int, q, o, scale: float, weights, ws,
+                       ws_bytes: int, stream=None) -> None:
+    """sc_attention that also adds the weight every cached key received to ``weights``
+    (fp32 [n_layers][n_slots][heads][tokens], ``sc_cache_weights_bytes`` bytes)."""
+    _check(lib.sc_attention_weigh(plan.handle, cache.handle, layer, _ptr(q), _ptr(o), scale,
+                                  _ptr(weights), _ptr(ws), ws_bytes, _stream(stream)))
 
 
 # ---------------------------------------------------------------------- block

@@ -6,6 +6,7 @@
 #include <cstdarg>
 #include <cstdint>
 #include <map>
+#include <memory>
 #include <string>
 #include <utility>
 #include <vector>
@@ -30,6 +31,8 @@ struct StateEntry {
   std::vector<int32_t> slots;    // pages_per_chunk slot ids, frames ascending
   std::vector<uint8_t> written;  // per layer
 };
+
+struct WeighLaunches;  // weigh.hip
 
 inline size_t dtype_size(int32_t dtype) { return dtype == SC_DTYPE_F32 ? 4 : 2; }
 
@@ -64,8 +67,11 @@ struct sc_plan {
   std::vector<sc::StateKey> page_state;
   const sc_cache* cache;
   int32_t nq;  // query tokens per node
+  int32_t shared = 0;  // leading pages that every node's list has in common (sc_plan_share)
   // page slots in the bf16 attention's traversal order (built on first use)
   mutable std::vector<int32_t> attn_slot;
+  // its pages by the nodes that read them (built on first use)
+  mutable std::shared_ptr<const sc::WeighLaunches> weigh;
 };
 
 namespace sc {
@@ -99,9 +105,13 @@ int attention_check(const sc_plan* plan, const sc_cache* cache);
 int launch_attention(const sc_plan* plan, const sc_cache* cache, int32_t layer,
                      const void* q, void* o, float scale, void* ws, size_t ws_bytes,
                      hipStream_t stream);
-// Workspace of the bf16 attention for a plan (0 for fp32 caches and plans
-// whose units fill whole rounds of the CUs), and its bound over all plans
-// (at most kAttnMaxPieces partial results).
+// The same with the rows' logarithmic sums, fp32 [head][row] (log2; fp32 caches:
+// natural), where lse is not NULL.
+int launch_attention_lse(const sc_plan* plan, const sc_cache* cache, int32_t layer, const void* q, void* o, float* lse,
+                         float scale, void* ws, size_t ws_bytes, hipStream_t stream);
+// Workspace of the attention for a plan (0 for fp32 caches and plans whose units
+// fill whole rounds of the CUs, unless the nodes share a prefix), and its bound
+// over all plans (at most kAttnMaxPieces partial results).
 constexpr int32_t kAttnMaxPieces = 1024;
 constexpr int32_t kAttnMinSplitTiles = 32;  // mean 64-key tiles per unit below which nothing is cut
 size_t attention_workspace_bytes(const sc_plan* plan, const sc_cache* cache);
@@ -109,6 +119,17 @@ size_t attention_workspace_bound();
 int launch_append(const sc_cache* cache, int32_t layer, const int32_t* slots, int32_t chunk,
                   const void* k, const void* v, const sc_rope* rope, hipStream_t stream);
 int launch_rope_table(const sc_rope_desc* d, void* table, hipStream_t stream);
+
+// Adds the weight that every key of the plan's pages received to `weights` (the
+// whole array); lse: the rows' logarithmic sums.
+int launch_weigh(const sc_plan* plan, const sc_cache* cache, int32_t layer, const void* q, const float* lse,
+                 float scale, float* weights, hipStream_t stream);
+int launch_weights_clear(const sc_cache* cache, const int32_t* slots, int32_t n, float* weights, hipStream_t stream);
+// Whether a fold of so many states fits a launch: SC_OK or SC_EUNSUPPORTED; the
+// fold itself: slots of the n_src source pages, then the new state's.
+int condense_check(const sc_cache* cache, int32_t n_sources);
+int launch_condense(const sc_cache* cache, int32_t layer, int32_t n_layers, const int32_t* slots, int32_t n_src,
+                    float* weights, int32_t* kept, hipStream_t stream);
 
 // sc_block_forward in two halves: what it refuses, and its launches (whose
 // arguments have passed the first).  As one layer of a stack: sums_in: the sums of
@@ -152,6 +173,7 @@ enum TimerKind {
   TK_SAMPLER, TK_ATTN_COMBINE, TK_QK_NORM, TK_CROSS_ATTENTION, TK_GEMM_CROSS_Q,
   TK_GEMM_CROSS_OUT, TK_GEMM_CONDITION,
   TK_ROW_SCALE,  // launched by nothing: its name stays readable
+  TK_ATTN_WEIGH, TK_CONDENSE,
   TK_COUNT
 };
 void timer_begin(int kind, hipStream_t stream);

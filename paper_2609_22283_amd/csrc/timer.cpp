@@ -11,7 +11,7 @@ const char* const kNames[TK_COUNT] = {"attention", "gemm_qkv", "gemm_out", "gemm
                                       "gemm_down", "rmsnorm", "append", "sampler",
                                       "attention_combine", "qk_norm", "cross_attention",
                                       "gemm_cross_q", "gemm_cross_out", "gemm_condition",
-                                      "row_scale"};
+                                      "row_scale", "attention_weigh", "condense"};
 
 struct Record {
   int kind;

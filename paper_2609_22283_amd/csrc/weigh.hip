@@ -1,0 +1,370 @@
+// The weight that every cached key received: column sums of the attention's
+// probability matrices.
+//
+//   w[slot][head][token] += sum over the nodes i that read the slot, and their
+//                           rows q, of exp2(unit q . k - lse[q])
+//
+// lse: the rows' logarithmic sums, left by the attention itself (log2 units), so a
+// second Q K^T is all that is computed; the probabilities are never stored.  A
+// work-group owns keys, holds them in registers and streams through the rows of
+// every node that reads them: nothing is summed across work-groups, so the
+// result does not depend on their order.  Keys read by the same nodes are taken
+// together, page after page.
+#include <algorithm>
+#include <climits>
+#include <cmath>
+#include <cstring>
+#include <map>
+
+#include "attention_core.h"
+
+namespace sc {
+
+constexpr int kWeighPages = 512, kWeighGroups = 64;
+
+// Pages in groups with the same readers (bit i: node i).
+struct WeighPlan {
+  uint64_t readers[kWeighGroups];
+  int32_t page0[kWeighGroups + 1];  // a group's pages are page_slot[page0[g] .. page0[g + 1])
+  int32_t block0[kWeighGroups];     // its first key block (INT32_MAX past the last group)
+  int32_t page_slot[kWeighPages];
+};
+
+struct WeighGeom {
+  const char* layer_base;
+  uint64_t slot_bytes;
+  float* weights;    // this layer's
+  const float* lse;  // [head][row]
+  int32_t n_heads, tpp, nq, rows, blocks;
+  DivMagic tpp_div, nq_div;
+  float unit;       // bf16: |scale| log2(e)
+  float scale;      // fp32
+  uint32_t q_flip;  // bf16: sign bits of a negative scale
+};
+
+// A work-group's keys: those of block `blk` of KB keys, and the rows that read them.
+struct WeighItem {
+  int32_t head, key0, n_keys, page0;  // key0: first key within the group's n_keys
+  uint64_t readers;
+};
+__device__ __forceinline__ WeighItem weigh_item(const WeighPlan& plan, const WeighGeom& g, int32_t kb) {
+  const int32_t i = (int32_t)xcd_remap(blockIdx.x, gridDim.x);  // an XCD's work-groups share the rows of a few heads
+  WeighItem it;
+  it.head = i / g.blocks;
+  const int32_t blk = i % g.blocks;
+  const int32_t grp = __builtin_popcountll(__builtin_amdgcn_ballot_w64(plan.block0[threadIdx.x & 63] <= blk)) - 1;
+  it.readers = plan.readers[grp];
+  it.page0 = plan.page0[grp];
+  it.n_keys = (plan.page0[grp + 1] - it.page0) * g.tpp;
+  it.key0 = (blk - plan.block0[grp]) * kb;
+  return it;
+}
+
+// Slot and token of a key of the group (clamped to its last one).
+struct WeighKey {
+  int32_t slot, token;
+};
+__device__ __forceinline__ WeighKey weigh_key(const WeighPlan& plan, const WeighGeom& g, const WeighItem& it, int32_t key) {
+  key = min(key, it.n_keys - 1);
+  const int32_t p = (int32_t)fast_div((uint32_t)key, g.tpp_div);
+  return WeighKey{plan.page_slot[it.page0 + p], key - p * g.tpp};
+}
+
+// The reading nodes in order, one per lane.
+__device__ __forceinline__ void list_readers(uint64_t readers, int32_t lane, int32_t* nodes) {
+  if (readers >> lane & 1) nodes[__builtin_popcountll(readers & ((1ull << lane) - 1))] = lane;
+}
+
+// Row of the pack that is the r-th of the reading nodes' rows.
+__device__ __forceinline__ int32_t reader_row(const WeighGeom& g, const int32_t* nodes, int32_t r) {
+  const int32_t i = (int32_t)fast_div((uint32_t)r, g.nq_div);
+  return nodes[i] * g.nq + (r - i * g.nq);
+}
+
+// The 16 columns (queries) of a result added up, in every lane.
+__device__ __forceinline__ float column_sum(float x) {
+  x += __shfl_xor(x, 1);
+  x += __shfl_xor(x, 2);
+  x += __shfl_xor(x, 4);
+  return x + __shfl_xor(x, 8);
+}
+
+typedef float f32x4a __attribute__((ext_vector_type(4), aligned(4)));
+
+// Adds the sums of keys key .. key + 3 (a multiple of 4; pages hold whole runs of 8).
+__device__ __forceinline__ void add_weights(const WeighPlan& plan, const WeighGeom& g, const WeighItem& it, int32_t key,
+                                            const f32x4& w) {
+  if (key >= it.n_keys) return;
+  const WeighKey k = weigh_key(plan, g, it, key);
+  f32x4a* p = reinterpret_cast<f32x4a*>(g.weights + ((size_t)k.slot * g.n_heads + it.head) * g.tpp + k.token);
+  *p = *p + w;
+}
+
+// 16 bytes per lane from an address of its own into LDS (see dma16).
+__device__ __forceinline__ void dma16_at(const char* p, uint32_t lds) {
+  uint32_t saved;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %2\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %1, off\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "v"(p), "s"(lds)
+      : "memory");
+}
+
+// bf16: four waves of 16 KW keys each, which stay in registers as the A operand of
+// S^T = K Q^T; tiles of 64 rows of q go through LDS (two buffers, 16-byte columns
+// swizzled by the row), shared by the waves.
+constexpr int WG_NW = 4, WG_QB = 64;
+template <int KW>
+__global__ __launch_bounds__(64 * WG_NW, 2) void weigh_bf16_kernel(const uint16_t* __restrict__ q, WeighGeom g,
+                                                                   WeighPlan plan) {
+  __shared__ __attribute__((aligned(1024))) char tiles[2][WG_QB * HDB * 2];
+  __shared__ int32_t nodes[kMaxNodes];
+  const int32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int32_t lg = lane >> 4, c = lane & 15;
+  const WeighItem it = weigh_item(plan, g, 16 * KW * WG_NW);
+  if (wave == 0) list_readers(it.readers, lane, nodes);
+  const int32_t key0 = it.key0 + 16 * KW * wave;
+  bf16x8 kf[KW][4];
+#pragma unroll
+  for (int b = 0; b < KW; ++b) {
+    const WeighKey k = weigh_key(plan, g, it, key0 + 16 * b + c);
+    const char* kp = g.layer_base + (size_t)k.slot * g.slot_bytes + ((size_t)it.head * g.tpp + k.token) * (HDB * 2) + 16 * lg;
+#pragma unroll
+    for (int ds = 0; ds < 4; ++ds) {
+      u32x4 u = *reinterpret_cast<const u32x4*>(kp + 64 * ds);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) u[e] ^= g.q_flip;
+      kf[b][ds] = __builtin_bit_cast(bf16x8, u);
+    }
+  }
+  __syncthreads();
+  const int32_t n_rows = __builtin_popcountll(it.readers) * g.nq;
+  const char* qh = reinterpret_cast<const char*>(q) + (size_t)it.head * (HDB * 2);
+  const size_t row_bytes = (size_t)g.n_heads * (HDB * 2);
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(tiles[0])) + 4096 * wave;
+  // copies this wave's 16 rows of a tile and returns lane l's lse of its row l
+  // (past the last row: the last row's values at lse +inf, which gives no weight)
+  const auto fetch = [&](int32_t t, int32_t buf) __attribute__((always_inline)) {
+    const int32_t r = WG_QB * t + lane, row = reader_row(g, nodes, min(r, n_rows - 1));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int32_t tr = 16 * wave + 4 * j + lg;
+      const int32_t src = __shfl(row, tr);
+      dma16_at(qh + (size_t)src * row_bytes + ((c ^ (tr & 15)) << 4), lds0 + buf * (WG_QB * HDB * 2) + 1024 * j);
+    }
+    const float l = g.lse[(size_t)it.head * g.rows + row];
+    return r < n_rows ? l : INFINITY;
+  };
+  f32x4 w[KW];
+#pragma unroll
+  for (int b = 0; b < KW; ++b) w[b] = f32x4{};
+  const int32_t nt = (n_rows + WG_QB - 1) / WG_QB;
+  float lse = fetch(0, 0);
+  for (int32_t t = 0; t < nt; ++t) {
+    landed();
+    const float l = lse;
+    if (t + 1 < nt) lse = fetch(t + 1, (t + 1) & 1);
+    const char* tile = tiles[t & 1];
+#pragma unroll
+    for (int qb = 0; qb < WG_QB / 16; ++qb) {
+      f32x4 s[KW];
+#pragma unroll
+      for (int b = 0; b < KW; ++b) s[b] = f32x4{};
+#pragma unroll
+      for (int ds = 0; ds < 4; ++ds) {
+        const bf16x8 f = *reinterpret_cast<const bf16x8*>(tile + (16 * qb + c) * 256 + (((4 * ds + lg) ^ c) << 4));
+#pragma unroll
+        for (int b = 0; b < KW; ++b) s[b] = mfma16(kf[b][ds], f, s[b]);
+      }
+      const float lq = __shfl(l, 16 * qb + c);
+#pragma unroll
+      for (int b = 0; b < KW; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) w[b][r] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], g.unit, -lq));
+    }
+  }
+#pragma unroll
+  for (int b = 0; b < KW; ++b) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) w[b][r] = column_sum(w[b][r]);
+    if (c == 0) add_weights(plan, g, it, key0 + 16 * b + 4 * lg, w[b]);
+  }
+}
+
+// fp32: a work-group of eight waves owns 16 keys; its waves take the 16-row blocks in
+// turn and add up through LDS, in wave order.  Operands as in attn_f32_kernel.
+constexpr int WF_NW = 8, WF_KB = 16;
+template <int HD>
+__global__ __launch_bounds__(64 * WF_NW) void weigh_f32_kernel(const float* __restrict__ q, WeighGeom g, WeighPlan plan) {
+  constexpr int NJ = HD / 16;
+  __shared__ f32x4 part[WF_NW][4];
+  __shared__ int32_t nodes[kMaxNodes];
+  const int32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int32_t lg = lane >> 4, c = lane & 15;
+  const WeighItem it = weigh_item(plan, g, WF_KB);
+  if (wave == 0) list_readers(it.readers, lane, nodes);
+  const WeighKey k = weigh_key(plan, g, it, it.key0 + c);
+  const float* kp = reinterpret_cast<const float*>(g.layer_base + (size_t)k.slot * g.slot_bytes) +
+                    ((size_t)it.head * g.tpp + k.token) * HD + 4 * lg;
+  f32x4 kf[NJ];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) kf[j] = *reinterpret_cast<const f32x4u*>(kp + 16 * j);
+  __syncthreads();
+  const int32_t n_rows = __builtin_popcountll(it.readers) * g.nq;
+  f32x4 w = {};
+  for (int32_t r0 = 16 * wave; r0 < n_rows; r0 += 16 * WF_NW) {
+    const int32_t r = r0 + c, row = reader_row(g, nodes, min(r, n_rows - 1));
+    const float* qp = q + ((size_t)row * g.n_heads + it.head) * HD + 4 * lg;
+    f32x4 qr[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) qr[j] = *reinterpret_cast<const f32x4u*>(qp + 16 * j) * g.scale;
+    const float l = r < n_rows ? g.lse[(size_t)it.head * g.rows + row] : INFINITY;
+    f32x4 s0 = {}, s1 = {};
+#pragma unroll
+    for (int j = 0; j < NJ; j += 2)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[j][e], qr[j][e], s0, 0, 0, 0);
+        s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[j + 1][e], qr[j + 1][e], s1, 0, 0, 0);
+      }
+    s0 += s1;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] += expf(s0[e] - l);
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w[e] = column_sum(w[e]);
+  if (c == 0) part[wave][lg] = w;
+  __syncthreads();
+  if (wave == 0 && c == 0) {
+#pragma unroll
+    for (int v = 1; v < WF_NW; ++v) w += part[v][lg];
+    add_weights(plan, g, it, it.key0 + 4 * lg, w);
+  }
+}
+
+// Zeroes the weights of slots, one slot of one layer per work-group.
+struct SlotList {
+  int32_t slot[64];
+};
+__global__ __launch_bounds__(256) void weights_clear_kernel(float* weights, size_t slot_floats, int32_t n_slots, SlotList s) {
+  float* p = weights + ((size_t)blockIdx.y * n_slots + s.slot[blockIdx.x]) * slot_floats;
+  for (size_t i = threadIdx.x; i < slot_floats; i += 256) p[i] = 0.f;
+}
+
+// A plan's distinct pages by their readers, most readers first (the longest
+// work-groups start first), in launches of bounded argument size.  A property of
+// the plan alone: found on its first use and kept in it.
+struct WeighLaunches {
+  std::vector<WeighPlan> plans;
+};
+
+static const WeighLaunches* weigh_launches(const sc_plan* p) {
+  if (p->weigh) return p->weigh.get();
+  std::map<int32_t, uint64_t> readers;
+  const int32_t n = (int32_t)p->nodes.size();
+  const uint64_t all = n == 64 ? ~0ull : (1ull << n) - 1;
+  for (int32_t i = 0; i < p->shared; ++i) readers[p->page_slot[i]] = all;
+  for (int32_t i = 0; i < n; ++i)
+    for (int32_t k = p->page_off[i] + p->shared; k < p->page_off[i + 1]; ++k) readers[p->page_slot[k]] |= 1ull << i;
+  std::map<uint64_t, std::vector<int32_t>> groups;
+  for (const auto& kv : readers) groups[kv.second].push_back(kv.first);
+  std::vector<std::pair<uint64_t, std::vector<int32_t>>> order(groups.begin(), groups.end());
+  std::stable_sort(order.begin(), order.end(), [](const auto& a, const auto& b) {
+    return __builtin_popcountll(a.first) > __builtin_popcountll(b.first);
+  });
+  auto out = std::make_shared<WeighLaunches>();
+  int32_t pages = kWeighPages, count = kWeighGroups;  // of the launch being filled
+  for (const auto& grp : order)
+    for (size_t at = 0; at < grp.second.size();) {
+      if (pages == kWeighPages || count == kWeighGroups) {
+        out->plans.emplace_back();
+        std::memset(&out->plans.back(), 0, sizeof(WeighPlan));
+        pages = count = 0;
+      }
+      WeighPlan& w = out->plans.back();
+      const size_t take = std::min(grp.second.size() - at, (size_t)(kWeighPages - pages));
+      w.readers[count] = grp.first;
+      w.page0[count] = pages;
+      std::copy(grp.second.begin() + at, grp.second.begin() + at + take, w.page_slot + pages);
+      pages += (int32_t)take;
+      at += take;
+      for (int32_t k = ++count; k <= kWeighGroups; ++k) w.page0[k] = pages;
+    }
+  p->weigh = out;
+  return out.get();
+}
+
+int launch_weigh(const sc_plan* p, const sc_cache* c, int32_t layer, const void* q, const float* lse, float scale,
+                 float* weights, hipStream_t stream) {
+  const sc_cache_desc& d = c->d;
+  WeighGeom g;
+  std::memset(&g, 0, sizeof g);
+  g.layer_base = c->pool + (size_t)layer * d.n_slots * c->slot_bytes;
+  g.slot_bytes = c->slot_bytes;
+  g.weights = weights + (size_t)layer * d.n_slots * d.n_heads * d.tokens_per_page;
+  g.lse = lse;
+  g.n_heads = d.n_heads;
+  g.tpp = d.tokens_per_page;
+  g.nq = p->nq;
+  g.rows = (int32_t)p->nodes.size() * p->nq;
+  g.tpp_div = magic_div((uint32_t)g.tpp);
+  g.nq_div = magic_div((uint32_t)g.nq);
+  g.unit = std::fabs(scale) * 1.4426950408889634f;
+  g.scale = scale;
+  g.q_flip = std::signbit(scale) ? 0x80008000u : 0u;
+  for (const WeighPlan& from : weigh_launches(p)->plans) {
+    WeighPlan plan = from;
+    const auto blocks = [&](int32_t kb) {
+      int64_t n = 0;
+      for (int32_t i = 0; i < kWeighGroups; ++i) {
+        const int64_t keys = (int64_t)(plan.page0[i + 1] - plan.page0[i]) * g.tpp;
+        plan.block0[i] = keys ? (int32_t)n : INT32_MAX;
+        n += (keys + kb - 1) / kb;
+      }
+      return (int32_t)n;
+    };
+    timer_begin(TK_ATTN_WEIGH, stream);
+    if (d.dtype == SC_DTYPE_F32) {
+      g.blocks = blocks(WF_KB);
+      const dim3 grid((uint32_t)(g.blocks * d.n_heads));
+      if (d.head_dim == 64)
+        hipLaunchKernelGGL((weigh_f32_kernel<64>), grid, dim3(64 * WF_NW), 0, stream, static_cast<const float*>(q), g, plan);
+      else
+        hipLaunchKernelGGL((weigh_f32_kernel<128>), grid, dim3(64 * WF_NW), 0, stream, static_cast<const float*>(q), g, plan);
+    } else {
+      const uint16_t* qb = static_cast<const uint16_t*>(q);
+      g.blocks = blocks(16 * 4 * WG_NW);
+      if (g.blocks * d.n_heads >= kCUs) {
+        hipLaunchKernelGGL((weigh_bf16_kernel<4>), dim3((uint32_t)(g.blocks * d.n_heads)), dim3(64 * WG_NW), 0, stream, qb, g, plan);
+      } else {
+        g.blocks = blocks(16 * WG_NW);
+        hipLaunchKernelGGL((weigh_bf16_kernel<1>), dim3((uint32_t)(g.blocks * d.n_heads)), dim3(64 * WG_NW), 0, stream, qb, g, plan);
+      }
+    }
+    timer_end(TK_ATTN_WEIGH, stream);
+    SC_HIP(hipGetLastError());
+  }
+  return SC_OK;
+}
+
+int launch_weights_clear(const sc_cache* c, const int32_t* slots, int32_t n, float* weights, hipStream_t stream) {
+  for (int32_t at = 0; at < n; at += 64) {
+    SlotList s;
+    const int32_t m = std::min(n - at, 64);
+    std::memset(&s, 0, sizeof s);
+    std::copy(slots + at, slots + at + m, s.slot);
+    for (int32_t l0 = 0; l0 < c->d.n_layers; l0 += 65535) {
+      const size_t slot_floats = (size_t)c->d.n_heads * c->d.tokens_per_page;
+      hipLaunchKernelGGL(weights_clear_kernel, dim3((uint32_t)m, (uint32_t)std::min(c->d.n_layers - l0, 65535)), dim3(256), 0,
+                         stream, weights + (size_t)l0 * c->d.n_slots * slot_floats, slot_floats, c->d.n_slots, s);
+    }
+    SC_HIP(hipGetLastError());
+  }
+  return SC_OK;
+}
+
+}  // namespace sc
