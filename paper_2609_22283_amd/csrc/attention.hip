@@ -97,10 +97,10 @@ static AttnSchedule workspace_schedule(const sc_plan* p, const sc_cache* c) {
   return ts;
 }
 
-static size_t share_workspace_bytes(const sc_plan* p, const sc_cache* c);
+static size_t share_workspace_bytes(const sc_plan* p, const sc_cache* c, bool lse);
 size_t attention_workspace_bytes(const sc_plan* p, const sc_cache* c) {
   if (p->nodes.empty()) return 0;
-  if (p->shared) return share_workspace_bytes(p, c);
+  if (p->shared) return share_workspace_bytes(p, c, false);
   return c->d.dtype == SC_DTYPE_BF16 ? workspace_schedule(p, c).partial_bytes() : 0;
 }
 
@@ -251,10 +251,10 @@ static void shared_order(const sc_plan* p, AttnPlan& plan) {
 }
 
 // The fields of a launch that follow from the plan and the cache alone.
-static AttnGeom attn_geom(const sc_plan* p, const sc_cache* c, int32_t layer, float scale) {
+static LseGeom attn_geom(const sc_plan* p, const sc_cache* c, int32_t layer, float scale) {
   const sc_cache_desc& d = c->d;
-  AttnGeom g;
-  std::memset(&g, 0, sizeof g);
+  LseGeom g;
+  std::memset(static_cast<void*>(&g), 0, sizeof g);
   g.layer_base = c->pool + (size_t)layer * d.n_slots * c->slot_bytes;
   g.slot_bytes = c->slot_bytes;
   g.kv_half = c->kv_half;
@@ -311,14 +311,14 @@ void launch_form<PlainAttn>(const AttnShape& sh, uint32_t items, const AttnGeom&
   }
 }
 
-// Launches a plan by a schedule (unused for fp32 caches); lse: where the rows'
-// logarithmic sums go, or NULL.
-static int launch_scheduled(const sc_plan* p, const sc_cache* c, int32_t layer, const void* q, void* o,
+// Launches a plan by a schedule (unused for fp32 caches); exact: on the LseAttn forms,
+// with lse where the rows' logarithmic sums go, or NULL.
+static int launch_scheduled(const sc_plan* p, const sc_cache* c, int32_t layer, const void* q, void* o, bool exact,
                             float* lse, float scale, void* ws, const AttnSchedule& ts, hipStream_t stream) {
   const sc_cache_desc& d = c->d;
   AttnPlan plan;
   shared_order(p, plan);
-  AttnGeom g = attn_geom(p, c, layer, scale);
+  LseGeom g = attn_geom(p, c, layer, scale);
   g.lse = lse;
   uint32_t items;
   if (d.dtype == SC_DTYPE_F32) {
@@ -339,7 +339,7 @@ static int launch_scheduled(const sc_plan* p, const sc_cache* c, int32_t layer, 
     g.part_ml = g.part_o + (size_t)g.tail_units * g.tail_split * bq * HDB;
     items = (uint32_t)(g.whole_units + g.tail_units * g.tail_split);
   }
-  if (lse) {
+  if (exact) {
     launch_form<LseAttn>(ts.sh, items, g, plan, q, o, d.dtype, d.head_dim, stream);
   } else if (d.dtype == SC_DTYPE_BF16 && ts.sh.bq == WV_BQ) {
     const uint16_t* qb = static_cast<const uint16_t*>(q);
@@ -347,11 +347,11 @@ static int launch_scheduled(const sc_plan* p, const sc_cache* c, int32_t layer, 
     const AttnAhead ahead = take_ahead((int32_t)items, ts.us);
     timer_begin(TK_ATTENTION, stream);
     if (ahead.n)
-      hipLaunchKernelGGL((attn_waves_kernel<AttnAhead>), dim3(kCUs), dim3(64 * WV_NW), 0, stream, qb, ob, g, plan,
-                         ahead);
+      hipLaunchKernelGGL((attn_waves_kernel<AttnAhead>), dim3(kCUs), dim3(64 * WV_NW), 0, stream, qb, ob,
+                         static_cast<const AttnGeom&>(g), plan, ahead);
     else
-      hipLaunchKernelGGL((attn_waves_kernel<NoAhead>), dim3(items), dim3(64 * WV_NW), 0, stream, qb, ob, g, plan,
-                         NoAhead{});
+      hipLaunchKernelGGL((attn_waves_kernel<NoAhead>), dim3(items), dim3(64 * WV_NW), 0, stream, qb, ob,
+                         static_cast<const AttnGeom&>(g), plan, NoAhead{});
     timer_end(TK_ATTENTION, stream);
   } else {
     launch_form<PlainAttn>(ts.sh, items, g, plan, q, o, d.dtype, d.head_dim, stream);
@@ -361,17 +361,22 @@ static int launch_scheduled(const sc_plan* p, const sc_cache* c, int32_t layer, 
 }
 
 // ------------------------------------------------------- a prefix shared by the pack
-// A plan of sc_plan_share runs in one of two ways, whichever is estimated cheaper:
+// A plan of sc_plan_share, and any plan whose rows' logarithmic sums are asked for,
+// runs in one of two ways, whichever is estimated cheaper:
 // its nodes' whole page lists as any plan's (the nodes of long chunks fill their
 // query tiles by themselves, and nothing is left to merge), or as a SharePlan,
 // which reads the prefix once for all rows: a node of few queries leaves most of
 // a query tile empty, and n nodes would read the prefix n times.
 struct ShareSchedule {
+  size_t room = 0;          // it was found for
+  bool lse = false;
   bool whole_lists = false;  // the nodes' whole page lists, by `lists`
   AttnSchedule lists{};
   AttnShape sh{};
-  int32_t p_pieces = 0, own_tiles = 0;  // pieces of the prefix; key tiles per piece of the own pages
-  size_t bytes = 0;                     // its partials
+  int32_t p_tiles = 1, o_tiles = 1;  // key tiles per piece of the prefix and of the own pages
+  int32_t p_pieces = 0, o_pieces = 1;
+  bool own_waves = false;
+  size_t bytes = 0;  // its partials
   double us = 1e30;
 };
 
@@ -389,12 +394,51 @@ static bool lists_fit(const sc_plan* p, const sc_cache* c) {
          (c->d.dtype == SC_DTYPE_F32 || c->d.tokens_per_page >= 32 * attn_shape(p, c).kh);
 }
 
+// Own pages of at most so many 32-key tiles are a wave's work (attn_waves_kernel).
+constexpr int32_t kOwnWaveTiles = 6;
+
+// The time at which `slots` work-groups at once have done classes of items, one class
+// after the other: class k is count[k] items of us[k] each.
+static double makespan(int64_t slots, const double* count, const double* us, int classes) {
+  struct Level {
+    double free, at;  // so many slots are free from this time on
+  } lv[16] = {{(double)slots, 0.0}};
+  int n = 1;
+  double end = 0.0;
+  for (int k = 0; k < classes; ++k)
+    for (double left = count[k]; left > 0;) {
+      int first = 0;
+      for (int i = 1; i < n; ++i)
+        if (lv[i].at < lv[first].at) first = i;
+      const double take = std::min(left, lv[first].free);
+      // whole rounds of the earliest slots at once, as long as no other slot is earlier
+      const double at = lv[first].at + us[k];
+      end = std::max(end, at);
+      left -= take;
+      lv[first].free -= take;
+      int same = -1;
+      for (int i = 0; i < n; ++i)
+        if (lv[i].free > 0 && std::fabs(lv[i].at - at) < 1e-3) same = i;
+      if (same >= 0)
+        lv[same].free += take;
+      else if (lv[first].free <= 0)
+        lv[first] = Level{take, at};
+      else if (n < 16)
+        lv[n++] = Level{take, at};
+      else
+        return end + left * us[k] / slots;
+      if (lv[first].free <= 0 && n > 1) lv[first] = lv[--n];
+    }
+  return end;
+}
+
 // The cheapest way within `room` bytes of partials, by estimated time in us: the
-// items' times as in attn_schedule (fp32: 0.21 us per 16-key tile and 6), dealt
-// out prefix first and the own pages' into the last round's gap; no less than
-// the pages take from HBM at 5 MB per us; the partials written at the same rate
-// and read by the merging kernel, 4 us and 0.2 per MB.
-static ShareSchedule share_schedule(const sc_plan* p, const sc_cache* c, size_t room) {
+// items' times as in attn_schedule (fp32: 0.36 us per 16-key tile of 128 channels and
+// 6), dealt out in their order; no less than the
+// pages take from HBM, at 5 MB per us and 25 KB per us of a CU (what the copies in
+// flight of a work-group fetch); the partials written at the same rate and read by
+// the merging kernel, 4 us and 0.2 per MB.
+static ShareSchedule find_share_schedule(const sc_plan* p, const sc_cache* c, size_t room, bool lse) {
   const sc_cache_desc& d = c->d;
   const bool f32 = d.dtype == SC_DTYPE_F32;
   const int32_t n = (int32_t)p->nodes.size(), H = d.n_heads;
@@ -405,11 +449,13 @@ static ShareSchedule share_schedule(const sc_plan* p, const sc_cache* c, size_t 
     own_max = std::max<int64_t>(own_max, own_pages(p, i));
   }
   ShareSchedule best;
+  best.room = room;
+  best.lse = lse;
   if (lists_fit(p, c)) {
     best.whole_lists = true;
     if (f32) {
       const double tiles = (double)share_tiles(c, {}, (int64_t)p->page_slot.size()) / n;
-      best.us = std::ceil((double)n * H * ((p->nq + F32_BQ - 1) / F32_BQ) / kCUs) * (6.0 + 0.21 * tiles);
+      best.us = std::ceil((double)n * H * ((p->nq + F32_BQ - 1) / F32_BQ) / kCUs) * (6.0 + 0.36 * d.head_dim / 128 * tiles);
     } else {
       best.lists = attn_schedule(p, c, std::min(room, workspace_schedule(p, c).partial_bytes()));
       best.bytes = best.lists.partial_bytes();
@@ -418,36 +464,42 @@ static ShareSchedule share_schedule(const sc_plan* p, const sc_cache* c, size_t 
       best.us = std::max(best.lists.us, (double)p->page_slot.size() * c->slot_bytes / 10e6);
     }
   }
-  const double hbm = (double)(p->shared + own) * c->slot_bytes / 5e6 + 5.0;
+  const double page_bytes = (double)(p->shared + own) * c->slot_bytes;
   const AttnShape forms[] = {{WV_BQ, 1, 1}, {BQ_TINY, 1, 4}, {BQ_SMALL, 2, 2}, {BQ_MAX, 2, 2}};
   for (AttnShape sh : forms) {
     if (f32) sh = AttnShape{F32_BQ, 0, 1};
     if (!f32 && d.tokens_per_page < 32 * sh.kh) continue;
-    const int32_t bq = sh.bq, slots = f32 || bq == WV_BQ ? kCUs : kCUs * per_cu(sh);
-    const double a = f32 ? 0.21 : (bq == BQ_MAX ? 1.5 : bq == BQ_SMALL ? 1.6 : bq == BQ_TINY ? 2.0 : 0.44) * sh.kh / 2;
+    const int32_t bq = sh.bq, per = f32 || bq == WV_BQ ? 1 : per_cu(sh), slots = kCUs * per;
+    const double a = f32 ? 0.36 * d.head_dim / 128 : (bq == BQ_MAX ? 1.5 : bq == BQ_SMALL ? 1.6 : bq == BQ_TINY ? 2.0 : 0.44) * sh.kh / 2;
     const double f = f32 ? 6.0 : bq == BQ_MAX ? 6.0 : bq == BQ_SMALL ? 8.0 : bq == BQ_TINY ? 2.5 : 6.5;
-    const int64_t pt = share_tiles(c, sh, p->shared);
-    const int64_t p_units = (int64_t)H * ((rows + bq - 1) / bq), o_units = (int64_t)H * n * ((p->nq + bq - 1) / bq);
-    for (int64_t P = 1; P <= std::min<int64_t>(pt, 256); P += 1 + P / 16) {
-      const int64_t len = (pt + P - 1) / P;
-      const int64_t most = (share_tiles(c, sh, own_max) + len - 1) / len;
-      const size_t bytes = (size_t)((P + most) * H * rows) * (d.head_dim + 2) * sizeof(float);
-      if (bytes > room || P * p_units + most * o_units > INT32_MAX / 2) continue;
-      const double ot = (double)share_tiles(c, sh, own) / n, op = std::max(1.0, std::ceil(ot / len));
-      const double tp = a * len + f, to = a * ot / op + f, o_items = (double)o_units * op;
-      const int64_t items = P * p_units, full = items / slots, rest = items % slots;
-      double us = (double)full * tp;
-      const double gap = rest ? (double)(slots - rest) * tp : 0.0;
-      if (rest) us += tp;
-      if (o_items * to > gap) us += std::ceil((o_items * to - gap) / (slots * to)) * to;
-      us = std::max(us, hbm) + (double)bytes / 5e6 + 4.0 + 0.2e-6 * (double)bytes;
-      if (us < best.us - 1e-9) {
+    const int64_t pt = p->shared ? share_tiles(c, sh, p->shared) : 0, ot_max = share_tiles(c, sh, own_max);
+    const double p_units = p->shared ? (double)H * ((rows + bq - 1) / bq) : 0.0;
+    const double o_units = (double)H * n * ((p->nq + bq - 1) / bq);
+    const bool waves = p->shared && bq == WV_BQ && ot_max <= kOwnWaveTiles;
+    const int64_t cut = pt ? pt : ot_max;
+    // lengths of a piece: the whole segment, then shorter by an eighth or so each
+    for (int64_t len = cut; len >= 1; len -= std::max<int64_t>(1, len / 16)) {
+      const int64_t pp = (pt + len - 1) / len, oo = waves ? 1 : (ot_max + len - 1) / len;
+      const size_t bytes = (size_t)((pp + oo) * H * rows) * (d.head_dim + 2) * sizeof(float);
+      if (bytes > room || pp * p_units + oo * o_units > INT32_MAX / 2) continue;
+      const double ot = (double)share_tiles(c, sh, own) / n;
+      const double count[] = {(double)(pt / len) * p_units, pt % len ? p_units : 0.0,
+                              waves ? std::ceil(o_units / WV_NW) : o_units * std::ceil(ot / len)};
+      const double us[] = {a * len + f, a * (double)(pt % len) + f,
+                           waves ? 6.0 + 0.9 * ot : a * std::min<double>(len, ot) + f};
+      const double cus = std::min<double>(kCUs, std::ceil((pt ? pp * p_units : count[2]) / per));
+      const double t = std::max(makespan(slots, count, us, 3), page_bytes / std::min(5e6, 25e3 * cus) + 3.0) +
+                       (double)bytes / 5e6 + 4.0 + 0.2e-6 * (double)bytes;
+      if (t < best.us - 1e-9) {
         best.whole_lists = false;
         best.sh = sh;
-        best.p_pieces = (int32_t)P;
-        best.own_tiles = (int32_t)len;
+        best.p_tiles = (int32_t)len;
+        best.o_tiles = (int32_t)(waves ? ot_max : len);
+        best.p_pieces = (int32_t)pp;
+        best.o_pieces = (int32_t)oo;
+        best.own_waves = waves;
         best.bytes = bytes;
-        best.us = us;
+        best.us = t;
       }
     }
     if (f32) break;
@@ -455,8 +507,19 @@ static ShareSchedule share_schedule(const sc_plan* p, const sc_cache* c, size_t 
   return best;
 }
 
-static size_t share_workspace_bytes(const sc_plan* p, const sc_cache* c) {
-  return share_schedule(p, c, attention_workspace_bound()).bytes;
+// Found once per plan, for the few rooms that its calls ask for.
+static const ShareSchedule& share_schedule(const sc_plan* p, const sc_cache* c, size_t room, bool lse) {
+  for (const auto& s : p->share)
+    if (s->room == room && s->lse == lse) return *s;
+  p->share.push_back(std::make_shared<ShareSchedule>(find_share_schedule(p, c, room, lse)));
+  return *p->share.back();
+}
+
+static size_t share_workspace_bytes(const sc_plan* p, const sc_cache* c, bool lse) {
+  return share_schedule(p, c, attention_workspace_bound(), lse).bytes;
+}
+size_t attention_lse_workspace_bytes(const sc_plan* p, const sc_cache* c) {
+  return p->nodes.empty() ? 0 : share_workspace_bytes(p, c, true);
 }
 
 // Neither way fits: more pages in the lists than a launch takes, and more rows
@@ -471,35 +534,35 @@ static int share_check(const sc_plan* p, const sc_cache* c) {
 
 static int launch_share(const sc_plan* p, const sc_cache* c, int32_t layer, const void* q, void* o, float* lse,
                         float scale, void* ws, const ShareSchedule& s, hipStream_t stream) {
-  if (s.whole_lists) return launch_scheduled(p, c, layer, q, o, lse, scale, ws, s.lists, stream);
+  if (s.whole_lists) return launch_scheduled(p, c, layer, q, o, true, lse, scale, ws, s.lists, stream);
   if (reinterpret_cast<uintptr_t>(ws) & 15) return fail(SC_EINVAL, "workspace must be 16-byte aligned");
   const sc_cache_desc& d = c->d;
-  AttnGeom g = attn_geom(p, c, layer, scale);
+  LseGeom g = attn_geom(p, c, layer, scale);
   SharePlan plan;
   g.lse = lse;
   g.p_qtiles = (g.rows + s.sh.bq - 1) / s.sh.bq;
   g.n_qtiles = (p->nq + s.sh.bq - 1) / s.sh.bq;
   g.p_pieces = s.p_pieces;
+  g.p_tiles = s.p_tiles;
+  g.p_full = p->shared ? (int32_t)(share_tiles(c, s.sh, p->shared) / s.p_tiles) : 0;
+  g.o_pieces = s.o_pieces;
+  g.o_tiles = s.o_tiles;
+  g.own_waves = s.own_waves;
   std::copy(p->page_slot.begin(), p->page_slot.begin() + p->shared, plan.page_slot);
   int32_t pages = p->shared;
-  int64_t items = (int64_t)g.p_pieces * g.p_qtiles * d.n_heads;
-  int64_t most = 0;
-  plan.page_off[0] = plan.item_off[0] = 0;
+  plan.page_off[0] = 0;
   for (int32_t i = 0; i < g.n_nodes; ++i) {
     plan.page_off[i + 1] = pages;
-    plan.item_off[i + 1] = (int32_t)items;
     std::copy(p->page_slot.begin() + p->page_off[i] + p->shared, p->page_slot.begin() + p->page_off[i + 1],
               plan.page_slot + pages);
     pages += own_pages(p, i);
-    const int64_t pieces = (share_tiles(c, s.sh, own_pages(p, i)) + s.own_tiles - 1) / s.own_tiles;
-    most = std::max(most, pieces);
-    items += pieces * g.n_qtiles * d.n_heads;
   }
-  for (int32_t i = g.n_nodes + 1; i <= kMaxNodes; ++i) plan.item_off[i] = INT32_MAX;
-  plan.item_off[kMaxNodes + 1] = (int32_t)items;
   for (int32_t i = g.n_nodes + 1; i <= kMaxNodes + 1; ++i) plan.page_off[i] = pages;
+  const int64_t o_units = (int64_t)g.n_nodes * g.n_qtiles * d.n_heads;
+  const int64_t items = (int64_t)g.p_pieces * g.p_qtiles * d.n_heads +
+                        (s.own_waves ? (o_units + WV_NW - 1) / WV_NW : o_units * g.o_pieces);
   g.part_o = static_cast<float*>(ws);
-  g.part_ml = g.part_o + (size_t)(g.p_pieces + most) * d.n_heads * g.rows * d.head_dim;
+  g.part_ml = g.part_o + (size_t)(g.p_pieces + g.o_pieces) * d.n_heads * g.rows * d.head_dim;
   launch_form<ShareAttn>(s.sh, (uint32_t)items, g, plan, q, o, d.dtype, d.head_dim, stream);
   SC_HIP(hipGetLastError());
   return SC_OK;
@@ -509,13 +572,14 @@ int launch_attention_lse(const sc_plan* p, const sc_cache* c, int32_t layer, con
                          float scale, void* ws, size_t ws_bytes, hipStream_t stream) {
   const int rc = attention_check(p, c);
   if (rc != SC_OK) return rc;
-  const size_t need = attention_workspace_bytes(p, c);
+  const size_t need = lse ? attention_lse_workspace_bytes(p, c) : attention_workspace_bytes(p, c);
   if (ws_bytes < need || (need && !ws))
     return fail(SC_EINVAL, "attention workspace of %zu bytes, need %zu", ws_bytes, need);
-  if (p->shared)
-    return launch_share(p, c, layer, q, o, lse, scale, ws, share_schedule(p, c, attention_workspace_bound()), stream);
+  if (p->shared || lse)
+    return launch_share(p, c, layer, q, o, lse, scale, ws, share_schedule(p, c, attention_workspace_bound(), lse),
+                        stream);
   const AttnSchedule ts = c->d.dtype == SC_DTYPE_F32 ? AttnSchedule{} : attn_schedule(p, c, need);
-  return launch_scheduled(p, c, layer, q, o, lse, scale, ws, ts, stream);
+  return launch_scheduled(p, c, layer, q, o, false, nullptr, scale, ws, ts, stream);
 }
 
 int launch_attention(const sc_plan* p, const sc_cache* c, int32_t layer, const void* q, void* o,
@@ -537,7 +601,7 @@ extern "C" int sc_attention_form(const sc_plan* p, const sc_cache* c, int32_t* q
   *ring = *pieces = 1;
   AttnSchedule ts{};
   if (p->shared) {
-    const ShareSchedule s = share_schedule(p, c, attention_workspace_bound());
+    const ShareSchedule& s = share_schedule(p, c, attention_workspace_bound(), false);
     if (!s.whole_lists) {
       *queries = s.sh.bq;
       *ring = s.sh.ring;
@@ -600,11 +664,11 @@ extern "C" int sc_attention_noalloc(const sc_plan* p, const sc_cache* c, int32_t
   void* ptr = nullptr;
   if ((p->shared || c->d.dtype == SC_DTYPE_BF16) && (rc = scratch_address(&ptr)) != SC_OK) return rc;
   if (p->shared) {
-    const ShareSchedule s = share_schedule(p, c, kNoAllocScratchBytes);
+    const ShareSchedule& s = share_schedule(p, c, kNoAllocScratchBytes, false);
     if (s.us >= 1e30) return fail(SC_ECAPACITY, "the rows sharing a prefix need more partials than the scratch holds");
     return launch_share(p, c, layer, q, o, nullptr, scale, ptr, s, static_cast<hipStream_t>(stream));
   }
   AttnSchedule ts{};
   if (ptr) ts = attn_schedule(p, c, std::min(kNoAllocScratchBytes, attention_workspace_bytes(p, c)));
-  return launch_scheduled(p, c, layer, q, o, nullptr, scale, ptr, ts, static_cast<hipStream_t>(stream));
+  return launch_scheduled(p, c, layer, q, o, false, nullptr, scale, ptr, ts, static_cast<hipStream_t>(stream));
 }

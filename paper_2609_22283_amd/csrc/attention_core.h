@@ -20,11 +20,10 @@ struct AttnPlan {
 // A pack whose nodes read a common prefix before pages of their own.  Its key
 // segments are numbered like nodes: segment 0 is the prefix, read by the rows of all
 // nodes as one matrix, segment 1 + i the own pages of node i.  Each segment's
-// key range is cut into pieces, and every piece leaves a partial; item_off[s]:
-// the first work item of segment s (INT32_MAX past the last segment).
+// key tiles are cut into pieces of equal length (the last one shorter), and every
+// piece leaves a partial.
 struct SharePlan {
   int32_t page_off[kMaxNodes + 2];
-  int32_t item_off[kMaxNodes + 2];
   int32_t page_slot[kMaxPages];
 };
 
@@ -40,12 +39,19 @@ struct AttnGeom {
   float* part_o;          // [tail_units * tail_split][BQ][128] unnormalised partial outputs
   float* part_ml;         // [tail_units * tail_split][2][BQ] partial max (log2 units) and sum
                           // (BQ: queries per work-group of the instantiation launched)
-  // only the forms that give the rows' logarithmic sums (LseAttn, ShareAttn):
+};
+
+// What the forms that give the rows' logarithmic sums (LseAttn, ShareAttn) need beside.
+struct LseGeom : AttnGeom {
   float* lse;             // [head][row] log2 (fp32 caches: natural log) of the row's sum, or null
   float unit;             // |scale| log2(e); fp32 caches: 1
   uint32_t q_flip;        // bf16: sign bits of a negative scale
   int32_t rows;           // rows of the pack, n_nodes * nq
-  int32_t p_qtiles, p_pieces;  // ShareAttn: query tiles and key pieces of the prefix
+  // ShareAttn: query tiles of the prefix; pieces and tiles per piece of the prefix, and
+  // the most pieces and tiles per piece of own pages
+  int32_t p_qtiles, p_pieces, p_tiles, o_pieces, o_tiles;
+  int32_t p_full;              // pieces of the prefix of full length (p_pieces, or one less)
+  int32_t own_waves;           // ShareAttn: a wave to itself for each node, head and query tile (attn_waves_kernel)
   DivMagic nq_div;
 };
 
@@ -57,16 +63,24 @@ struct AttnGeom {
 //   ShareAttn  the same over a SharePlan
 struct PlainAttn {
   using Plan = AttnPlan;
+  using Geom = AttnGeom;
   static constexpr bool kLse = false, kShare = false;
 };
 struct LseAttn {
   using Plan = AttnPlan;
+  using Geom = LseGeom;
   static constexpr bool kLse = true, kShare = false;
 };
 struct ShareAttn {
   using Plan = SharePlan;
+  using Geom = LseGeom;
   static constexpr bool kLse = true, kShare = true;
 };
+template <class M>
+__device__ __forceinline__ float unit_of(const typename M::Geom& g) {
+  if constexpr (M::kLse) return g.unit;
+  return 1.f;
+}
 
 struct AttnItem {
   int32_t head, node, qt;
@@ -75,6 +89,21 @@ struct AttnItem {
   int32_t slot;     // partial slot, or -1 for a whole unit
   int32_t row0, rows;  // ShareAttn: the segment's first row and its rows
 };
+
+// The item's fields in scalar registers: out of divisions they come in vector ones, which
+// the long-context forms have none of to spare (eight spilled registers in the loop
+// cost them a third: a reload waits for every copy in flight).
+__device__ __forceinline__ void in_scalars(AttnItem& it) {
+  it.head = __builtin_amdgcn_readfirstlane(it.head);
+  it.node = __builtin_amdgcn_readfirstlane(it.node);
+  it.qt = __builtin_amdgcn_readfirstlane(it.qt);
+  it.ta = __builtin_amdgcn_readfirstlane(it.ta);
+  it.tb = __builtin_amdgcn_readfirstlane(it.tb);
+  it.ntiles = __builtin_amdgcn_readfirstlane(it.ntiles);
+  it.slot = __builtin_amdgcn_readfirstlane(it.slot);
+  it.row0 = __builtin_amdgcn_readfirstlane(it.row0);
+  it.rows = __builtin_amdgcn_readfirstlane(it.rows);
+}
 
 // First row of an item's node or segment, and its rows.
 template <class M>
@@ -86,44 +115,85 @@ __device__ __forceinline__ int32_t item_rows(const AttnItem& it, const AttnGeom&
   return M::kShare ? it.rows : g.nq;
 }
 
-// Items of a SharePlan: the prefix's first (the long ones), each part remapped on
-// its own so that every XCD gets its share of both.  Query tiles fastest: the
-// work-groups that read one piece of the keys run side by side.  Key tiles are of
-// 32 KH keys of the concatenated pages, or (KH 0, the fp32 kernel) of 16 keys of one.
+// Key tiles of a SharePlan's segment: of 32 KH keys of the concatenated pages, or
+// (KH 0, the fp32 kernel) of 16 keys of one page.
 template <int KH>
-__device__ __forceinline__ AttnItem decode_item(const SharePlan& plan, const AttnGeom& g, uint32_t b) {
+__device__ __forceinline__ int32_t share_tiles(const SharePlan& plan, const AttnGeom& g, int32_t seg) {
+  const int32_t npages = plan.page_off[seg + 1] - plan.page_off[seg];
+  return KH ? (npages * g.tpp + 32 * KH - 1) / (32 * (KH ? KH : 1)) : npages * ((g.tpp + 15) / 16);
+}
+
+// Items of a SharePlan: the prefix's full pieces, its shorter last ones, the own
+// pages'; each kind remapped on its own, since a work-group's XCD is fixed by its
+// number and every XCD has to get its share of each.  Query tiles fastest, then (own pages) nodes:
+// the work-groups that an XCD runs side by side read the same keys.  A piece past
+// the end of a short list is empty (ta == tb).
+template <int KH>
+__device__ __forceinline__ AttnItem decode_item(const SharePlan& plan, const LseGeom& g, uint32_t b) {
   AttnItem it;
-  const uint32_t n0 = (uint32_t)plan.item_off[1];
-  int32_t local, qtiles, pieces;
+  const uint32_t n0 = (uint32_t)(g.p_pieces * g.p_qtiles * g.n_heads);
+  int32_t piece, len;
   if (b < n0) {
-    local = (int32_t)xcd_remap(b, n0);
+    const uint32_t full = (uint32_t)(g.p_full * g.p_qtiles * g.n_heads);
+    const int32_t i = (int32_t)(b < full ? xcd_remap(b, full) : full + xcd_remap(b - full, n0 - full));
+    const int32_t unit = i % (g.p_qtiles * g.n_heads);
+    piece = i / (g.p_qtiles * g.n_heads);
+    it.qt = unit % g.p_qtiles;
+    it.head = unit / g.p_qtiles;
     it.node = 0;
     it.row0 = 0;
     it.rows = g.rows;
-    qtiles = g.p_qtiles;
-    pieces = g.p_pieces;
+    it.slot = piece;
+    len = g.p_tiles;
   } else {
-    const int32_t i = (int32_t)(n0 + xcd_remap(b - n0, gridDim.x - n0));
-    const int32_t lane = threadIdx.x & 63;
-    it.node = __builtin_popcountll(__builtin_amdgcn_ballot_w64(plan.item_off[1 + lane] <= i));
-    const int32_t first = plan.item_off[it.node];
-    local = i - first;
+    const int32_t i = (int32_t)xcd_remap(b - n0, gridDim.x - n0), per = g.n_qtiles * g.n_nodes;
+    const int32_t unit = i % (per * g.n_heads);
+    piece = i / (per * g.n_heads);
+    it.qt = unit % g.n_qtiles;
+    it.node = 1 + unit / g.n_qtiles % g.n_nodes;
+    it.head = unit / per;
     it.row0 = (it.node - 1) * g.nq;
     it.rows = g.nq;
-    qtiles = g.n_qtiles;
-    const int32_t end = it.node == g.n_nodes ? (int32_t)gridDim.x : plan.item_off[it.node + 1];
-    pieces = (end - first) / (qtiles * g.n_heads);
+    it.slot = g.p_pieces + piece;
+    len = g.o_tiles;
   }
-  it.qt = local % qtiles;
-  it.head = local / qtiles % g.n_heads;
-  const int32_t piece = local / qtiles / g.n_heads;
-  it.slot = (it.node == 0 ? 0 : g.p_pieces) + piece;
-  const int32_t npages = plan.page_off[it.node + 1] - plan.page_off[it.node];
-  it.ntiles = KH ? (npages * g.tpp + 32 * KH - 1) / (32 * KH) : npages * ((g.tpp + 15) / 16);
-  it.ta = (int32_t)((int64_t)piece * it.ntiles / pieces);
-  it.tb = (int32_t)((int64_t)(piece + 1) * it.ntiles / pieces);
+  it.ntiles = share_tiles<KH>(plan, g, it.node);
+  it.ta = min(piece * len, it.ntiles);
+  it.tb = min(it.ta + len, it.ntiles);
   return it;
 }
+
+// Direct global -> LDS copy of 16 bytes per lane (gfx950 LDS DMA): lane i
+// of the wave writes bytes [16 i, 16 i + 16) after the wave-uniform LDS
+// address, so the XOR swizzle is applied by choosing each lane's source
+// (base + off).  Written as inline asm: while a copy it knows of is in
+// flight, the compiler waits for every LDS read with lgkmcnt(0), so no
+// fragment read could overlap another; the copies themselves complete
+// under this wave's explicit vmcnt waits (landed, landed_but).  M0, which
+// carries the LDS address, is saved and restored.
+__device__ __forceinline__ uint32_t lds_addr(const char* p) {
+  return (uint32_t)reinterpret_cast<uintptr_t>(p);
+}
+__device__ __forceinline__ void dma16(const char* base, uint32_t off, char* lds_wave_base) {
+  uint32_t saved;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %3\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %1, %2\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "v"(off), "s"(base), "s"(lds_addr(lds_wave_base))
+      : "memory");
+}
+
+// All but this wave's N newest copies have landed.
+template <int N>
+__device__ __forceinline__ void copies_landed() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+// This wave's LDS reads are done: what they read may be copied over.
+__device__ __forceinline__ void reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 // ------------------------------------------------------------- fp32 kernel
 // Work-group: 16 queries of one (node, head).  Its eight waves take eight
@@ -145,20 +215,30 @@ __device__ __forceinline__ AttnItem decode_item(const SharePlan& plan, const Att
 // 40 waves in flight and a chain of 128 dependent FMAs per key.
 // 4 nodes x 312 queries x 2184 keys, 2 heads of 128: 61 us (46 TFLOP/s; 59 before
 // the values behind a page's end were cleared) against 15.6 ms.
+// STAGED (pages on 16-byte boundaries): each wave copies its tiles into LDS, K(t + 1)
+// over K(t) once that has been read and V(t + 1) likewise, and takes the operands from
+// there.  The loads above put adjacent lanes on adjacent rows, so each of their 16
+// bytes is a cache access of its own.  16 x 100 rows over 12384 keys, 12 heads of 64:
+// 669 us (91 TFLOP/s of 154), 834 without.
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 constexpr int F32_NW = 8, F32_BQ = 16, F32_BK = 16;
 
-template <int HD, class M = PlainAttn>
+template <int HD, class M = PlainAttn, bool STAGED = false>
 __global__ __launch_bounds__(64 * F32_NW) void attn_f32_kernel(const float* __restrict__ q, float* __restrict__ o,
-                                                               AttnGeom g, typename M::Plan plan) {
+                                                               typename M::Geom g, typename M::Plan plan) {
   constexpr int NJ = HD / 16;  // 16-channel blocks
-  __shared__ f32x4 part[F32_NW / 2][NJ][64];
+  constexpr int ROW = HD * 4, TILE = F32_BK * ROW, CP = TILE / 1024;  // a K or V^T tile, its copies
+  constexpr int PART = F32_NW / 2 * NJ * 64 * 16;
+  __shared__ __attribute__((aligned(1024))) char smem[STAGED ? F32_NW * 2 * TILE : PART];
+  static_assert(!STAGED || PART <= F32_NW * 2 * TILE, "the merge fits the tiles");
+  f32x4(*const part)[NJ][64] = reinterpret_cast<f32x4(*)[NJ][64]>(smem);
   __shared__ float ml[2][F32_NW][F32_BQ];
   const int32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int32_t lg = lane >> 4, c = lane & 15;
   AttnItem it;
   if constexpr (M::kShare) {
     it = decode_item<0>(plan, g, blockIdx.x);
+    if (it.ta == it.tb) return;
   } else {
     // query tiles fastest: an XCD's work-groups share the K/V of one or two (node, head)s
     const int32_t unit = (int32_t)xcd_remap(blockIdx.x, gridDim.x);
@@ -196,13 +276,46 @@ __global__ __launch_bounds__(64 * F32_NW) void attn_f32_kernel(const float* __re
 #pragma unroll
     for (int j = 0; j < NJ; ++j) kf[j] = *reinterpret_cast<const f32x4u*>(kb + 16 * j);
   };
+  // STAGED: 16-byte columns are swizzled by the row (K: its number, V^T: a quarter of it)
+  char* const kl = smem + wave * 2 * TILE;
+  char* const vl = kl + TILE;
+  const auto slot_base = [&](int32_t pg) { return g.layer_base + (size_t)plan.page_slot[p0 + pg] * g.slot_bytes; };
+  const auto stage_k = [&]() __attribute__((always_inline)) {
+    constexpr int LPR = ROW / 16;  // lanes per row
+    const char* base = slot_base(page) + (size_t)head * g.tpp * ROW;
+#pragma unroll
+    for (int j = 0; j < CP; ++j) {
+      const int32_t r = (64 / LPR) * j + lane / LPR, col = (lane % LPR) ^ r;
+      dma16(base, (uint32_t)min(F32_BK * tt + r, g.tpp - 1) * ROW + 16 * col, kl + 1024 * j);
+    }
+  };
+  const auto stage_v = [&]() __attribute__((always_inline)) {
+    const char* base = slot_base(page) + g.kv_half + (size_t)head * g.tpp * ROW;
+#pragma unroll
+    for (int j = 0; j < CP; ++j) {
+      const int32_t d = 16 * j + (lane >> 2), key = F32_BK * tt + 4 * ((lane & 3) ^ (d >> 2 & 3));
+      dma16(base, ((uint32_t)d * g.tpp + (key < g.tpp ? key : 0)) * 4, vl + 1024 * j);
+    }
+  };
   float m = -INFINITY, l = 0.f;
   f32x4 kf[NJ];
-  if (t < t_end) load_k(kf);
+  if (t < t_end) {
+    if constexpr (STAGED) {
+      stage_k();
+      stage_v();
+    } else {
+      load_k(kf);
+    }
+  }
   while (t < t_end) {
     const int32_t k0 = F32_BK * tt + 4 * lg;  // this lane's first key of the tile, within the page
     f32x4 vf[NJ];
-    {
+    if constexpr (STAGED) {
+      copies_landed<CP>();  // K(t); V(t) may still be under way
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) kf[j] = *reinterpret_cast<const f32x4*>(kl + c * ROW + (((4 * j + lg) ^ c) << 4));
+      reads_done();
+    } else {
       const float* vb = reinterpret_cast<const float*>(g.layer_base + (size_t)plan.page_slot[p0 + page] * g.slot_bytes +
                                                        g.kv_half) +
                         ((size_t)head * HD + c) * g.tpp + (k0 < g.tpp ? k0 : 0);
@@ -223,7 +336,13 @@ __global__ __launch_bounds__(64 * F32_NW) void attn_f32_kernel(const float* __re
       tt = 0;
       ++page;
     }
-    if (t < t_end) load_k(kf);
+    const bool more = t < t_end;
+    if (more) {
+      if constexpr (STAGED)
+        stage_k();
+      else
+        load_k(kf);
+    }
     f32x4 s = s0 + s1;
     if (k0 + 4 > g.tpp) s = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};  // pages hold whole runs of 8 keys
     float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
@@ -242,6 +361,16 @@ __global__ __launch_bounds__(64 * F32_NW) void attn_f32_kernel(const float* __re
 #pragma unroll
     for (int e = 0; e < 4; ++e) p[e] = expf(s[e] - ms);
     l += (p[0] + p[1]) + (p[2] + p[3]);
+    if constexpr (STAGED) {
+      if (more)
+        copies_landed<CP>();  // V(t); K(t + 1) may still be under way
+      else
+        copies_landed<0>();
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) vf[j] = *reinterpret_cast<const f32x4*>(vl + (16 * j + c) * 64 + ((lg ^ (c >> 2)) << 4));
+      reads_done();
+      if (more) stage_v();
+    }
     if (page_end && k0 >= g.tpp)
 #pragma unroll
       for (int j = 0; j < NJ; ++j) vf[j] = f32x4{};
@@ -251,7 +380,7 @@ __global__ __launch_bounds__(64 * F32_NW) void attn_f32_kernel(const float* __re
       for (int j = 0; j < NJ; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[j][e], p[e], acc[j], 0, 0, 0);
   }
   // merge: every wave scales its part to the common maximum, then a tree of
-  // LDS additions (a wave without tiles adds zeros)
+  // LDS additions (a wave without tiles adds zeros), over the tiles
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
   if (lg == 0) {
@@ -295,7 +424,7 @@ __global__ __launch_bounds__(64 * F32_NW) void attn_f32_kernel(const float* __re
   if (wave == 0 && row < g.nq) {
     const float inv = 1.f / lt;
     if constexpr (M::kLse)
-      if (lg == 0) g.lse[(size_t)head * g.rows + row0 + row] = mt + logf(lt);
+      if (g.lse && lg == 0) g.lse[(size_t)head * g.rows + row0 + row] = mt + logf(lt);
 #pragma unroll
     for (int j = 0; j < NJ; ++j) *reinterpret_cast<f32x4u*>(o + qoff + 16 * j) = acc[j] * inv;
   }
@@ -350,7 +479,11 @@ __device__ __forceinline__ uint32_t kswz(int32_t row) { return (uint32_t)((row &
 
 struct AttnLane {
   // per-lane LDS read offsets (bytes) inside one buffer
-  uint32_t koff[2][4];  // K row of block b, 16-byte column 4 ds + g (second 32 rows add 8192)
+  // K row of block 0, 16-byte column 4 ds + g (second 32 rows add 8192).  Block 1's
+  // rows lie 4 below, which flips bit 2 of the swizzle: its column 4 ds + g is
+  // stored where block 0's column 4 (ds ^ 1) + g is, 1024 bytes on.
+  uint32_t koff[4];
+  __device__ __forceinline__ uint32_t k(int b, int ds) const { return koff[ds ^ b] + 1024u * b; }
   uint32_t voff[2];     // V^T row c, 16-byte column 4 h + g (16-row block db adds 32 BK)
 };
 
@@ -369,12 +502,9 @@ __device__ __forceinline__ uint32_t vswz(int32_t d) {
 template <int KH>
 __device__ __forceinline__ AttnLane attn_lane(int32_t c, int32_t g) {
   AttnLane L;
+  const int32_t row = 8 * (c >> 2) + (c & 3);
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    const int32_t row = 8 * (c >> 2) + 4 * b + (c & 3);
-#pragma unroll
-    for (int ds = 0; ds < 4; ++ds) L.koff[b][ds] = row * 256 + (((4 * ds + g) ^ kswz(row)) << 4);
-  }
+  for (int ds = 0; ds < 4; ++ds) L.koff[ds] = row * 256 + (((4 * ds + g) ^ kswz(row)) << 4);
 #pragma unroll
   for (int h = 0; h < 2; ++h)
     L.voff[h] = c * (64 * KH) + (((4 * h + g) ^ vswz<KH>(c)) << 4);  // h < KH only is used
@@ -396,7 +526,7 @@ __device__ __forceinline__ void load_q(const uint16_t* q, const AttnGeom& g, siz
 // The forms with logarithmic sums keep the values and scale the logits instead, by
 // |scale|: only the sign goes into q.
 template <class M>
-__device__ __forceinline__ void scale_q(const AttnGeom& g, bf16x8 (&qreg)[4]) {
+__device__ __forceinline__ void scale_q(const typename M::Geom& g, bf16x8 (&qreg)[4]) {
   if constexpr (M::kLse) {
 #pragma unroll
     for (int ds = 0; ds < 4; ++ds) {
@@ -483,6 +613,8 @@ __device__ __forceinline__ void probs(const STile<KH>& s, bf16x8 (&pb)[KH][2]) {
 }
 
 // p = exp2(unit s): this lane's sums of the unrounded values are added to l.
+// (Taking the maximum off here, by an fma, instead of in the products' accumulators
+// was 1 % slower.)
 template <int KH>
 __device__ __forceinline__ void probs_sum(const STile<KH>& s, float unit, bf16x8 (&pb)[KH][2], float (&l)[2]) {
 #pragma unroll
@@ -523,30 +655,6 @@ __device__ __forceinline__ void probs_tile(const STile<KH>& s, bf16x8 (&pb)[KH][
   }
 }
 
-// Direct global -> LDS copy of 16 bytes per lane (gfx950 LDS DMA): lane i
-// of the wave writes bytes [16 i, 16 i + 16) after the wave-uniform LDS
-// address, so the XOR swizzle is applied by choosing each lane's source
-// (base + off).  Written as inline asm: while a copy it knows of is in
-// flight, the compiler waits for every LDS read with lgkmcnt(0), so no
-// fragment read could overlap another; the copies themselves complete
-// under this wave's explicit vmcnt waits (landed, landed_but).  M0, which
-// carries the LDS address, is saved and restored.
-__device__ __forceinline__ uint32_t lds_addr(const char* p) {
-  return (uint32_t)reinterpret_cast<uintptr_t>(p);
-}
-__device__ __forceinline__ void dma16(const char* base, uint32_t off, char* lds_wave_base) {
-  uint32_t saved;
-  asm volatile(
-      "s_mov_b32 %0, m0\n\t"
-      "s_mov_b32 m0, %3\n\t"
-      "s_nop 0\n\t"
-      "global_load_lds_dwordx4 %1, %2\n\t"
-      "s_mov_b32 m0, %0"
-      : "=&s"(saved)
-      : "v"(off), "s"(base), "s"(lds_addr(lds_wave_base))
-      : "memory");
-}
-
 // Copies of BK-key K and V^T tiles of one (node, head) from the paged cache
 // into LDS, split over the NW waves of a work-group.  A tile spans at most
 // two pages (pages hold >= BK tokens), so the page of a key is chosen against
@@ -575,8 +683,12 @@ struct KvTiles {
   int32_t npages, nk, tpp, wave;
   uint32_t slot_bytes, khead, vhead, kbad;
   DivMagic tpp_div;
-  uint32_t klane[KCP], vlane[VCP];
-  int32_t vkey[VCP], krow0;
+  // Lane offsets of the copies.  Both swizzles are XORs of bits of the row, and copy j
+  // adds its own bits to rows that have none there: its offset is the first copy's
+  // with a constant XORed in, which costs no register.
+  uint32_t kl0;      // K: the first row's bytes and the swizzled column
+  uint32_t vl[KH];   // V^T: rows of even and odd copies (their swizzles alternate), with the key's bytes
+  int32_t vk0;       // key offset in the tile, of even copies
 
   template <class Plan>
   __device__ __forceinline__ KvTiles(const Plan& plan, const AttnGeom& g, int32_t node, int32_t head,
@@ -593,21 +705,16 @@ struct KvTiles {
     khead = (uint32_t)head * tpp * HDB * 2;
     vhead = (uint32_t)g.kv_half + (uint32_t)head * HDB * tpp * 2;
     kbad = (uint32_t)page_slot[npages - 1] * slot_bytes + khead + (uint32_t)(tpp - 1) * 256;
-    krow0 = 4 * KCP * wave + (lane >> 4);
-    const int32_t kp = lane & 15;
+    const int32_t krow0 = 4 * KCP * wave + (lane >> 4), kp = lane & 15;
+    kl0 = (uint32_t)krow0 * 256 + ((kp ^ kswz(krow0)) << 4);  // plus key t0 * 256
     const int32_t vrow0 = RPI * VCP * wave + (lane >> (KH + 1)), vp = lane & (LPR - 1);  // LPR = 2^(KH+1)
+    vk0 = 8 * (vp ^ (int32_t)vswz<KH>(vrow0));
 #pragma unroll
-    for (int j = 0; j < KCP; ++j) {
-      const int32_t row = krow0 + 4 * j;
-      klane[j] = (uint32_t)row * 256 + ((kp ^ kswz(row)) << 4);  // plus key t0 * 256
-    }
-#pragma unroll
-    for (int j = 0; j < VCP; ++j) {
-      const int32_t d = vrow0 + RPI * j;
-      vkey[j] = 8 * (vp ^ (int32_t)vswz<KH>(d));                     // key offset in tile
-      vlane[j] = (uint32_t)d * tpp * 2 + (uint32_t)vkey[j] * 2;      // plus key t0 * 2
-    }
+    for (int j = 0; j < KH; ++j) vl[j] = (uint32_t)vrow0 * tpp * 2 + (uint32_t)vkey(j) * 2;  // plus key t0 * 2
   }
+  __device__ __forceinline__ int32_t vkey(int j) const { return KH == 2 ? vk0 ^ (32 * (j & 1)) : vk0; }
+  // Offset of K copy j from that of the first (kl: kl0).
+  static __device__ __forceinline__ uint32_t klane(uint32_t kl, int j) { return kl ^ (kswz(4 * j) << 4); }
   // Page slots of the tile starting at key t0 >= 0 (two scalar loads),
   // fetched ahead of the copy that uses them so their latency overlaps other
   // work (a step, or the barrier wait before the copy).  Clamped to the
@@ -629,17 +736,20 @@ struct KvTiles {
     const uint32_t lo = sl.lo + khead + (uint32_t)(t0 - sl.plo * tpp) * 256;
     const uint32_t hi = sl.hi + khead + (uint32_t)(t0 - bkey) * 256;
     const int32_t lim = nk - t0, split = bkey - t0;
+    uint32_t k = kl0;
+    asm volatile("" : "+v"(k));  // the offsets are made here, not kept
 #pragma unroll
     for (int j = 0; j < KCP; ++j) {
       const int32_t rg = 4 * KCP * wave + 4 * j;  // first tile row of this copy (wave-uniform)
-      const uint32_t src = rg >= lim ? kbad + (klane[j] & 255u) : (rg >= split ? hi : lo) + klane[j];
-      dma16(lbase, src, kl + rg * 256);
+      const bool past = rg >= lim;
+      const uint32_t base = past ? kbad : (rg >= split ? hi : lo) + 1024u * j;
+      dma16(lbase, base + (klane(k, j) & (past ? 255u : ~0u)), kl + rg * 256);
     }
   }
   // A V^T row holds the tile's BK keys; a page boundary or the node's end
   // falls inside the tile for about one tile in a page, so the per-lane
   // choice is taken only then (wave-uniform branch).
-  __device__ __forceinline__ void copy_v(int32_t t0, char* vl, const Slots& sl) const {
+  __device__ __forceinline__ void copy_v(int32_t t0, char* vt, const Slots& sl) const {
     const int32_t bkey = (sl.plo + 1) * tpp;
     const uint32_t lo = sl.lo + vhead + (uint32_t)(t0 - sl.plo * tpp) * 2;
     const int32_t lim = nk - t0, split = bkey - t0;
@@ -648,20 +758,20 @@ struct KvTiles {
       for (int j = 0; j < VCP; ++j) {
         // opaque, so the offset stays one add of the scalar base (the
         // compiler otherwise re-derives it with a per-lane multiply)
-        uint32_t off = vlane[j];
+        uint32_t off = vl[j % KH];
         asm volatile("" : "+v"(off));
-        dma16(lbase, lo + off, vl + (RPI * VCP * wave + RPI * j) * 2 * BK);
+        dma16(lbase, lo + (uint32_t)(RPI * 2 * j) * tpp + off, vt + (RPI * VCP * wave + RPI * j) * 2 * BK);
       }
       return;
     }
     const uint32_t hi = sl.hi + vhead + (uint32_t)(t0 - bkey) * 2;
 #pragma unroll
     for (int j = 0; j < VCP; ++j) {
-      const int32_t rk = vkey[j];
+      const int32_t rk = vkey(j);
       const bool in = rk < lim;
-      const uint32_t off = in ? vlane[j] : vlane[j] - (uint32_t)rk * 2;
+      const uint32_t at = vl[j % KH] + (uint32_t)(RPI * 2 * j) * tpp, off = in ? at : at - (uint32_t)rk * 2;
       const uint32_t base = (in && rk >= split) ? hi : lo;
-      dma16(lbase, base + off, vl + (RPI * VCP * wave + RPI * j) * 2 * BK);
+      dma16(lbase, base + off, vt + (RPI * VCP * wave + RPI * j) * 2 * BK);
     }
   }
 };
@@ -741,7 +851,7 @@ __device__ __forceinline__ AttnItem decode_item(const AttnPlan& plan, const Attn
 // of a whole unit, or a piece's unnormalised partial with its max and sum.
 // oacc[db] holds, in lane (g, c) value r, O[query c][16 db + 4 g + r].
 template <int BQ, class M>
-__device__ __forceinline__ void store_rows(const AttnItem& it, const AttnGeom& g, uint16_t* o,
+__device__ __forceinline__ void store_rows(const AttnItem& it, const typename M::Geom& g, uint16_t* o,
                                            const f32x4 (&oacc)[8], float m_run, float l_run,
                                            int32_t lrow, int32_t lg) {
   const float l_tot = group_sum(l_run);
@@ -753,7 +863,7 @@ __device__ __forceinline__ void store_rows(const AttnItem& it, const AttnGeom& g
 #pragma unroll
     for (int db = 0; db < 8; ++db) *reinterpret_cast<f32x4*>(po + 16 * db) = oacc[db];
     if (lg == 0) {
-      g.part_ml[2 * at] = l_tot == 0.f ? -INFINITY : m_run * g.unit;
+      g.part_ml[2 * at] = l_tot == 0.f ? -INFINITY : m_run * unit_of<M>(g);
       g.part_ml[2 * at + 1] = l_tot;
     }
     return;
@@ -771,15 +881,15 @@ __device__ __forceinline__ void store_rows(const AttnItem& it, const AttnGeom& g
         *reinterpret_cast<u32x2*>(op + 16 * db) = v;
       }
       if constexpr (M::kLse)
-        if (lg == 0)
-          g.lse[(size_t)it.head * g.rows + (size_t)it.node * g.nq + qrow] = m_run * g.unit + __builtin_amdgcn_logf(l_tot);
+        if (g.lse && lg == 0)
+          g.lse[(size_t)it.head * g.rows + (size_t)it.node * g.nq + qrow] = m_run * unit_of<M>(g) + __builtin_amdgcn_logf(l_tot);
     }
   } else {
     float* po = g.part_o + ((size_t)it.slot * BQ + lrow) * HDB + 4 * lg;
 #pragma unroll
     for (int db = 0; db < 8; ++db) *reinterpret_cast<f32x4*>(po + 16 * db) = oacc[db];
     if (lg == 0) {
-      g.part_ml[((size_t)it.slot * 2 + 0) * BQ + lrow] = !M::kLse ? m_run : l_tot == 0.f ? -INFINITY : m_run * g.unit;
+      g.part_ml[((size_t)it.slot * 2 + 0) * BQ + lrow] = !M::kLse ? m_run : l_tot == 0.f ? -INFINITY : m_run * unit_of<M>(g);
       g.part_ml[((size_t)it.slot * 2 + 1) * BQ + lrow] = l_tot;
     }
   }
@@ -805,7 +915,7 @@ __device__ __forceinline__ void qk_tile(const char* kl, const AttnLane& L, const
     for (int h = 0; h < KH; ++h)
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        const bf16x8 a = *reinterpret_cast<const bf16x8*>(kl + L.koff[b][ds] + h * 8192);
+        const bf16x8 a = *reinterpret_cast<const bf16x8*>(kl + L.k(b, ds) + h * 8192);
         acc[h][b][0] = mfma16(a, qreg[0][ds], acc[h][b][0]);
         acc[h][b][1] = mfma16(a, qreg[1][ds], acc[h][b][1]);
       }
@@ -849,8 +959,7 @@ __device__ __forceinline__ void clear_past(char* vl, const AttnLane& L, int32_t 
 // cores while the exponentials of tile t run on the vector ALUs, then
 // O^T += V(t)^T P(t) and the row sums lsum += 1^T P(t).  K runs one tile
 // ahead of V: K(t+1) sits in K buffer KN, V(t) in V buffer VC.
-// (The forms with logarithmic sums add up the exponentials themselves, in
-// lsum[qb][0] and [1].)
+// (The forms with logarithmic sums add up the exponentials themselves, in lsum[qb][0].)
 template <class M, int KH, int KN, int VC, bool NEXT, bool MASK>
 __device__ __forceinline__ void attn_step(char* smem, const AttnLane& L, const bf16x8 (&qreg)[2][4],
                                           f32x4 (&oacc)[2][8], STile<KH>& s, const float (&m)[2],
@@ -867,7 +976,7 @@ __device__ __forceinline__ void attn_step(char* smem, const AttnLane& L, const b
     const char* kl = smem + KN * T::KT_BYTES;
     const char* vl = smem + 2 * T::KT_BYTES + VC * T::VT_BYTES;
     auto frag = [&](int i) -> bf16x8 {
-      if (i < NKF) return *reinterpret_cast<const bf16x8*>(kl + L.koff[i & 1][i >> 2] + ((i >> 1) & 1) * 8192);
+      if (i < NKF) return *reinterpret_cast<const bf16x8*>(kl + L.k(i & 1, i >> 2) + ((i >> 1) & 1) * 8192);
       const int j = i - NKF;
       return *reinterpret_cast<const bf16x8*>(vl + L.voff[j >> 3] + (j & 7) * (16 * 2 * T::BK));
     };
@@ -898,8 +1007,7 @@ __device__ __forceinline__ void attn_step(char* smem, const AttnLane& L, const b
           const float p1 = __builtin_amdgcn_exp2f(s[ph][(pe + 1) >> 2][pq][(pe + 1) & 3] * unit);
           pb[ph][pq][pe] = static_cast<__bf16>(p0);
           pb[ph][pq][pe + 1] = static_cast<__bf16>(p1);
-          lsum[pq][0] += p0;
-          lsum[pq][1] += p1;
+          lsum[pq][0] += p0 + p1;
         } else {
           pb[ph][pq][pe] = static_cast<__bf16>(__builtin_amdgcn_exp2f(s[ph][pe >> 2][pq][pe & 3]));
           pb[ph][pq][pe + 1] = static_cast<__bf16>(__builtin_amdgcn_exp2f(s[ph][(pe + 1) >> 2][pq][(pe + 1) & 3]));
@@ -1022,7 +1130,7 @@ __device__ __forceinline__ void attn_exact(char* smem, const KvTiles<NW, KH>& kv
 // streams K/V from HBM: it trades resident waves for copies in flight.
 template <int NW, int KH, int D, class M = PlainAttn>
 __global__ __launch_bounds__(64 * NW, NW == 8 || D == 4 ? 1 : 2) void attn_bf16_kernel(const uint16_t* __restrict__ q,
-                                                                    uint16_t* __restrict__ o, AttnGeom g,
+                                                                    uint16_t* __restrict__ o, typename M::Geom g,
                                                                     typename M::Plan plan) {
   constexpr int BQ = 32 * NW;
   using T = Tile<KH>;
@@ -1031,7 +1139,8 @@ __global__ __launch_bounds__(64 * NW, NW == 8 || D == 4 ? 1 : 2) void attn_bf16_
   // K buffers 0 .. D-1 then V^T buffers 0 .. D-1 (KT_BYTES, VT_BYTES each)
   __shared__ __attribute__((aligned(1024))) char smem[D * (KT_BYTES + VT_BYTES)];
   __shared__ int32_t any_bad;
-  const AttnItem it = decode_item<KH>(plan, g, blockIdx.x);
+  AttnItem it = decode_item<KH>(plan, g, blockIdx.x);
+  if constexpr (M::kLse) in_scalars(it);
   if (it.ta == it.tb) return;  // empty piece of a unit shorter than the split
   const int32_t ta = it.ta, ntiles = it.tb;  // this item's key tiles: [ta, ntiles)
   const int32_t tid = threadIdx.x, lane = tid & 63;
@@ -1097,7 +1206,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 || D == 4 ? 1 : 2) void attn_bf16_
     for (; t + 2 < ntiles; t += 2) {
       kv.copy_k((t + 2) * BK, smem, sk);
       kv.copy_v((t + 1) * BK, smem + 2 * KT_BYTES + VT_BYTES, sv);
-      if constexpr (ACT) attn_step<M, KH, 1, 0, true, false>(smem, L, qreg, oacc, s, m, lsum, ones, t * BK, nk, lg, g.unit);
+      if constexpr (ACT) attn_step<M, KH, 1, 0, true, false>(smem, L, qreg, oacc, s, m, lsum, ones, t * BK, nk, lg, unit_of<M>(g));
       // the next copies' page slots: their scalar loads share the LDS wait
       // counter, so they are issued after the step's fragment reads (a wait
       // for one fragment would otherwise wait for them too)
@@ -1108,7 +1217,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 || D == 4 ? 1 : 2) void attn_bf16_
       if (t + 3 < ntiles) kv.copy_k((t + 3) * BK, smem + KT_BYTES, sk);
       kv.copy_v((t + 2) * BK, smem + 2 * KT_BYTES, sv);
       if constexpr (ACT)
-        attn_step<M, KH, 0, 1, true, false>(smem, L, qreg, oacc, s, m, lsum, ones, (t + 1) * BK, nk, lg, g.unit);
+        attn_step<M, KH, 0, 1, true, false>(smem, L, qreg, oacc, s, m, lsum, ones, (t + 1) * BK, nk, lg, unit_of<M>(g));
       __builtin_amdgcn_sched_barrier(0);
       sk = kv.slots(min(t + 4, it.ntiles - 1) * BK);
       sv = kv.slots(min(t + 3, it.ntiles - 1) * BK);
@@ -1116,20 +1225,20 @@ __global__ __launch_bounds__(64 * NW, NW == 8 || D == 4 ? 1 : 2) void attn_bf16_
     }
     if (t + 1 < ntiles) {  // two tiles left, parity 0
       kv.copy_v((t + 1) * BK, smem + 2 * KT_BYTES + VT_BYTES, sv);
-      if constexpr (ACT) attn_step<M, KH, 1, 0, true, false>(smem, L, qreg, oacc, s, m, lsum, ones, t * BK, nk, lg, g.unit);
+      if constexpr (ACT) attn_step<M, KH, 1, 0, true, false>(smem, L, qreg, oacc, s, m, lsum, ones, t * BK, nk, lg, unit_of<M>(g));
       landed();
       ++t;
       if constexpr (ACT) {
         if (ragged)
-          attn_step<M, KH, 0, 1, false, true>(smem, L, qreg, oacc, s, m, lsum, ones, t * BK, nk, lg, g.unit);
+          attn_step<M, KH, 0, 1, false, true>(smem, L, qreg, oacc, s, m, lsum, ones, t * BK, nk, lg, unit_of<M>(g));
         else
-          attn_step<M, KH, 0, 1, false, false>(smem, L, qreg, oacc, s, m, lsum, ones, t * BK, nk, lg, g.unit);
+          attn_step<M, KH, 0, 1, false, false>(smem, L, qreg, oacc, s, m, lsum, ones, t * BK, nk, lg, unit_of<M>(g));
       }
     } else if constexpr (ACT) {  // one tile left, parity 0 (masking twice is harmless)
       if (ragged)
-        attn_step<M, KH, 1, 0, false, true>(smem, L, qreg, oacc, s, m, lsum, ones, t * BK, nk, lg, g.unit);
+        attn_step<M, KH, 1, 0, false, true>(smem, L, qreg, oacc, s, m, lsum, ones, t * BK, nk, lg, unit_of<M>(g));
       else
-        attn_step<M, KH, 1, 0, false, false>(smem, L, qreg, oacc, s, m, lsum, ones, t * BK, nk, lg, g.unit);
+        attn_step<M, KH, 1, 0, false, false>(smem, L, qreg, oacc, s, m, lsum, ones, t * BK, nk, lg, unit_of<M>(g));
     }
   };
   auto weights_of = [&](bf16x8 (&pb)[KH][2]) __attribute__((always_inline)) {
@@ -1248,17 +1357,13 @@ __global__ __launch_bounds__(64 * NW, NW == 8 || D == 4 ? 1 : 2) void attn_bf16_
     else
       run_ring(std::false_type{});
   }
-  if constexpr (M::kLse) {  // per lane, of its keys' share
-    lsum[0][0] += lsum[0][1];
-    lsum[1][0] += lsum[1][1];
-  }
   // the guard, on the final sums (also NaN / inf)
   const bool bad = __builtin_amdgcn_ballot_w64(!(lsum[0][0] < P_GUARD && lsum[1][0] < P_GUARD)) != 0;
   l[0] = lsum[0][0];  // zero outside lanes 0..15, so the group sum is the row sum
   l[1] = lsum[1][0];
   if (bad && lane == 0) atomicOr(&any_bad, 1);
   __syncthreads();  // every wave is done with the ring; any_bad is final
-  if (any_bad) attn_exact<M>(smem, kv, L, qreg, oacc, m, l, ta, ntiles, lg, g.unit);
+  if (any_bad) attn_exact<M>(smem, kv, L, qreg, oacc, m, l, ta, ntiles, lg, unit_of<M>(g));
 #pragma unroll
   for (int qb = 0; qb < 2; ++qb) store_rows<BQ, M>(it, g, o, oacc[qb], m[qb], l[qb], wave * 32 + 16 * qb + c, lg);
 }
@@ -1302,7 +1407,8 @@ struct WaveTiles : KvTiles<1, 1> {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int32_t rg = 16 * h + 4 * j;
-        off[j] = (rg >= lim ? kbad + (klane[4 * h + j] & 255u) : (rg >= split ? hi : lo) + klane[4 * h + j]) +
+        const uint32_t k = klane(kl0, 4 * h + j);
+        off[j] = (rg >= lim ? kbad + (k & 255u) : (rg >= split ? hi : lo) + 1024u * (4 * h + j) + k) +
                  (kCopyBias - 1024 * j);
       }
       copy_group<4>(biased, off, lds + 4096 * h);
@@ -1318,22 +1424,15 @@ struct WaveTiles : KvTiles<1, 1> {
       uint32_t off[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int32_t rk = vkey[4 * h + j];
+        const int32_t rk = vkey(4 * h + j);
         const bool in = rk < lim;
-        off[j] = (in && rk >= split ? hi : lo) + vlane[4 * h + j] - (in ? 0u : (uint32_t)rk * 2) + (kCopyBias - 1024 * j);
+        off[j] = (in && rk >= split ? hi : lo) + vl[0] + (uint32_t)(RPI * 2 * (4 * h + j)) * tpp - (in ? 0u : (uint32_t)rk * 2) +
+                 (kCopyBias - 1024 * j);
       }
       copy_group<4>(biased, off, lds + 4096 * h);
     }
   }
 };
-
-// All but this wave's N newest copies have landed.
-template <int N>
-__device__ __forceinline__ void copies_landed() {
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
-// This wave's LDS reads are done: what they read may be copied over.
-__device__ __forceinline__ void reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 // Ranges that the work-groups past the attention's own read and drop (ReadAhead).
 // A few dozen of these work-groups take 10 - 18 us and leave most CUs without
@@ -1371,7 +1470,7 @@ struct NoAhead {};
 // Ahead: AttnAhead, or NoAhead where nothing is to be read.
 template <class Ahead, class M = PlainAttn>
 __global__ __launch_bounds__(64 * WV_NW, 2) void attn_waves_kernel(const uint16_t* __restrict__ q,
-                                                                   uint16_t* __restrict__ o, AttnGeom g,
+                                                                   uint16_t* __restrict__ o, typename M::Geom g,
                                                                    typename M::Plan plan, Ahead ahead) {
   uint32_t units = gridDim.x;
   if constexpr (std::is_same_v<Ahead, AttnAhead>) {
@@ -1388,8 +1487,27 @@ __global__ __launch_bounds__(64 * WV_NW, 2) void attn_waves_kernel(const uint16_
   const int32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int32_t lg = lane >> 4, c = lane & 15;
   AttnItem it;
+  bool alone = false;  // this wave has the item to itself
   if constexpr (M::kShare) {
-    it = decode_item<1>(plan, g, blockIdx.x);
+    const uint32_t n0 = (uint32_t)(g.p_pieces * g.p_qtiles * g.n_heads);
+    alone = g.own_waves && blockIdx.x >= n0;
+    if (alone) {
+      // own pages of a few tiles: nodes fastest within a head, so that the rows of q
+      // and the partials of a work-group's waves lie side by side
+      const int32_t i = (int32_t)(blockIdx.x - n0) * WV_NW + wave, per = g.n_nodes * g.n_qtiles;
+      if (i >= per * g.n_heads) return;
+      it.head = i / per;
+      it.node = 1 + i % per / g.n_qtiles;
+      it.qt = i % g.n_qtiles;
+      it.row0 = (it.node - 1) * g.nq;
+      it.rows = g.nq;
+      it.slot = g.p_pieces;
+      it.ta = 0;
+      it.tb = share_tiles<1>(plan, g, it.node);
+    } else {
+      it = decode_item<1>(plan, g, blockIdx.x);
+      if (it.ta == it.tb) return;
+    }
   } else {
     // query tiles fastest: an XCD's work-groups share the K/V of a few (node, head)s
     const int32_t unit = (int32_t)xcd_remap(blockIdx.x, units);
@@ -1408,8 +1526,8 @@ __global__ __launch_bounds__(64 * WV_NW, 2) void attn_waves_kernel(const uint16_
     tile0 = it.ta;
     nt = it.tb - it.ta;
   }
-  const int32_t t_end = tile0 + (wave + 1) * nt / WV_NW;
-  int32_t t = tile0 + wave * nt / WV_NW;
+  const int32_t t_end = alone ? nt : tile0 + (wave + 1) * nt / WV_NW;
+  int32_t t = alone ? 0 : tile0 + wave * nt / WV_NW;
   char* const kl = smem + wave * (Tile<1>::KT_BYTES + Tile<1>::VT_BYTES);
   char* const vl = kl + Tile<1>::KT_BYTES;
   const uint32_t kd = __builtin_amdgcn_readfirstlane(lds_addr(kl)), vd = kd + Tile<1>::KT_BYTES;  // for the copies
@@ -1452,7 +1570,7 @@ __global__ __launch_bounds__(64 * WV_NW, 2) void attn_waves_kernel(const uint16_
         const bool up = mx[qb] > lim[qb];
         const float d = up ? mx[qb] : 0.f;
         const float alpha =
-            lim[qb] == 0.f ? __builtin_amdgcn_exp2f(M::kLse ? -d * g.unit : -d) : 1.f;  // nothing to scale before the first
+            lim[qb] == 0.f ? __builtin_amdgcn_exp2f(-d * unit_of<M>(g)) : 1.f;  // nothing to scale before the first
         m[qb] += d;
         lim[qb] = up ? 0.f : lim[qb];
 #pragma unroll
@@ -1493,6 +1611,22 @@ __global__ __launch_bounds__(64 * WV_NW, 2) void attn_waves_kernel(const uint16_
     for (int qb = 0; qb < 2; ++qb) {
       lsum[qb][0] = group_sum(lsum[qb][0]);
       m[qb] *= g.unit;  // in log2 units from here on
+    }
+  if constexpr (M::kShare)
+    if (alone) {
+#pragma unroll
+      for (int qb = 0; qb < 2; ++qb) {
+        const int32_t row = qt * WV_BQ + 16 * qb + c;
+        if (row >= rows) continue;
+        const size_t at = ((size_t)it.slot * g.n_heads + head) * g.rows + row0 + row;
+#pragma unroll
+        for (int db = 0; db < 8; ++db) *reinterpret_cast<f32x4*>(g.part_o + at * HDB + 16 * db + 4 * lg) = oacc[qb][db];
+        if (lg == 0) {
+          g.part_ml[2 * at] = lim[qb] == 0.f ? m[qb] : -INFINITY;
+          g.part_ml[2 * at + 1] = lsum[qb][0];
+        }
+      }
+      return;
     }
   if (lg == 0)
 #pragma unroll
@@ -1539,7 +1673,7 @@ __global__ __launch_bounds__(64 * WV_NW, 2) void attn_waves_kernel(const uint16_
     }
     if (row < rows) {
       if constexpr (M::kLse)
-        if (wave == 0 && lg == 0) g.lse[(size_t)head * g.rows + row0 + row] = mrow[qb] + __builtin_amdgcn_logf(lrow[qb]);
+        if (g.lse && wave == 0 && lg == 0) g.lse[(size_t)head * g.rows + row0 + row] = mrow[qb] + __builtin_amdgcn_logf(lrow[qb]);
       u32x2 v;
       v.x = pack_bf16x2(a[0] * inv[qb], a[1] * inv[qb]);
       v.y = pack_bf16x2(a[2] * inv[qb], a[3] * inv[qb]);
@@ -1554,7 +1688,7 @@ __global__ __launch_bounds__(64 * WV_NW, 2) void attn_waves_kernel(const uint16_
 // With m = max m_p:
 //   O = sum_p 2^(m_p - m) O_p / sum_p 2^(m_p - m) l_p.
 template <int BQ, int KH, class M = PlainAttn>
-__global__ __launch_bounds__(256) void attn_combine_kernel(uint16_t* __restrict__ o, AttnGeom g, AttnPlan plan) {
+__global__ __launch_bounds__(256) void attn_combine_kernel(uint16_t* __restrict__ o, typename M::Geom g, AttnPlan plan) {
   const int32_t tu = blockIdx.x;
   const int32_t unit = g.whole_units + tu;
   const int32_t qt = unit % g.n_qtiles;
@@ -1582,7 +1716,7 @@ __global__ __launch_bounds__(256) void attn_combine_kernel(uint16_t* __restrict_
   }
   const float inv = 1.f / l;
   if constexpr (M::kLse)
-    if (dl == 0) g.lse[(size_t)head * g.rows + (size_t)node * g.nq + qrow] = m + __builtin_amdgcn_logf(l);
+    if (g.lse && dl == 0) g.lse[(size_t)head * g.rows + (size_t)node * g.nq + qrow] = m + __builtin_amdgcn_logf(l);
   u32x2 r;
   r.x = pack_bf16x2(acc[0] * inv, acc[1] * inv);
   r.y = pack_bf16x2(acc[2] * inv, acc[3] * inv);
@@ -1593,30 +1727,42 @@ __global__ __launch_bounds__(256) void attn_combine_kernel(uint16_t* __restrict_
 // row's own node, in that order.  GR groups of 32 lanes share a row (and each
 // holds 4 of its HD outputs per lane, or 2): one group where the partials are
 // few, eight where there are many and the chain of loads would set the time.
-template <int HD, int GR, bool F32>
-__global__ __launch_bounds__(256) void attn_share_combine_kernel(void* __restrict__ o, AttnGeom g, SharePlan plan) {
+template <int HD, int GR, int KH>
+__global__ __launch_bounds__(256) void attn_share_combine_kernel(void* __restrict__ o, LseGeom g, SharePlan plan) {
   constexpr int V = HD / 32;
+  constexpr bool F32 = KH == 0;
   typedef float fv __attribute__((ext_vector_type(V)));
   __shared__ fv red[8][32];
   const int32_t grp = threadIdx.x >> 5, dl = threadIdx.x & 31;
   const int32_t row = GR == 8 ? (int32_t)blockIdx.x : (int32_t)blockIdx.x * 8 + grp, head = blockIdx.y;
   if (row >= g.rows) return;  // the whole work-group where its lanes share a row
   const int32_t node = 1 + (int32_t)fast_div((uint32_t)row, g.nq_div);
-  const int32_t items = (node == g.n_nodes ? plan.item_off[kMaxNodes + 1] : plan.item_off[node + 1]) - plan.item_off[node];
-  const int32_t P = g.p_pieces, n = P + items / (g.n_qtiles * g.n_heads);
+  const int32_t n = g.p_pieces + (g.own_waves ? 1 : (share_tiles<KH>(plan, g, node) + g.o_tiles - 1) / g.o_tiles);
   const auto at = [&](int32_t p) { return ((size_t)p * g.n_heads + head) * g.rows + row; };
   const auto ex = [](float x) { return F32 ? expf(x) : __builtin_amdgcn_exp2f(x); };
-  float m = -INFINITY;
-  for (int32_t p = dl; p < n; p += 32) m = fmaxf(m, g.part_ml[2 * at(p)]);
+  // the first partials are on their way while the maximum is found
+  constexpr int AHEAD = 4;
+  const int32_t p0 = GR == 8 ? grp : 0;
+  fv first[AHEAD];
+#pragma unroll
+  for (int j = 0; j < AHEAD; ++j)
+    first[j] = *reinterpret_cast<const fv*>(g.part_o + at(min(p0 + GR * j, n - 1)) * HD + V * dl);
+  const float m0 = dl < n ? g.part_ml[2 * at(dl)] : -INFINITY, l0 = dl < n ? g.part_ml[2 * at(dl) + 1] : 0.f;
+  float m = m0;
+  for (int32_t p = dl + 32; p < n; p += 32) m = fmaxf(m, g.part_ml[2 * at(p)]);
 #pragma unroll
   for (int x = 16; x; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
-  float l = 0.f;
-  for (int32_t p = dl; p < n; p += 32) l += ex(g.part_ml[2 * at(p)] - m) * g.part_ml[2 * at(p) + 1];
+  const float e0 = dl < n ? ex(m0 - m) : 0.f;
+  float l = e0 * l0;
+  for (int32_t p = dl + 32; p < n; p += 32) l += ex(g.part_ml[2 * at(p)] - m) * g.part_ml[2 * at(p) + 1];
 #pragma unroll
   for (int x = 16; x; x >>= 1) l += __shfl_xor(l, x);
   fv acc = {};
+#pragma unroll
+  for (int j = 0; j < AHEAD; ++j)
+    if (p0 + GR * j < n) acc += __shfl(e0, p0 + GR * j, 32) * first[j];
 #pragma unroll 4
-  for (int32_t p = GR == 8 ? grp : 0; p < n; p += GR)
+  for (int32_t p = p0 + GR * AHEAD; p < n; p += GR)
     acc += ex(g.part_ml[2 * at(p)] - m) * *reinterpret_cast<const fv*>(g.part_o + at(p) * HD + V * dl);
   if constexpr (GR == 8) {
     red[grp][dl] = acc;
@@ -1659,13 +1805,13 @@ struct AttnSchedule {
 // Enqueues the kernel of a form, and where its pieces left partials the kernel that
 // merges them.
 template <class M>
-void launch_form(const AttnShape& sh, uint32_t items, const AttnGeom& g, const typename M::Plan& plan, const void* q,
+void launch_form(const AttnShape& sh, uint32_t items, const typename M::Geom& g, const typename M::Plan& plan, const void* q,
                  void* o, int32_t dtype, int32_t head_dim, hipStream_t stream);
 template <>  // attention_lse.hip
-void launch_form<LseAttn>(const AttnShape&, uint32_t, const AttnGeom&, const AttnPlan&, const void*, void*, int32_t,
+void launch_form<LseAttn>(const AttnShape&, uint32_t, const LseGeom&, const AttnPlan&, const void*, void*, int32_t,
                           int32_t, hipStream_t);
 template <>
-void launch_form<ShareAttn>(const AttnShape&, uint32_t, const AttnGeom&, const SharePlan&, const void*, void*, int32_t,
+void launch_form<ShareAttn>(const AttnShape&, uint32_t, const LseGeom&, const SharePlan&, const void*, void*, int32_t,
                             int32_t, hipStream_t);
 
 }  // namespace sc

@@ -5,14 +5,20 @@
 namespace sc {
 
 template <class M>
-static void launch_main(const AttnShape& sh, uint32_t items, const AttnGeom& g, const typename M::Plan& plan,
+static void launch_main(const AttnShape& sh, uint32_t items, const typename M::Geom& g, const typename M::Plan& plan,
                         const void* q, void* o, int32_t dtype, int32_t head_dim, hipStream_t stream) {
   timer_begin(TK_ATTENTION, stream);
   if (dtype == SC_DTYPE_F32) {
     const float* qf = static_cast<const float*>(q);
     float* of = static_cast<float*>(o);
-    if (head_dim == 64)
+    // a pool that is only element-aligned: the copies into LDS move 16 bytes at a time
+    const bool staged = (reinterpret_cast<uintptr_t>(g.layer_base) & 15) == 0;
+    if (head_dim == 64 && staged)
+      hipLaunchKernelGGL((attn_f32_kernel<64, M, true>), dim3(items), dim3(64 * F32_NW), 0, stream, qf, of, g, plan);
+    else if (head_dim == 64)
       hipLaunchKernelGGL((attn_f32_kernel<64, M>), dim3(items), dim3(64 * F32_NW), 0, stream, qf, of, g, plan);
+    else if (staged)
+      hipLaunchKernelGGL((attn_f32_kernel<128, M, true>), dim3(items), dim3(64 * F32_NW), 0, stream, qf, of, g, plan);
     else
       hipLaunchKernelGGL((attn_f32_kernel<128, M>), dim3(items), dim3(64 * F32_NW), 0, stream, qf, of, g, plan);
     timer_end(TK_ATTENTION, stream);
@@ -35,7 +41,7 @@ static void launch_main(const AttnShape& sh, uint32_t items, const AttnGeom& g, 
 }
 
 template <>
-void launch_form<LseAttn>(const AttnShape& sh, uint32_t items, const AttnGeom& g, const AttnPlan& plan, const void* q,
+void launch_form<LseAttn>(const AttnShape& sh, uint32_t items, const LseGeom& g, const AttnPlan& plan, const void* q,
                           void* o, int32_t dtype, int32_t head_dim, hipStream_t stream) {
   launch_main<LseAttn>(sh, items, g, plan, q, o, dtype, head_dim, stream);
   if (!g.tail_units) return;
@@ -52,25 +58,29 @@ void launch_form<LseAttn>(const AttnShape& sh, uint32_t items, const AttnGeom& g
 }
 
 template <>
-void launch_form<ShareAttn>(const AttnShape& sh, uint32_t items, const AttnGeom& g, const SharePlan& plan,
+void launch_form<ShareAttn>(const AttnShape& sh, uint32_t items, const LseGeom& g, const SharePlan& plan,
                             const void* q, void* o, int32_t dtype, int32_t head_dim, hipStream_t stream) {
   launch_main<ShareAttn>(sh, items, g, plan, q, o, dtype, head_dim, stream);
   timer_begin(TK_ATTN_COMBINE, stream);
-  const bool many = g.p_pieces >= 8;  // the chain of a row's loads, split over eight groups of lanes
+  // many: the chain of a row's loads, split over eight groups of lanes
+  const bool many = g.p_pieces + g.o_pieces > 8, f32 = dtype == SC_DTYPE_F32;
   const dim3 grid(many ? (uint32_t)g.rows : (uint32_t)(g.rows + 7) / 8, (uint32_t)g.n_heads);
-  const bool f32 = dtype == SC_DTYPE_F32;
   if (f32 && head_dim == 64 && many)
-    hipLaunchKernelGGL((attn_share_combine_kernel<64, 8, true>), grid, dim3(256), 0, stream, o, g, plan);
+    hipLaunchKernelGGL((attn_share_combine_kernel<64, 8, 0>), grid, dim3(256), 0, stream, o, g, plan);
   else if (f32 && head_dim == 64)
-    hipLaunchKernelGGL((attn_share_combine_kernel<64, 1, true>), grid, dim3(256), 0, stream, o, g, plan);
+    hipLaunchKernelGGL((attn_share_combine_kernel<64, 1, 0>), grid, dim3(256), 0, stream, o, g, plan);
   else if (f32 && many)
-    hipLaunchKernelGGL((attn_share_combine_kernel<128, 8, true>), grid, dim3(256), 0, stream, o, g, plan);
+    hipLaunchKernelGGL((attn_share_combine_kernel<128, 8, 0>), grid, dim3(256), 0, stream, o, g, plan);
   else if (f32)
-    hipLaunchKernelGGL((attn_share_combine_kernel<128, 1, true>), grid, dim3(256), 0, stream, o, g, plan);
+    hipLaunchKernelGGL((attn_share_combine_kernel<128, 1, 0>), grid, dim3(256), 0, stream, o, g, plan);
+  else if (sh.kh == 1 && many)
+    hipLaunchKernelGGL((attn_share_combine_kernel<128, 8, 1>), grid, dim3(256), 0, stream, o, g, plan);
+  else if (sh.kh == 1)
+    hipLaunchKernelGGL((attn_share_combine_kernel<128, 1, 1>), grid, dim3(256), 0, stream, o, g, plan);
   else if (many)
-    hipLaunchKernelGGL((attn_share_combine_kernel<128, 8, false>), grid, dim3(256), 0, stream, o, g, plan);
+    hipLaunchKernelGGL((attn_share_combine_kernel<128, 8, 2>), grid, dim3(256), 0, stream, o, g, plan);
   else
-    hipLaunchKernelGGL((attn_share_combine_kernel<128, 1, false>), grid, dim3(256), 0, stream, o, g, plan);
+    hipLaunchKernelGGL((attn_share_combine_kernel<128, 1, 2>), grid, dim3(256), 0, stream, o, g, plan);
   timer_end(TK_ATTN_COMBINE, stream);
 }
 

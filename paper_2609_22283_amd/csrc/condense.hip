@@ -5,8 +5,8 @@
 // Two launches.  condense_select_kernel finds each head's tokens: the n-th largest
 // weight by radix selection over the weights' bits (11 + 11 + 10), then one pass
 // that gives every kept token its place.  One work-group per layer and head: a
-// selection is a chain of counts over all of a head's tokens, and the tokens lie in
-// LDS meanwhile.  condense_gather_kernel moves the data: K rows whole, V^T rows
+// selection is a chain of counts over all of a head's tokens, which stay in
+// registers meanwhile.  condense_gather_kernel moves the data: K rows whole, V^T rows
 // element by element (their tokens are adjacent), eight tokens of a row to a store.
 #include <algorithm>
 #include <cstring>
@@ -38,93 +38,131 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-constexpr int CS_T = 1024, CS_BINS = 2048;
+constexpr int CS_BINS = 2048;
 
-// Inclusive sums over the work-group's threads of two counts packed in 64 bits.
-__device__ __forceinline__ uint64_t block_scan(uint64_t x, uint64_t* sums, int32_t tid) {
-  const int32_t lane = tid & 63, wave = tid >> 6;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint64_t y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
-  if (lane == 63) sums[wave] = x;
-  __syncthreads();
-  uint64_t before = 0;
-  for (int32_t w = 0; w < wave; ++w) before += sums[w];
-  __syncthreads();
-  return x + before;
+// Inclusive sum over the lanes of a wave.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+#define SC_STEP(ctrl, rows) x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, rows, 0xf, false)
+  SC_STEP(0x111, 0xf);  // row_shr 1, 2, 4, 8: within 16 lanes
+  SC_STEP(0x112, 0xf);
+  SC_STEP(0x114, 0xf);
+  SC_STEP(0x118, 0xf);
+  SC_STEP(0x142, 0xa);  // lane 15 of a row to the next, lane 31 to the upper half
+  SC_STEP(0x143, 0xc);
+#undef SC_STEP
+  return x;
 }
 
-// MAX: tokens kept in LDS (0: read again from memory in each pass).
-template <int MAX>
-__global__ __launch_bounds__(CS_T) void condense_select_kernel(CondenseGeom g, CondenseSlots slots) {
-  __shared__ uint32_t keys[MAX ? MAX : 1];
-  __shared__ uint32_t hist[CS_BINS];
-  __shared__ uint64_t sums[CS_T / 64];
-  __shared__ uint32_t found[2];
+// The same over the T threads of a work-group (sums: T / 64 words of LDS, its own).
+template <int T>
+__device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* sums, int32_t tid) {
+  x = wave_scan(x);
+  if ((tid & 63) == 63) sums[tid >> 6] = x;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < T / 64 - 1; ++w) x += w < (tid >> 6) ? sums[w] : 0u;
+  return x;
+}
+
+// T threads hold R tokens each, in order (R a multiple of 8: eight tokens lie in
+// one page); R 0: any number of tokens, read again in each pass.  C copies of a
+// counter: fewer lanes of a wave meet in one.
+template <int T, int R, int C>
+__global__ __launch_bounds__(T) void condense_select_kernel(CondenseGeom g, CondenseSlots slots) {
+  constexpr int BPT = CS_BINS / T;    // bins of a thread, counted together by it:
+  constexpr int ROW = BPT * C + 4;    // their counters, and a gap that spreads the threads over the banks
+  __shared__ __attribute__((aligned(16))) uint32_t hist[T * ROW];
+  __shared__ uint32_t sums[5][T / 64];
+  __shared__ uint32_t found[3][2];
   const int32_t tid = threadIdx.x, head = blockIdx.x, layer = blockIdx.y, N = g.n_src * g.tpp;
   const float* w = g.weights + ((size_t)layer * g.n_slots * g.n_heads + head) * g.tpp;
-  const auto load = [&](int32_t i) {
-    const int32_t p = (int32_t)fast_div((uint32_t)i, g.tpp_div);
-    return weight_key(w[(size_t)slots.slot[p] * g.n_heads * g.tpp + (i - p * g.tpp)]);
+  const int32_t per = R ? R : ((N + T - 1) / T + 7) / 8 * 8, i0 = tid * per;
+  constexpr int RR = R ? R : 8;
+  uint32_t keys[RR];
+  // eight tokens from i on (past the end: of the lowest key, and counted by nothing)
+  const auto load = [&](int32_t i, uint32_t* k) __attribute__((always_inline)) {
+    const int32_t p = (int32_t)fast_div((uint32_t)min(i, N - 8), g.tpp_div);
+    const float* from = w + (size_t)slots.slot[p] * g.n_heads * g.tpp + (min(i, N - 8) - p * g.tpp);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) k[e] = weight_key(from[e]);
   };
-  if constexpr (MAX > 0)
-    for (int32_t i = tid; i < N; i += CS_T) keys[i] = load(i);
-  const auto key = [&](int32_t i) {
-    if constexpr (MAX > 0) return keys[i];
-    return load(i);
+  // f(key) for this thread's tokens in order
+  const auto each = [&](auto f) __attribute__((always_inline)) {
+    if constexpr (R > 0) {
+#pragma unroll
+      for (int e = 0; e < R; ++e)
+        if (i0 + e < N) f(keys[e], i0 + e);
+    } else {
+      for (int32_t i = i0; i < min(i0 + per, N); i += 8) {
+        load(i, keys);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f(keys[e], i + e);
+      }
+    }
   };
-  // the n-th largest key, `prefix` its bits found so far, `want` its rank among the
+  for (int32_t b = tid; b < T * ROW; b += T) hist[b] = 0;
+  if constexpr (R > 0)
+#pragma unroll
+    for (int e = 0; e < R; e += 8) load(i0 + e, keys + e);
+  __syncthreads();
+  // the n-th largest key: `prefix` its bits found so far, `want` its rank among the
   // keys that share them
   uint32_t prefix = 0, want = (uint32_t)g.n;
 #pragma unroll
   for (int pass = 0; pass < 3; ++pass) {
     const int sh = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-    for (int32_t b = tid; b < CS_BINS; b += CS_T) hist[b] = 0;
+    each([&](uint32_t k, int32_t) __attribute__((always_inline)) {
+      if (pass == 0 || k >> (sh + bits) == prefix)
+      {
+        const uint32_t bin = CS_BINS - 1 - (k >> sh & ((1u << bits) - 1));  // from the top
+        atomicAdd(&hist[bin / BPT * ROW + bin % BPT * C + (tid & (C - 1))], 1u);
+      }
+    });
     __syncthreads();
-    for (int32_t i = tid; i < N; i += CS_T) {
-      const uint32_t k = key(i);
-      if (pass == 0 || k >> (sh + bits) == prefix) atomicAdd(&hist[k >> sh & ((1u << bits) - 1)], 1u);
+    // this thread's bins, and zeros in their place for the next pass
+    uint32_t count[BPT], all = 0;
+    u32x4* mine = reinterpret_cast<u32x4*>(hist + tid * ROW);
+#pragma unroll
+    for (int b = 0; b < BPT; ++b) count[b] = 0;
+#pragma unroll
+    for (int v = 0; v < BPT * C / 4; ++v) {
+      const u32x4 c = mine[v];
+      if (pass < 2) mine[v] = u32x4{};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) count[(4 * v + e) / C] += c[e];
     }
+#pragma unroll
+    for (int b = 0; b < BPT; ++b) all += count[b];
+    const uint32_t upto = block_scan<T>(all, sums[pass], tid);
+    uint32_t before = upto - all;
+    if (before < want && want <= upto)
+#pragma unroll
+      for (int b = 0; b < BPT; ++b) {
+        if (before < want && want <= before + count[b]) {
+          found[pass][0] = (uint32_t)(CS_BINS - 1 - BPT * tid - b);
+          found[pass][1] = want - before;
+        }
+        before += count[b];
+      }
     __syncthreads();
-    // bins from the top, two to a thread
-    const uint32_t hi = hist[CS_BINS - 1 - 2 * tid], lo = hist[CS_BINS - 2 - 2 * tid];
-    const uint32_t upto = (uint32_t)block_scan(hi + lo, sums, tid), before = upto - hi - lo;
-    if (before < want && want <= upto) {
-      const bool first = want <= before + hi;
-      found[0] = (uint32_t)(CS_BINS - 1 - 2 * tid) - (first ? 0u : 1u);
-      found[1] = want - before - (first ? 0u : hi);
-    }
-    __syncthreads();
-    prefix = prefix << bits | found[0];
-    want = found[1];
-    __syncthreads();
+    prefix = prefix << bits | found[pass][0];
+    want = found[pass][1];
   }
-  // every key above `prefix` is kept, and the first `want` that equal it; a thread
-  // takes a run of tokens (of odd length: LDS banks)
-  const int32_t run = (N + CS_T - 1) / CS_T | 1;
-  const int32_t i0 = min(tid * run, N), i1 = min(i0 + run, N);
+  // every key above `prefix` is kept, and the first `want` that equal it
   uint32_t above = 0, equal = 0;
-  for (int32_t i = i0; i < i1; ++i) {
-    const uint32_t k = key(i);
+  each([&](uint32_t k, int32_t) __attribute__((always_inline)) {
     above += k > prefix;
     equal += k == prefix;
-  }
-  const uint64_t own = (uint64_t)equal << 32 | above, upto = block_scan(own, sums, tid) - own;
-  above = (uint32_t)upto;
-  equal = (uint32_t)(upto >> 32);
+  });
+  const uint32_t own_above = above, own_equal = equal;
+  above = block_scan<T>(above, sums[3], tid) - own_above;
+  equal = block_scan<T>(equal, sums[4], tid) - own_equal;
   int32_t* kept = g.kept + ((size_t)layer * g.n_heads + head) * g.n;
-  for (int32_t i = i0; i < i1; ++i) {
-    const uint32_t k = key(i);
-    if (k > prefix) {
-      kept[above + min(equal, want)] = i;
-      ++above;
-    } else if (k == prefix) {
-      if (equal < want) kept[above + equal] = i;
-      ++equal;
-    }
-  }
+  each([&](uint32_t k, int32_t i) __attribute__((always_inline)) {
+    if (k > prefix || (k == prefix && equal < want)) kept[above + min(equal, want)] = i;
+    above += k > prefix;
+    equal += k == prefix;
+  });
 }
 
 // E: the elements' type (uint16_t or uint32_t), HD the head dim.
@@ -221,12 +259,17 @@ int launch_condense(const sc_cache* c, int32_t layer, int32_t n_layers, const in
     g.kept = kept + (size_t)l * d.n_heads * g.n;
     const dim3 heads((uint32_t)d.n_heads, (uint32_t)m), grid((uint32_t)(k_blocks + v_blocks), (uint32_t)(m * d.n_heads));
     timer_begin(TK_CONDENSE, stream);
-    if (N <= 8192)
-      hipLaunchKernelGGL((condense_select_kernel<8192>), heads, dim3(CS_T), 0, stream, g, s);
-    else if (N <= 36864)
-      hipLaunchKernelGGL((condense_select_kernel<36864>), heads, dim3(CS_T), 0, stream, g, s);
+    // few tokens: fewer waves meet at each barrier
+    if (N <= 256 * 8)
+      hipLaunchKernelGGL((condense_select_kernel<256, 8, 1>), heads, dim3(256), 0, stream, g, s);
+    else if (N <= 1024 * 8)
+      hipLaunchKernelGGL((condense_select_kernel<1024, 8, 4>), heads, dim3(1024), 0, stream, g, s);
+    else if (N <= 1024 * 16)
+      hipLaunchKernelGGL((condense_select_kernel<1024, 16, 4>), heads, dim3(1024), 0, stream, g, s);
+    else if (N <= 1024 * 40)
+      hipLaunchKernelGGL((condense_select_kernel<1024, 40, 4>), heads, dim3(1024), 0, stream, g, s);
     else
-      hipLaunchKernelGGL((condense_select_kernel<0>), heads, dim3(CS_T), 0, stream, g, s);
+      hipLaunchKernelGGL((condense_select_kernel<1024, 0, 4>), heads, dim3(1024), 0, stream, g, s);
     if (d.dtype == SC_DTYPE_F32 && d.head_dim == 64)
       hipLaunchKernelGGL((condense_gather_kernel<uint32_t, 64>), grid, dim3(CG_T), 0, stream, g, s, k_blocks);
     else if (d.dtype == SC_DTYPE_F32)

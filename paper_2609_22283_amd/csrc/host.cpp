@@ -31,17 +31,22 @@ int plan_check(const sc_plan* plan, const sc_cache* cache, int32_t layer) {
   if (plan->cache != cache) return fail(SC_EINVAL, "plan was built for another cache");
   if (layer < 0 || layer >= cache->d.n_layers)
     return fail(SC_EINVAL, "layer %d outside [0, %d)", layer, cache->d.n_layers);
-  for (size_t p = 0; p < plan->page_slot.size(); ++p) {
-    int32_t s = plan->page_slot[p];
-    if (!cache->used[s] || cache->gen[s] != plan->page_gen[p])
-      return fail(SC_ESTALE, "slot %d was released after the plan was built", s);
-  }
+  // pages that every node's list starts with are looked at once
+  const int32_t n = (int32_t)plan->nodes.size();
+  const auto first = [&](int32_t i) { return (size_t)plan->page_off[i] + (i ? plan->shared : 0); };
+  for (int32_t i = 0; i < n; ++i)
+    for (size_t p = first(i); p < (size_t)plan->page_off[i + 1]; ++p) {
+      int32_t s = plan->page_slot[p];
+      if (!cache->used[s] || cache->gen[s] != plan->page_gen[p])
+        return fail(SC_ESTALE, "slot %d was released after the plan was built", s);
+    }
   // every slot is still the one planned (above), so its flag is its state's
   const uint8_t* wr = cache->slot_written.data() + (size_t)layer * cache->d.n_slots;
-  for (size_t p = 0; p < plan->page_slot.size(); ++p)
-    if (!wr[plan->page_slot[p]])
-      return fail(SC_EUNAVAILABLE, "state (%d,%d) has no K/V at layer %d",
-                  plan->page_state[p].first, plan->page_state[p].second, layer);
+  for (int32_t i = 0; i < n; ++i)
+    for (size_t p = first(i); p < (size_t)plan->page_off[i + 1]; ++p)
+      if (!wr[plan->page_slot[p]])
+        return fail(SC_EUNAVAILABLE, "state (%d,%d) has no K/V at layer %d",
+                    plan->page_state[p].first, plan->page_state[p].second, layer);
   return SC_OK;
 }
 

@@ -32,6 +32,7 @@ struct StateEntry {
   std::vector<uint8_t> written;  // per layer
 };
 
+struct ShareSchedule;  // attention.hip
 struct WeighLaunches;  // weigh.hip
 
 inline size_t dtype_size(int32_t dtype) { return dtype == SC_DTYPE_F32 ? 4 : 2; }
@@ -70,6 +71,8 @@ struct sc_plan {
   int32_t shared = 0;  // leading pages that every node's list has in common (sc_plan_share)
   // page slots in the bf16 attention's traversal order (built on first use)
   mutable std::vector<int32_t> attn_slot;
+  // how it runs with a shared prefix or logarithmic sums (attention.hip; found on first use)
+  mutable std::vector<std::shared_ptr<const sc::ShareSchedule>> share;
   // its pages by the nodes that read them (built on first use)
   mutable std::shared_ptr<const sc::WeighLaunches> weigh;
 };
@@ -115,15 +118,17 @@ int launch_attention_lse(const sc_plan* plan, const sc_cache* cache, int32_t lay
 constexpr int32_t kAttnMaxPieces = 1024;
 constexpr int32_t kAttnMinSplitTiles = 32;  // mean 64-key tiles per unit below which nothing is cut
 size_t attention_workspace_bytes(const sc_plan* plan, const sc_cache* cache);
+size_t attention_lse_workspace_bytes(const sc_plan* plan, const sc_cache* cache);  // with the logarithmic sums
 size_t attention_workspace_bound();
 int launch_append(const sc_cache* cache, int32_t layer, const int32_t* slots, int32_t chunk,
                   const void* k, const void* v, const sc_rope* rope, hipStream_t stream);
 int launch_rope_table(const sc_rope_desc* d, void* table, hipStream_t stream);
 
 // Adds the weight that every key of the plan's pages received to `weights` (the
-// whole array); lse: the rows' logarithmic sums.
+// whole array); lse: the rows' logarithmic sums; part: weigh_workspace_bytes() bytes.
+size_t weigh_workspace_bytes(const sc_plan* plan, const sc_cache* cache);
 int launch_weigh(const sc_plan* plan, const sc_cache* cache, int32_t layer, const void* q, const float* lse,
-                 float scale, float* weights, hipStream_t stream);
+                 float scale, float* weights, float* part, hipStream_t stream);
 int launch_weights_clear(const sc_cache* cache, const int32_t* slots, int32_t n, float* weights, hipStream_t stream);
 // Whether a fold of so many states fits a launch: SC_OK or SC_EUNSUPPORTED; the
 // fold itself: slots of the n_src source pages, then the new state's.

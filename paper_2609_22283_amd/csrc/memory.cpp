@@ -88,11 +88,15 @@ extern "C" int sc_cache_weights_clear(const sc_cache* c, sc_node st, float* weig
                               static_cast<hipStream_t>(stream));
 }
 
-// attention partials | the rows' logarithmic sums [head][row]
+// the attention's partials, then the splits' sums of the weights | the rows'
+// logarithmic sums [head][row]
+static size_t weigh_partials(const sc_plan* p, const sc_cache* c) {
+  return align256(std::max(attention_lse_workspace_bytes(p, c), weigh_workspace_bytes(p, c)));
+}
+
 extern "C" size_t sc_attention_weigh_workspace_bytes(const sc_plan* p, const sc_cache* c) {
-  if (!p || !c || p->cache != c) return 0;
-  return align256(attention_workspace_bytes(p, c)) +
-         (size_t)p->nodes.size() * p->nq * c->d.n_heads * sizeof(float);
+  if (!p || !c || p->cache != c || p->nodes.empty() || attention_check(p, c) != SC_OK) return 0;
+  return weigh_partials(p, c) + (size_t)p->nodes.size() * p->nq * c->d.n_heads * sizeof(float);
 }
 
 extern "C" int sc_attention_weigh(const sc_plan* p, const sc_cache* c, int32_t layer, const void* q, void* o,
@@ -100,18 +104,19 @@ extern "C" int sc_attention_weigh(const sc_plan* p, const sc_cache* c, int32_t l
   return guarded([&]() -> int {
     if (!p || !c || !q || !o || !weights) return fail(SC_EINVAL, "null argument");
     if (!std::isfinite(scale)) return fail(SC_EINVAL, "scale must be finite");
+    if (reinterpret_cast<uintptr_t>(q) & 15) return fail(SC_EINVAL, "q must be 16-byte aligned");
     int rc = plan_check(p, c, layer);
     if (rc != SC_OK) return rc;
     if (p->nodes.empty()) return SC_OK;
     if ((rc = attention_check(p, c)) != SC_OK) return rc;
-    if (!ws || ws_bytes < sc_attention_weigh_workspace_bytes(p, c))
-      return fail(SC_EINVAL, "workspace of %zu bytes, need %zu", ws ? ws_bytes : 0, sc_attention_weigh_workspace_bytes(p, c));
+    const size_t need = sc_attention_weigh_workspace_bytes(p, c);
+    if (!ws || ws_bytes < need) return fail(SC_EINVAL, "workspace of %zu bytes, need %zu", ws ? ws_bytes : 0, need);
     if (reinterpret_cast<uintptr_t>(ws) & 15) return fail(SC_EINVAL, "workspace must be 16-byte aligned");
     hipStream_t stream = static_cast<hipStream_t>(stream_);
-    const size_t part = attention_workspace_bytes(p, c);
-    float* lse = reinterpret_cast<float*>(static_cast<char*>(ws) + align256(part));
+    const size_t part = weigh_partials(p, c);
+    float* lse = reinterpret_cast<float*>(static_cast<char*>(ws) + part);
     if ((rc = launch_attention_lse(p, c, layer, q, o, lse, scale, ws, part, stream)) != SC_OK) return rc;
-    return launch_weigh(p, c, layer, q, lse, scale, weights, stream);
+    return launch_weigh(p, c, layer, q, lse, scale, weights, static_cast<float*>(ws), stream);
   });
 }
 

@@ -7,9 +7,10 @@
 // lse: the rows' logarithmic sums, left by the attention itself (log2 units), so a
 // second Q K^T is all that is computed; the probabilities are never stored.  A
 // work-group owns keys, holds them in registers and streams through the rows of
-// every node that reads them: nothing is summed across work-groups, so the
-// result does not depend on their order.  Keys read by the same nodes are taken
-// together, page after page.
+// every node that reads them.  Keys read by the same nodes are taken together, page
+// after page.  Where that leaves CUs idle, the rows are split over work-groups, whose
+// sums a second launch adds in their order: no atomics, so equal calls give equal
+// bits.
 #include <algorithm>
 #include <climits>
 #include <cmath>
@@ -34,8 +35,9 @@ struct WeighGeom {
   const char* layer_base;
   uint64_t slot_bytes;
   float* weights;    // this layer's
+  float* part;       // [split][head][key of the launch] sums of the splits' rows, if splits > 1
   const float* lse;  // [head][row]
-  int32_t n_heads, tpp, nq, rows, blocks;
+  int32_t n_heads, tpp, nq, rows, blocks, splits, keys;  // keys: of the launch
   DivMagic tpp_div, nq_div;
   float unit;       // bf16: |scale| log2(e)
   float scale;      // fp32
@@ -44,13 +46,14 @@ struct WeighGeom {
 
 // A work-group's keys: those of block `blk` of KB keys, and the rows that read them.
 struct WeighItem {
-  int32_t head, key0, n_keys, page0;  // key0: first key within the group's n_keys
+  int32_t head, split, key0, n_keys, page0;  // key0: first key within the group's n_keys
   uint64_t readers;
 };
 __device__ __forceinline__ WeighItem weigh_item(const WeighPlan& plan, const WeighGeom& g, int32_t kb) {
   const int32_t i = (int32_t)xcd_remap(blockIdx.x, gridDim.x);  // an XCD's work-groups share the rows of a few heads
   WeighItem it;
-  it.head = i / g.blocks;
+  it.head = i / (g.blocks * g.splits);
+  it.split = i / g.blocks % g.splits;
   const int32_t blk = i % g.blocks;
   const int32_t grp = __builtin_popcountll(__builtin_amdgcn_ballot_w64(plan.block0[threadIdx.x & 63] <= blk)) - 1;
   it.readers = plan.readers[grp];
@@ -95,6 +98,11 @@ typedef float f32x4a __attribute__((ext_vector_type(4), aligned(4)));
 __device__ __forceinline__ void add_weights(const WeighPlan& plan, const WeighGeom& g, const WeighItem& it, int32_t key,
                                             const f32x4& w) {
   if (key >= it.n_keys) return;
+  if (g.splits > 1) {
+    float* p = g.part + ((size_t)it.split * g.n_heads + it.head) * g.keys + it.page0 * g.tpp + key;
+    *reinterpret_cast<f32x4a*>(p) = w;
+    return;
+  }
   const WeighKey k = weigh_key(plan, g, it, key);
   f32x4a* p = reinterpret_cast<f32x4a*>(g.weights + ((size_t)k.slot * g.n_heads + it.head) * g.tpp + k.token);
   *p = *p + w;
@@ -162,12 +170,15 @@ __global__ __launch_bounds__(64 * WG_NW, 2) void weigh_bf16_kernel(const uint16_
   f32x4 w[KW];
 #pragma unroll
   for (int b = 0; b < KW; ++b) w[b] = f32x4{};
-  const int32_t nt = (n_rows + WG_QB - 1) / WG_QB;
-  float lse = fetch(0, 0);
-  for (int32_t t = 0; t < nt; ++t) {
+  const int32_t tiles_in_all = (n_rows + WG_QB - 1) / WG_QB;
+  int32_t t = (int32_t)((int64_t)it.split * tiles_in_all / g.splits);
+  const int32_t t_end = (int32_t)((int64_t)(it.split + 1) * tiles_in_all / g.splits);
+  float lse = 0.f;
+  if (t < t_end) lse = fetch(t, t & 1);
+  for (; t < t_end; ++t) {
     landed();
     const float l = lse;
-    if (t + 1 < nt) lse = fetch(t + 1, (t + 1) & 1);
+    if (t + 1 < t_end) lse = fetch(t + 1, (t + 1) & 1);
     const char* tile = tiles[t & 1];
 #pragma unroll
     for (int qb = 0; qb < WG_QB / 16; ++qb) {
@@ -195,55 +206,89 @@ __global__ __launch_bounds__(64 * WG_NW, 2) void weigh_bf16_kernel(const uint16_
   }
 }
 
-// fp32: a work-group of eight waves owns 16 keys; its waves take the 16-row blocks in
-// turn and add up through LDS, in wave order.  Operands as in attn_f32_kernel.
-constexpr int WF_NW = 8, WF_KB = 16;
+// fp32: the same with eight waves of 16 keys, 32-row tiles and fp32 MFMAs, whose
+// contraction index of product (j, e) in lane group g is channel 16 j + 4 g + e.
+constexpr int WF_NW = 8, WF_KB = 16 * WF_NW, WF_QB = 32;
 template <int HD>
 __global__ __launch_bounds__(64 * WF_NW) void weigh_f32_kernel(const float* __restrict__ q, WeighGeom g, WeighPlan plan) {
-  constexpr int NJ = HD / 16;
-  __shared__ f32x4 part[WF_NW][4];
+  constexpr int NJ = HD / 16, ROW = HD * 4, CP = WF_QB * ROW / (1024 * WF_NW), RPC = 1024 / ROW;  // copies of a wave, rows of one
+  __shared__ __attribute__((aligned(1024))) char tiles[2][WF_QB * ROW];
   __shared__ int32_t nodes[kMaxNodes];
   const int32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int32_t lg = lane >> 4, c = lane & 15;
   const WeighItem it = weigh_item(plan, g, WF_KB);
   if (wave == 0) list_readers(it.readers, lane, nodes);
-  const WeighKey k = weigh_key(plan, g, it, it.key0 + c);
+  const int32_t key0 = it.key0 + 16 * wave;
+  const WeighKey k = weigh_key(plan, g, it, key0 + c);
   const float* kp = reinterpret_cast<const float*>(g.layer_base + (size_t)k.slot * g.slot_bytes) +
                     ((size_t)it.head * g.tpp + k.token) * HD + 4 * lg;
   f32x4 kf[NJ];
 #pragma unroll
-  for (int j = 0; j < NJ; ++j) kf[j] = *reinterpret_cast<const f32x4u*>(kp + 16 * j);
+  for (int j = 0; j < NJ; ++j) kf[j] = *reinterpret_cast<const f32x4u*>(kp + 16 * j) * g.scale;
   __syncthreads();
   const int32_t n_rows = __builtin_popcountll(it.readers) * g.nq;
+  const char* qh = reinterpret_cast<const char*>(q) + (size_t)it.head * ROW;
+  const size_t row_bytes = (size_t)g.n_heads * ROW;
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(tiles[0])) + 1024 * CP * wave;
+  const auto fetch = [&](int32_t t, int32_t buf) __attribute__((always_inline)) {
+    const int32_t r = WF_QB * t + (lane & (WF_QB - 1)), row = reader_row(g, nodes, min(r, n_rows - 1));
+#pragma unroll
+    for (int j = 0; j < CP; ++j) {
+      const int32_t tr = RPC * (CP * wave + j) + lane / (ROW / 16), col = lane & (ROW / 16 - 1);
+      const int32_t src = __shfl(row, tr);
+      dma16_at(qh + (size_t)src * row_bytes + ((col ^ (tr & 15)) << 4), lds0 + buf * (WF_QB * ROW) + 1024 * j);
+    }
+    const float l = g.lse[(size_t)it.head * g.rows + row];
+    return r < n_rows ? l : INFINITY;
+  };
   f32x4 w = {};
-  for (int32_t r0 = 16 * wave; r0 < n_rows; r0 += 16 * WF_NW) {
-    const int32_t r = r0 + c, row = reader_row(g, nodes, min(r, n_rows - 1));
-    const float* qp = q + ((size_t)row * g.n_heads + it.head) * HD + 4 * lg;
-    f32x4 qr[NJ];
+  const int32_t tiles_in_all = (n_rows + WF_QB - 1) / WF_QB;
+  int32_t t = (int32_t)((int64_t)it.split * tiles_in_all / g.splits);
+  const int32_t t_end = (int32_t)((int64_t)(it.split + 1) * tiles_in_all / g.splits);
+  float lse = 0.f;
+  if (t < t_end) lse = fetch(t, t & 1);
+  for (; t < t_end; ++t) {
+    landed();
+    const float l = lse;
+    if (t + 1 < t_end) lse = fetch(t + 1, (t + 1) & 1);
+    const char* tile = tiles[t & 1];
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) qr[j] = *reinterpret_cast<const f32x4u*>(qp + 16 * j) * g.scale;
-    const float l = r < n_rows ? g.lse[(size_t)it.head * g.rows + row] : INFINITY;
-    f32x4 s0 = {}, s1 = {};
+    for (int rb = 0; rb < WF_QB / 16; ++rb) {
+      f32x4 s0 = {}, s1 = {};
 #pragma unroll
-    for (int j = 0; j < NJ; j += 2)
+      for (int j = 0; j < NJ; j += 2) {
+        const char* at = tile + (16 * rb + c) * ROW;
+        const f32x4 q0 = *reinterpret_cast<const f32x4*>(at + (((4 * j + lg) ^ c) << 4));
+        const f32x4 q1 = *reinterpret_cast<const f32x4*>(at + (((4 * j + 4 + lg) ^ c) << 4));
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[j][e], qr[j][e], s0, 0, 0, 0);
-        s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[j + 1][e], qr[j + 1][e], s1, 0, 0, 0);
+        for (int e = 0; e < 4; ++e) {
+          s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[j][e], q0[e], s0, 0, 0, 0);
+          s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[j + 1][e], q1[e], s1, 0, 0, 0);
+        }
       }
-    s0 += s1;
+      s0 += s1;
+      const float lq = __shfl(l, 16 * rb + c);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] += expf(s0[e] - l);
+      for (int e = 0; e < 4; ++e) w[e] += expf(s0[e] - lq);
+    }
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e) w[e] = column_sum(w[e]);
-  if (c == 0) part[wave][lg] = w;
-  __syncthreads();
-  if (wave == 0 && c == 0) {
-#pragma unroll
-    for (int v = 1; v < WF_NW; ++v) w += part[v][lg];
-    add_weights(plan, g, it, it.key0 + 4 * lg, w);
-  }
+  if (c == 0) add_weights(plan, g, it, key0 + 4 * lg, w);
+}
+
+// Adds the splits' sums, in their order: four keys of a head to a thread.
+__global__ __launch_bounds__(256) void weigh_add_kernel(WeighGeom g, WeighPlan plan) {
+  const int32_t key = 4 * (int32_t)(blockIdx.x * 256 + threadIdx.x), head = blockIdx.y;
+  if (key >= g.keys) return;
+  const int32_t p = (int32_t)fast_div((uint32_t)key, g.tpp_div);
+  const float* part = g.part + (size_t)head * g.keys + key;
+  const size_t stride = (size_t)g.n_heads * g.keys;
+  f32x4 w = *reinterpret_cast<const f32x4a*>(part);
+#pragma unroll 4
+  for (int32_t s = 1; s < g.splits; ++s) w += *reinterpret_cast<const f32x4a*>(part + s * stride);
+  f32x4a* to = reinterpret_cast<f32x4a*>(g.weights + ((size_t)plan.page_slot[p] * g.n_heads + head) * g.tpp + (key - p * g.tpp));
+  *to = *to + w;
 }
 
 // Zeroes the weights of slots, one slot of one layer per work-group.
@@ -258,11 +303,69 @@ __global__ __launch_bounds__(256) void weights_clear_kernel(float* weights, size
 // A plan's distinct pages by their readers, most readers first (the longest
 // work-groups start first), in launches of bounded argument size.  A property of
 // the plan alone: found on its first use and kept in it.
+// How a launch runs: 16-key blocks per wave (bf16) and splits of the rows.
+struct WeighForm {
+  int32_t kw, splits, blocks, keys;
+};
 struct WeighLaunches {
   std::vector<WeighPlan> plans;
+  std::vector<WeighForm> forms;
+  size_t part_bytes;  // the most that a launch's splits leave
 };
 
-static const WeighLaunches* weigh_launches(const sc_plan* p) {
+// Key blocks of kb keys of a launch; block0 of its groups is set.
+static int32_t key_blocks(WeighPlan& plan, int32_t tpp, int32_t kb) {
+  int64_t n = 0;
+  for (int32_t i = 0; i < kWeighGroups; ++i) {
+    const int64_t keys = (int64_t)(plan.page0[i + 1] - plan.page0[i]) * tpp;
+    plan.block0[i] = keys ? (int32_t)n : INT32_MAX;
+    n += (keys + kb - 1) / kb;
+  }
+  return (int32_t)n;
+}
+
+// The cheapest form by estimated time.  Measured, per 64-row tile and work-group with
+// two of them to a CU: 2.1 us with 256 keys (1.07 PFLOP/s), 1.2 with 128, 0.8 with
+// 64, whose rows feed fewer products per LDS read; 4.5, 3 and 2.5 us to bring the
+// keys; fp32: 2.9 us per 32 rows and 128 keys, one to a CU, and 3.  All
+// work-groups' time over the slots, half of the longest one's tiles, and 5 us for
+// the launch that adds splits.  (Three nodes of 792 rows over windows of seven, 12
+// heads: 256 keys 93 us whole, 70 + 5 in halves, 64 + 5 in thirds, 71 + 5 in
+// sixths; 128 keys 74 and 67 + 5; 64 keys 96.  Four of 4680: 2010 whole, 1780 in
+// halves or quarters.  fp32, four of 312 rows, 2 heads: 114 us whole, 24 in
+// sixths, 21 in twelfths.)
+static WeighForm weigh_form(WeighPlan& plan, const sc_cache* c, int32_t nq) {
+  const bool f32 = c->d.dtype == SC_DTYPE_F32;
+  const int32_t tpp = c->d.tokens_per_page, H = c->d.n_heads;
+  WeighForm best{1, 1, 0, 0};
+  double best_us = 1e30;
+  for (int32_t kw = f32 ? 1 : 4; kw >= 1; kw /= 2) {
+    const int32_t kb = f32 ? WF_KB : 16 * kw * WG_NW, rows = f32 ? WF_QB : WG_QB;
+    const double t = f32 ? 2.9 : kw == 4 ? 2.1 : kw == 2 ? 1.2 : 0.8, slots = f32 ? kCUs : 2 * kCUs;
+    const double f = f32 ? 3.0 : kw == 4 ? 4.5 : kw == 2 ? 3.0 : 2.5;
+    double tiles = 0.0, most = 0.0;
+    int64_t blocks = 0, keys = 0;
+    for (int32_t i = 0; i < kWeighGroups; ++i) {
+      const int64_t k = (int64_t)(plan.page0[i + 1] - plan.page0[i]) * tpp, b = (k + kb - 1) / kb;
+      const double r = std::ceil((double)__builtin_popcountll(plan.readers[i]) * nq / rows);
+      keys += k;
+      blocks += b;
+      tiles += (double)b * r;
+      if (b) most = std::max(most, r);
+    }
+    for (int32_t s = 1; s <= 16 && s <= most; ++s) {
+      const double per = std::ceil(most / s);
+      const double us = H * (tiles * t + (double)blocks * s * f) / slots + 0.5 * per * t + (s > 1 ? 5.0 : 0.0);
+      if (us < best_us * 0.97 && blocks * H * s < INT32_MAX) {
+        best_us = us;
+        best = WeighForm{kw, s, (int32_t)blocks, (int32_t)keys};
+      }
+    }
+  }
+  return best;
+}
+
+static const WeighLaunches* weigh_launches(const sc_plan* p, const sc_cache* c) {
   if (p->weigh) return p->weigh.get();
   std::map<int32_t, uint64_t> readers;
   const int32_t n = (int32_t)p->nodes.size();
@@ -294,18 +397,29 @@ static const WeighLaunches* weigh_launches(const sc_plan* p) {
       at += take;
       for (int32_t k = ++count; k <= kWeighGroups; ++k) w.page0[k] = pages;
     }
+  out->part_bytes = 0;
+  for (WeighPlan& w : out->plans) {
+    const WeighForm f = weigh_form(w, c, p->nq);
+    key_blocks(w, c->d.tokens_per_page, c->d.dtype == SC_DTYPE_F32 ? WF_KB : 16 * f.kw * WG_NW);
+    out->forms.push_back(f);
+    if (f.splits > 1)
+      out->part_bytes = std::max(out->part_bytes, (size_t)f.splits * c->d.n_heads * f.keys * sizeof(float));
+  }
   p->weigh = out;
   return out.get();
 }
 
+size_t weigh_workspace_bytes(const sc_plan* p, const sc_cache* c) { return weigh_launches(p, c)->part_bytes; }
+
 int launch_weigh(const sc_plan* p, const sc_cache* c, int32_t layer, const void* q, const float* lse, float scale,
-                 float* weights, hipStream_t stream) {
+                 float* weights, float* part, hipStream_t stream) {
   const sc_cache_desc& d = c->d;
   WeighGeom g;
   std::memset(&g, 0, sizeof g);
   g.layer_base = c->pool + (size_t)layer * d.n_slots * c->slot_bytes;
   g.slot_bytes = c->slot_bytes;
   g.weights = weights + (size_t)layer * d.n_slots * d.n_heads * d.tokens_per_page;
+  g.part = part;
   g.lse = lse;
   g.n_heads = d.n_heads;
   g.tpp = d.tokens_per_page;
@@ -316,35 +430,33 @@ int launch_weigh(const sc_plan* p, const sc_cache* c, int32_t layer, const void*
   g.unit = std::fabs(scale) * 1.4426950408889634f;
   g.scale = scale;
   g.q_flip = std::signbit(scale) ? 0x80008000u : 0u;
-  for (const WeighPlan& from : weigh_launches(p)->plans) {
-    WeighPlan plan = from;
-    const auto blocks = [&](int32_t kb) {
-      int64_t n = 0;
-      for (int32_t i = 0; i < kWeighGroups; ++i) {
-        const int64_t keys = (int64_t)(plan.page0[i + 1] - plan.page0[i]) * g.tpp;
-        plan.block0[i] = keys ? (int32_t)n : INT32_MAX;
-        n += (keys + kb - 1) / kb;
-      }
-      return (int32_t)n;
-    };
+  const WeighLaunches* all = weigh_launches(p, c);
+  for (size_t i = 0; i < all->plans.size(); ++i) {
+    const WeighPlan& plan = all->plans[i];
+    const WeighForm& f = all->forms[i];
+    g.blocks = f.blocks;
+    g.splits = f.splits;
+    g.keys = f.keys;
+    const dim3 grid((uint32_t)(f.blocks * d.n_heads * f.splits));
     timer_begin(TK_ATTN_WEIGH, stream);
     if (d.dtype == SC_DTYPE_F32) {
-      g.blocks = blocks(WF_KB);
-      const dim3 grid((uint32_t)(g.blocks * d.n_heads));
+      const float* qf = static_cast<const float*>(q);
       if (d.head_dim == 64)
-        hipLaunchKernelGGL((weigh_f32_kernel<64>), grid, dim3(64 * WF_NW), 0, stream, static_cast<const float*>(q), g, plan);
+        hipLaunchKernelGGL((weigh_f32_kernel<64>), grid, dim3(64 * WF_NW), 0, stream, qf, g, plan);
       else
-        hipLaunchKernelGGL((weigh_f32_kernel<128>), grid, dim3(64 * WF_NW), 0, stream, static_cast<const float*>(q), g, plan);
+        hipLaunchKernelGGL((weigh_f32_kernel<128>), grid, dim3(64 * WF_NW), 0, stream, qf, g, plan);
     } else {
       const uint16_t* qb = static_cast<const uint16_t*>(q);
-      g.blocks = blocks(16 * 4 * WG_NW);
-      if (g.blocks * d.n_heads >= kCUs) {
-        hipLaunchKernelGGL((weigh_bf16_kernel<4>), dim3((uint32_t)(g.blocks * d.n_heads)), dim3(64 * WG_NW), 0, stream, qb, g, plan);
-      } else {
-        g.blocks = blocks(16 * WG_NW);
-        hipLaunchKernelGGL((weigh_bf16_kernel<1>), dim3((uint32_t)(g.blocks * d.n_heads)), dim3(64 * WG_NW), 0, stream, qb, g, plan);
-      }
+      if (f.kw == 4)
+        hipLaunchKernelGGL((weigh_bf16_kernel<4>), grid, dim3(64 * WG_NW), 0, stream, qb, g, plan);
+      else if (f.kw == 2)
+        hipLaunchKernelGGL((weigh_bf16_kernel<2>), grid, dim3(64 * WG_NW), 0, stream, qb, g, plan);
+      else
+        hipLaunchKernelGGL((weigh_bf16_kernel<1>), grid, dim3(64 * WG_NW), 0, stream, qb, g, plan);
     }
+    if (f.splits > 1)
+      hipLaunchKernelGGL(weigh_add_kernel, dim3((uint32_t)((f.keys / 4 + 255) / 256), (uint32_t)d.n_heads), dim3(256), 0,
+                         stream, g, plan);
     timer_end(TK_ATTN_WEIGH, stream);
     SC_HIP(hipGetLastError());
   }

@@ -160,3 +160,25 @@ def test_share_captured():
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(o, want)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_share_pool_off_16_byte_boundaries(hd):
+    """An fp32 pool that is only element-aligned: the same sums through other loads."""
+    states = [(c, 0) for c in range(9)]
+    case = MemCache("f32", 2, hd, 40, 1, states, seed=99)
+    own = states[6:]
+    plan = sc.sc_plan_share(sc.sc_plan_condition(case.cache, own, 20), states[:6])
+    q = case.queries(60)
+    aligned = _run(case, plan, q, 0.1)
+    want, _ = case.attend(q, [states[:6] + [s] for s in own], 0.1)
+    raw = torch.zeros(case.pool.numel() + 16, dtype=torch.uint8, device="cuda")
+    pool = raw[4:4 + case.pool.numel()]
+    cache = sc.sc_cache_create(pool, 1, 2, hd, 40, 1, case.n_slots, sc.SC_DTYPE_F32)
+    for st in states:
+        cache.append(0, st, *case.kv[st][0])
+    case.cache = cache
+    plan = sc.sc_plan_share(sc.sc_plan_condition(cache, own, 20), states[:6])
+    shifted = _run(case, plan, q, 0.1)
+    close("f32", shifted, want, "o")
+    assert torch.equal(shifted, aligned)

@@ -110,7 +110,7 @@ def test_weigh_sizes_and_refusals():
     call = lambda **k: sc.sc_attention_weigh(  # noqa: E731
         plan, k.get("cache", cache), k.get("layer", 0), k.get("q", PTR), PTR, k.get("scale", 0.1),
         k.get("weights", PTR), k.get("ws", PTR), k.get("nb", nb))
-    for bad in (dict(q=0), dict(weights=0), dict(scale=float("nan")), dict(scale=float("inf")), dict(layer=2),
+    for bad in (dict(q=0), dict(q=PTR + 8), dict(weights=0), dict(scale=float("nan")), dict(scale=float("inf")), dict(layer=2),
                 dict(layer=-1), dict(cache=_cache())):
         assert _code(call, **bad) == sc.SC_EINVAL, bad
     assert _code(call) == sc.SC_EUNAVAILABLE  # slots reserved, nothing written
