@@ -990,6 +990,19 @@ __device__ __forceinline__ void attn_step(char* smem, const AttnLane& L, const b
 #pragma unroll
           for (int r = 0; r < 4; ++r) sn[h][b][qb][r] = -m[qb];
     bf16x8 pb[2][2];
+    // the 32 exponentials, those of half 0 first: spread over the K fragments and the
+    // V^T fragments before the first that needs half 1
+    constexpr int NE = M::kLse ? 24 : 16;
+    auto prob = [&](int x) __attribute__((always_inline)) {
+      const int ph = x >> 4, pq = (x >> 3) & 1, pe = x & 7;
+      if constexpr (M::kLse) {
+        const float p = __builtin_amdgcn_exp2f(s[ph][pe >> 2][pq][pe & 3] * unit);
+        pb[ph][pq][pe] = static_cast<__bf16>(p);
+        lsum[pq][0] += p;
+      } else {
+        pb[ph][pq][pe] = static_cast<__bf16>(__builtin_amdgcn_exp2f(s[ph][pe >> 2][pq][pe & 3]));
+      }
+    };
     bf16x8 ring[PF];
 #pragma unroll
     for (int i = 0; i < PF; ++i) ring[i] = frag(i);
@@ -997,21 +1010,14 @@ __device__ __forceinline__ void attn_step(char* smem, const AttnLane& L, const b
     for (int i = 0; i < NF; ++i) {
       const bf16x8 f = ring[i % PF];
       if (i + PF < NF) ring[i % PF] = frag(i + PF);
+      if (i < NE) {
+#pragma unroll
+        for (int x = i * 32 / NE; x < (i + 1) * 32 / NE; ++x) prob(x);
+      }
       if (i < NKF) {  // K fragment (ds, h, b) = (i / 4, i / 2 mod 2, i mod 2), as in qk_tile
         const int ds = i >> 2, h = (i >> 1) & 1, b = i & 1;
         sn[h][b][0] = mfma16(f, qreg[0][ds], sn[h][b][0]);
         sn[h][b][1] = mfma16(f, qreg[1][ds], sn[h][b][1]);
-        const int ph = i >> 3, pq = (i >> 2) & 1, pe = 2 * (i & 3);  // pb[ph][pq] elements pe, pe + 1
-        if constexpr (M::kLse) {
-          const float p0 = __builtin_amdgcn_exp2f(s[ph][pe >> 2][pq][pe & 3] * unit);
-          const float p1 = __builtin_amdgcn_exp2f(s[ph][(pe + 1) >> 2][pq][(pe + 1) & 3] * unit);
-          pb[ph][pq][pe] = static_cast<__bf16>(p0);
-          pb[ph][pq][pe + 1] = static_cast<__bf16>(p1);
-          lsum[pq][0] += p0 + p1;
-        } else {
-          pb[ph][pq][pe] = static_cast<__bf16>(__builtin_amdgcn_exp2f(s[ph][pe >> 2][pq][pe & 3]));
-          pb[ph][pq][pe + 1] = static_cast<__bf16>(__builtin_amdgcn_exp2f(s[ph][(pe + 1) >> 2][pq][(pe + 1) & 3]));
-        }
       } else {  // V^T fragment (h, db) = (j / 8, j mod 8), as in pv_tile
         const int j = i - NKF, h = j >> 3, db = j & 7;
         oacc[0][db] = mfma16(f, pb[h][0], oacc[0][db]);
