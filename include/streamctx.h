@@ -414,6 +414,17 @@ int sc_attention_weigh(const sc_plan* plan, const sc_cache* cache, int32_t layer
                        void* o, float scale, float* weights, void* ws, size_t ws_bytes,
                        sc_stream stream);
 
+/* sc_stack_forward whose self-attention weighs the keys that it reads, at every
+ * layer: sc_attention_weigh in the place of sc_attention (so x agrees with
+ * sc_stack_forward within bf16 rounding, not in bits), the pack's own states among
+ * the weighed ones.  weigh_ws: a second workspace, 16-byte aligned, of
+ * sc_attention_weigh_workspace_bytes(plan, cache) bytes.  When a launch fails, the
+ * weights hold partial sums.  Limits and errors of both. */
+int sc_stack_forward_weigh(const sc_block_weights* layers, int32_t n_layers, sc_cache* cache,
+                           const sc_plan* plan, void* x, const sc_rope* rope, void* ws,
+                           size_t ws_bytes, float* weights, void* weigh_ws, size_t weigh_ws_bytes,
+                           sc_stream stream);
+
 /* Folds n cached states into one, in layers [layer, layer + n_layers): with the
  * sources' tokens numbered in the order of `sources` (frames ascending), each
  * head keeps its T = pages_per_chunk * tokens_per_page tokens of the largest

@@ -28,6 +28,7 @@ __all__ = [
     "sc_serial_steps", "sc_serial_step_node", "sc_block_workspace_views",
     "sc_attention_noalloc", "sc_attention_noalloc_scratch_bytes",
     "sc_cache_weights_bytes", "sc_attention_weigh_workspace_bytes", "sc_attention_weigh", "sc_plan_share",
+    "sc_stack_forward_weigh",
 ]
 
 SC_OK, SC_EINVAL, SC_EUNAVAILABLE, SC_ECAPACITY = 0, -1, -2, -3
@@ -53,7 +54,7 @@ EXPORTED_SYMBOLS = [
     "sc_serial_steps", "sc_serial_step_node", "sc_block_workspace_views",
     "sc_attention_noalloc", "sc_attention_noalloc_scratch_bytes",
     "sc_cache_weights_bytes", "sc_cache_weights_clear", "sc_attention_weigh_workspace_bytes",
-    "sc_attention_weigh", "sc_cache_condense", "sc_plan_share",
+    "sc_attention_weigh", "sc_cache_condense", "sc_plan_share", "sc_stack_forward_weigh",
 ]
 
 # The library and PyTorch must share one HIP runtime: torch ships its own
@@ -177,6 +178,8 @@ _SIG = {
     "sc_attention_weigh": (C.c_int, [_P, _P, C.c_int32, _P, _P, C.c_float, _P, _P, C.c_size_t, _P]),
     "sc_cache_condense": (C.c_int, [_P, C.c_int32, C.c_int32, C.POINTER(sc_node), C.c_int32, sc_node, _P, _P, _P]),
     "sc_plan_share": (C.c_int, [_P, C.POINTER(sc_node), C.c_int32, C.POINTER(_P)]),
+    "sc_stack_forward_weigh": (C.c_int, [C.POINTER(sc_block_weights), C.c_int32, _P, _P, _P,
+                                         C.POINTER(sc_rope), _P, C.c_size_t, _P, _P, C.c_size_t, _P]),
 }
 # ABI version this binding marshals for (SC_ABI_VERSION of the header)
 ABI_VERSION = 7
@@ -620,3 +623,13 @@ def sc_stack_forward(layers, cache: "Cache", plan: "Plan", x, rope: "Rope", ws, 
     _check(lib.sc_stack_forward(arr, len(layers), cache.handle, plan.handle, _ptr(x),
                                 C.byref(rope.struct) if rope is not None else None, _ptr(ws),
                                 ws_bytes, _stream(stream)))
+
+
+def sc_stack_forward_weigh(layers, cache: "Cache", plan: "Plan", x, rope: "Rope", ws, ws_bytes: int, weights,
+                           weigh_ws, weigh_ws_bytes: int, stream=None) -> None:
+    """sc_stack_forward that also adds the weight every cached key received to ``weights``."""
+    arr = (sc_block_weights * len(layers))(*[w.struct for w in layers])
+    _check(lib.sc_stack_forward_weigh(arr, len(layers), cache.handle, plan.handle, _ptr(x),
+                                      C.byref(rope.struct) if rope is not None else None, _ptr(ws),
+                                      ws_bytes, _ptr(weights), _ptr(weigh_ws), weigh_ws_bytes,
+                                      _stream(stream)))

@@ -584,6 +584,8 @@ int launch_attention_lse(const sc_plan* p, const sc_cache* c, int32_t layer, con
 
 int launch_attention(const sc_plan* p, const sc_cache* c, int32_t layer, const void* q, void* o,
                      float scale, void* ws, size_t ws_bytes, hipStream_t stream) {
+  if (const Weighing* w = Weighing::current; w && w->plan == p)
+    return launch_attention_weigh(p, c, layer, q, o, scale, w->weights, w->ws, stream);
   return launch_attention_lse(p, c, layer, q, o, nullptr, scale, ws, ws_bytes, stream);
 }
 

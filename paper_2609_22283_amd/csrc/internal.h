@@ -124,11 +124,6 @@ int launch_append(const sc_cache* cache, int32_t layer, const int32_t* slots, in
                   const void* k, const void* v, const sc_rope* rope, hipStream_t stream);
 int launch_rope_table(const sc_rope_desc* d, void* table, hipStream_t stream);
 
-// Adds the weight that every key of the plan's pages received to `weights` (the
-// whole array); lse: the rows' logarithmic sums; part: weigh_workspace_bytes() bytes.
-size_t weigh_workspace_bytes(const sc_plan* plan, const sc_cache* cache);
-int launch_weigh(const sc_plan* plan, const sc_cache* cache, int32_t layer, const void* q, const float* lse,
-                 float scale, float* weights, float* part, hipStream_t stream);
 int launch_weights_clear(const sc_cache* cache, const int32_t* slots, int32_t n, float* weights, hipStream_t stream);
 // Whether a fold of so many states fits a launch: SC_OK or SC_EUNSUPPORTED; the
 // fold itself: slots of the n_src source pages, then the new state's.
@@ -170,6 +165,26 @@ struct ReadAhead {
   void passed(int k) {
     if (next < k) next = k;
   }
+};
+
+// The attention with the weights of its keys (weigh.hip); ws: weigh_attention_bytes()
+// bytes, 16-byte aligned.
+size_t weigh_attention_bytes(const sc_plan* plan, const sc_cache* cache);
+int launch_attention_weigh(const sc_plan* plan, const sc_cache* cache, int32_t layer, const void* q, void* o,
+                           float scale, float* weights, void* ws, hipStream_t stream);
+
+// While an object of this kind lives, this thread's launch_attention calls over its
+// plan weigh the keys as well.
+struct Weighing {
+  const sc_plan* plan;
+  float* weights;
+  void* ws;
+  Weighing* const outer;
+  static inline thread_local Weighing* current = nullptr;
+  Weighing(const sc_plan* p, float* w, void* s) : plan(p), weights(w), ws(s), outer(current) { current = this; }
+  ~Weighing() { current = outer; }
+  Weighing(const Weighing&) = delete;
+  Weighing& operator=(const Weighing&) = delete;
 };
 
 // Kernel timer: launchers bracket their kernel with timer_begin/timer_end.

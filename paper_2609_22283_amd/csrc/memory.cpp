@@ -88,35 +88,46 @@ extern "C" int sc_cache_weights_clear(const sc_cache* c, sc_node st, float* weig
                               static_cast<hipStream_t>(stream));
 }
 
-// the attention's partials, then the splits' sums of the weights | the rows'
-// logarithmic sums [head][row]
-static size_t weigh_partials(const sc_plan* p, const sc_cache* c) {
-  return align256(std::max(attention_lse_workspace_bytes(p, c), weigh_workspace_bytes(p, c)));
-}
-
 extern "C" size_t sc_attention_weigh_workspace_bytes(const sc_plan* p, const sc_cache* c) {
   if (!p || !c || p->cache != c || p->nodes.empty() || attention_check(p, c) != SC_OK) return 0;
-  return weigh_partials(p, c) + (size_t)p->nodes.size() * p->nq * c->d.n_heads * sizeof(float);
+  return weigh_attention_bytes(p, c);
+}
+
+// What the weighing of a plan needs besides the attention itself.
+static int weigh_check(const sc_plan* p, const sc_cache* c, const float* weights, const void* ws, size_t ws_bytes) {
+  if (!weights) return fail(SC_EINVAL, "null argument");
+  if (p->nodes.empty()) return SC_OK;
+  const int rc = attention_check(p, c);
+  if (rc != SC_OK) return rc;
+  const size_t need = weigh_attention_bytes(p, c);
+  if (!ws || ws_bytes < need) return fail(SC_EINVAL, "workspace of %zu bytes, need %zu", ws ? ws_bytes : 0, need);
+  if (reinterpret_cast<uintptr_t>(ws) & 15) return fail(SC_EINVAL, "workspace must be 16-byte aligned");
+  return SC_OK;
 }
 
 extern "C" int sc_attention_weigh(const sc_plan* p, const sc_cache* c, int32_t layer, const void* q, void* o,
-                                  float scale, float* weights, void* ws, size_t ws_bytes, sc_stream stream_) {
+                                  float scale, float* weights, void* ws, size_t ws_bytes, sc_stream stream) {
   return guarded([&]() -> int {
     if (!p || !c || !q || !o || !weights) return fail(SC_EINVAL, "null argument");
     if (!std::isfinite(scale)) return fail(SC_EINVAL, "scale must be finite");
     if (reinterpret_cast<uintptr_t>(q) & 15) return fail(SC_EINVAL, "q must be 16-byte aligned");
     int rc = plan_check(p, c, layer);
-    if (rc != SC_OK) return rc;
+    if (rc != SC_OK || (rc = weigh_check(p, c, weights, ws, ws_bytes)) != SC_OK) return rc;
     if (p->nodes.empty()) return SC_OK;
-    if ((rc = attention_check(p, c)) != SC_OK) return rc;
-    const size_t need = sc_attention_weigh_workspace_bytes(p, c);
-    if (!ws || ws_bytes < need) return fail(SC_EINVAL, "workspace of %zu bytes, need %zu", ws ? ws_bytes : 0, need);
-    if (reinterpret_cast<uintptr_t>(ws) & 15) return fail(SC_EINVAL, "workspace must be 16-byte aligned");
-    hipStream_t stream = static_cast<hipStream_t>(stream_);
-    const size_t part = weigh_partials(p, c);
-    float* lse = reinterpret_cast<float*>(static_cast<char*>(ws) + part);
-    if ((rc = launch_attention_lse(p, c, layer, q, o, lse, scale, ws, part, stream)) != SC_OK) return rc;
-    return launch_weigh(p, c, layer, q, lse, scale, weights, static_cast<float*>(ws), stream);
+    return launch_attention_weigh(p, c, layer, q, o, scale, weights, ws, static_cast<hipStream_t>(stream));
+  });
+}
+
+extern "C" int sc_stack_forward_weigh(const sc_block_weights* layers, int32_t n_layers, sc_cache* c, const sc_plan* p,
+                                      void* x, const sc_rope* rope, void* ws, size_t ws_bytes, float* weights,
+                                      void* weigh_ws, size_t weigh_ws_bytes, sc_stream stream) {
+  return guarded([&]() -> int {
+    if (!c || !p) return fail(SC_EINVAL, "null argument");
+    if (p->cache != c) return fail(SC_EINVAL, "plan was built for another cache");
+    const int rc = weigh_check(p, c, weights, weigh_ws, weigh_ws_bytes);
+    if (rc != SC_OK) return rc;
+    const Weighing scope(p, weights, weigh_ws);
+    return sc_stack_forward(layers, n_layers, c, p, x, rope, ws, ws_bytes, stream);
   });
 }
 

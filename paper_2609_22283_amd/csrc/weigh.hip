@@ -409,9 +409,8 @@ static const WeighLaunches* weigh_launches(const sc_plan* p, const sc_cache* c) 
   return out.get();
 }
 
-size_t weigh_workspace_bytes(const sc_plan* p, const sc_cache* c) { return weigh_launches(p, c)->part_bytes; }
-
-int launch_weigh(const sc_plan* p, const sc_cache* c, int32_t layer, const void* q, const float* lse, float scale,
+// Adds the weights to the whole array `weights`; part: the launches' part_bytes.
+static int launch_weigh(const sc_plan* p, const sc_cache* c, int32_t layer, const void* q, const float* lse, float scale,
                  float* weights, float* part, hipStream_t stream) {
   const sc_cache_desc& d = c->d;
   WeighGeom g;
@@ -461,6 +460,24 @@ int launch_weigh(const sc_plan* p, const sc_cache* c, int32_t layer, const void*
     SC_HIP(hipGetLastError());
   }
   return SC_OK;
+}
+
+// the attention's partials, then the splits' sums of the weights | the rows'
+// logarithmic sums [head][row]
+static size_t partial_bytes(const sc_plan* p, const sc_cache* c) {
+  return (std::max(attention_lse_workspace_bytes(p, c), weigh_launches(p, c)->part_bytes) + 255) & ~size_t(255);
+}
+
+size_t weigh_attention_bytes(const sc_plan* p, const sc_cache* c) {
+  return partial_bytes(p, c) + (size_t)p->nodes.size() * p->nq * c->d.n_heads * sizeof(float);
+}
+
+int launch_attention_weigh(const sc_plan* p, const sc_cache* c, int32_t layer, const void* q, void* o, float scale,
+                           float* weights, void* ws, hipStream_t stream) {
+  const size_t part = partial_bytes(p, c);
+  float* lse = reinterpret_cast<float*>(static_cast<char*>(ws) + part);
+  const int rc = launch_attention_lse(p, c, layer, q, o, lse, scale, ws, part, stream);
+  return rc != SC_OK ? rc : launch_weigh(p, c, layer, q, lse, scale, weights, static_cast<float*>(ws), stream);
 }
 
 int launch_weights_clear(const sc_cache* c, const int32_t* slots, int32_t n, float* weights, hipStream_t stream) {

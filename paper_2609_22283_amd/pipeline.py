@@ -17,6 +17,13 @@ condition sequence (the condition c of Eq. 1): per forward, a condition plan
 maps each pack node to the condition its chunk reads (``condition_of``), and
 each layer's weights are bound to that plan.
 
+With ``memory`` set, what leaves the history window is not lost: the clean
+states that no later node selects are folded into one memory state that every
+node reads beside its window.  The stack weighs the keys that it reads
+(``sc_stack_forward_weigh``), each head keeps the heaviest tokens of the memory
+and the states that join it (``Cache.condense``), and the packs' plans get the
+memory as a shared prefix (``sc_plan_share``).
+
 Every computation runs in the library; this module sequences calls and moves
 device buffers.
 """
@@ -30,8 +37,10 @@ from . import binding as sc
 class StackPipeline:
     def __init__(self, *, layers: Sequence["sc.BlockWeights"], cache: "sc.Cache", rope: "sc.Rope",
                  xs, noise, policy: str, K: int, W: int, B: int, t_sched: Sequence[float],
-                 refresh: bool = True, stream=None, condition=None):
-        """``condition``: optional dict with ``cache`` (an sc.Cache holding the
+                 refresh: bool = True, stream=None, condition=None, memory: bool = False):
+        """``memory``: keep one memory state of what leaves the window, of as
+        many tokens as a chunk (the cache needs room for two states more; the
+        modes and hooks are the same).  ``condition``: optional dict with ``cache`` (an sc.Cache holding the
         condition K/V of every layer), ``cross`` (per layer: (w_q, w_o,
         q_norm or None)) and ``condition_of`` (chunk -> cached condition
         state; default (0, 0))."""
@@ -47,6 +56,15 @@ class StackPipeline:
         self.stage = torch.empty((max_pack * self.n_tok, self.hidden), dtype=xs.dtype, device=xs.device)
         self.ws_bytes = sc.sc_block_workspace_bytes(self.layers[0], max_pack * self.n_tok)
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=xs.device)
+        self.memory = None   # the cached state that holds it, once something has left the window
+        self.weights = None  # accumulated attention weight of every cached key
+        if memory:
+            d = cache.desc
+            self.weights = torch.zeros((d.n_layers, d.n_slots, d.n_heads, d.tokens_per_page),
+                                       dtype=torch.float32, device=xs.device)
+            self.kept = torch.empty((d.n_layers, d.n_heads, self.n_tok), dtype=torch.int32, device=xs.device)
+            self.weigh_ws = [torch.empty(0, dtype=torch.uint8, device=xs.device)]
+            self.cached = set()  # states of the nodes run so far that are still cached
 
     # ----------------------------------------------------------- schedules
     def rounds(self) -> List[List[Tuple[int, int]]]:
@@ -72,6 +90,11 @@ class StackPipeline:
         n = self.n_tok
         sel = sc.sc_selection_build(self.policy, self.K, self.W, nodes)
         plan = sc.sc_plan_build(sel, self.cache)
+        if self.weights is not None:
+            for node in nodes:
+                self.cache.weights_clear(node, self.weights, self.stream)
+            if self.memory is not None:
+                plan = sc.sc_plan_share(plan, [self.memory])
         for i, (c, _) in enumerate(nodes):
             self.stage[i * n:(i + 1) * n].copy_(self.xs[c])
         x = self.stage[:len(nodes) * n]
@@ -82,7 +105,16 @@ class StackPipeline:
             plan_c = sc.sc_plan_condition(cond["cache"], [of(c) for c, _ in nodes], n)
             layers = [w.with_cross(sc.CrossAttn(wq, wo, cond["cache"], plan_c, q_norm=qn))
                       for w, (wq, wo, qn) in zip(self.layers, cond["cross"])]
-        if layer_hook is None:
+        if self.weights is not None:
+            if layer_hook is not None:
+                raise ValueError("layer hooks observe single blocks; a stack with a memory runs in one call")
+            nb = sc.sc_attention_weigh_workspace_bytes(plan, self.cache)
+            if self.weigh_ws[-1].numel() < nb:  # the smaller ones may still be in use
+                self.weigh_ws.append(self.torch.empty(nb, dtype=self.torch.uint8, device=x.device))
+            sc.sc_stack_forward_weigh(layers, self.cache, plan, x, self.rope, self.ws, self.ws_bytes,
+                                      self.weights, self.weigh_ws[-1], nb, self.stream)
+            self.cached.update(tuple(node) for node in nodes)
+        elif layer_hook is None:
             sc.sc_stack_forward(layers, self.cache, plan, x, self.rope, self.ws, self.ws_bytes,
                                 self.stream)
         else:
@@ -96,6 +128,32 @@ class StackPipeline:
                 sc.sc_sampler_step([(c, j)], self.t_sched, self.K, self.xs[c],
                                    self.stage[i * n:(i + 1) * n], self.noise[c, j],
                                    n * self.hidden, self.stream)
+
+    def _fold_unread(self, future: Sequence[Tuple[int, int]]) -> None:
+        """Release what no node of ``future`` selects, the clean states among it
+        into the memory; the memory too once nothing is left to read it."""
+        off, chunk, level, _ = sc.sc_selection_build(self.policy, self.K, self.W, future).tables()
+        needed = {(chunk[s], level[s]) for i in range(len(future)) for s in range(off[i], off[i + 1] - 1)}
+        unread = sorted(self.cached - needed)
+        self.cached -= set(unread)
+        leaving = [st for st in unread if st[1] == 0] if future else []
+        for st in unread:
+            if st not in leaving:
+                self.cache.release(st)
+        old = [] if self.memory is None else [self.memory]
+        if not future:
+            for st in old:
+                self.cache.release(st)
+            self.memory = None
+        elif len(old + leaving) == 1:
+            self.memory = (old + leaving)[0]  # it fits whole
+        elif leaving:
+            into = (leaving[-1][0], self.K + 1)  # a level that no node has
+            self.cache.condense(0, self.cache.desc.n_layers, old + leaving, into, self.weights, self.kept,
+                                self.stream)
+            for st in old + leaving:
+                self.cache.release(st)
+            self.memory = into
 
     def run(self, mode: str = "packed", time_rounds: bool = False,
             kernel_timer_rounds: Tuple[int, int] = None, layer_hooks=None,
@@ -128,7 +186,10 @@ class StackPipeline:
             for nodes in group:
                 self.forward(nodes, (layer_hooks or {}).get(g))
                 done += len(nodes)
-            sc.sc_cache_release_unread(self.cache, self.policy, self.K, self.W, flat[done:])
+            if self.weights is None:
+                sc.sc_cache_release_unread(self.cache, self.policy, self.K, self.W, flat[done:])
+            else:
+                self._fold_unread(flat[done:])
             if time_rounds:
                 e1.record()
                 times.append((e0, e1))
