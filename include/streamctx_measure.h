@@ -26,7 +26,8 @@ extern "C" {
  * qk-norm and of the normalised condition queries and keys),
  * "cross_attention", "gemm_cross_q", "gemm_cross_out", "gemm_condition"
  * (the projections of sc_condition_append), "row_scale" (no launch of its
- * own any more: always 0).  A projection's time includes the launch that adds
+ * own any more: always 0), "attention_weigh" (the keys' weights, after the
+ * attention), "condense" (both launches of a fold).  A projection's time includes the launch that adds
  * the parts of a split contraction.  Enabling clears earlier records.  Events
  * are created lazily and reused; the cost is two event records per launch. */
 int sc_timer_enable(int on);
@@ -39,7 +40,8 @@ int sc_timer_read(const char* kind, int32_t* launches, double* total_ms);
  * query rows per work-group (bf16: 32 with a node's keys split over the waves,
  * 64, 128 or 256 with a unit's keys in order; fp32: 16); *ring: K/V tiles in
  * the LDS ring of a unit form, else 1; *pieces: key-range pieces that each
- * unit of the last round is cut into (1: none).
+ * unit of the last round is cut into (1: none).  A plan of sc_plan_share that
+ * reads its prefix once for all rows has minus the pieces of the prefix there.
  * sc_gemm_form: the projection of the given timer kind ("gemm_qkv", "gemm_out",
  * "gemm_up", "gemm_down", "gemm_cross_q", "gemm_cross_out", "gemm_condition")
  * at n_features x n_tokens outputs over k, in a block or a condition call.

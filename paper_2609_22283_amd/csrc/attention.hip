@@ -407,11 +407,21 @@ static double makespan(int64_t slots, const double* count, const double* us, int
   double end = 0.0;
   for (int k = 0; k < classes; ++k)
     for (double left = count[k]; left > 0;) {
+      double early = lv[0].at, late = lv[0].at;
+      for (int i = 1; i < n; ++i) {
+        early = std::min(early, lv[i].at);
+        late = std::max(late, lv[i].at);
+      }
+      if (left >= 2 * slots && late - early <= us[k]) {  // a round moves every slot on alike
+        const double rounds = std::floor(left / slots) - 1;
+        for (int i = 0; i < n; ++i) lv[i].at += rounds * us[k];
+        end = std::max(end, late + rounds * us[k]);
+        left -= rounds * slots;
+      }
       int first = 0;
       for (int i = 1; i < n; ++i)
         if (lv[i].at < lv[first].at) first = i;
       const double take = std::min(left, lv[first].free);
-      // whole rounds of the earliest slots at once, as long as no other slot is earlier
       const double at = lv[first].at + us[k];
       end = std::max(end, at);
       left -= take;
@@ -477,31 +487,34 @@ static ShareSchedule find_share_schedule(const sc_plan* p, const sc_cache* c, si
     const double o_units = (double)H * n * ((p->nq + bq - 1) / bq);
     const bool waves = p->shared && bq == WV_BQ && ot_max <= kOwnWaveTiles;
     const int64_t cut = pt ? pt : ot_max;
-    // lengths of a piece: the whole segment, then shorter by an eighth or so each
-    for (int64_t len = cut; len >= 1; len -= std::max<int64_t>(1, len / 16)) {
-      const int64_t pp = (pt + len - 1) / len, oo = waves ? 1 : (ot_max + len - 1) / len;
-      const size_t bytes = (size_t)((pp + oo) * H * rows) * (d.head_dim + 2) * sizeof(float);
-      if (bytes > room || pp * p_units + oo * o_units > INT32_MAX / 2) continue;
-      const double ot = (double)share_tiles(c, sh, own) / n;
-      const double count[] = {(double)(pt / len) * p_units, pt % len ? p_units : 0.0,
-                              waves ? std::ceil(o_units / WV_NW) : o_units * std::ceil(ot / len)};
-      const double us[] = {a * len + f, a * (double)(pt % len) + f,
-                           waves ? 6.0 + 0.9 * ot : a * std::min<double>(len, ot) + f};
-      const double cus = std::min<double>(kCUs, std::ceil((pt ? pp * p_units : count[2]) / per));
-      const double t = std::max(makespan(slots, count, us, 3), page_bytes / std::min(5e6, 25e3 * cus) + 3.0) +
-                       (double)bytes / 5e6 + 4.0 + 0.2e-6 * (double)bytes;
-      if (t < best.us - 1e-9) {
-        best.whole_lists = false;
-        best.sh = sh;
-        best.p_tiles = (int32_t)len;
-        best.o_tiles = (int32_t)(waves ? ot_max : len);
-        best.p_pieces = (int32_t)pp;
-        best.o_pieces = (int32_t)oo;
-        best.own_waves = waves;
-        best.bytes = bytes;
-        best.us = t;
+    // lengths of a piece: the whole prefix, then shorter by a sixteenth each; own pages
+    // in pieces of the same length, or whole
+    for (int64_t len = cut; len >= 1; len -= std::max<int64_t>(1, len / 16))
+      for (const int64_t o_len : {std::min(len, ot_max), ot_max}) {
+        if (waves && o_len != ot_max) continue;
+        const int64_t pp = (pt + len - 1) / len, oo = (ot_max + o_len - 1) / o_len;
+        const size_t bytes = (size_t)((pp + oo) * H * rows) * (d.head_dim + 2) * sizeof(float);
+        if (bytes > room || pp * p_units + oo * o_units > INT32_MAX / 2) continue;
+        const double ot = (double)share_tiles(c, sh, own) / n;
+        const double count[] = {(double)(pt / len) * p_units, pt % len ? p_units : 0.0,
+                                waves ? std::ceil(o_units / WV_NW) : o_units * std::ceil(ot / o_len)};
+        const double us[] = {a * len + f, a * (double)(pt % len) + f,
+                             waves ? 6.0 + 0.9 * ot : a * std::min<double>(o_len, ot) + f};
+        const double cus = std::min<double>(kCUs, std::ceil((pt ? pp * p_units : count[2]) / per));
+        const double t = std::max(makespan(slots, count, us, 3), page_bytes / std::min(5e6, 25e3 * cus) + 3.0) +
+                         (double)bytes / 5e6 + 4.0 + 0.2e-6 * (double)bytes;
+        if (t < best.us - 1e-9) {
+          best.whole_lists = false;
+          best.sh = sh;
+          best.p_tiles = (int32_t)len;
+          best.o_tiles = (int32_t)o_len;
+          best.p_pieces = (int32_t)pp;
+          best.o_pieces = (int32_t)oo;
+          best.own_waves = waves;
+          best.bytes = bytes;
+          best.us = t;
+        }
       }
-    }
     if (f32) break;
   }
   return best;
@@ -535,6 +548,7 @@ static int share_check(const sc_plan* p, const sc_cache* c) {
 static int launch_share(const sc_plan* p, const sc_cache* c, int32_t layer, const void* q, void* o, float* lse,
                         float scale, void* ws, const ShareSchedule& s, hipStream_t stream) {
   if (s.whole_lists) return launch_scheduled(p, c, layer, q, o, true, lse, scale, ws, s.lists, stream);
+  if (!s.sh.bq) return fail(SC_EUNSUPPORTED, "no way to run %zu rows over a shared prefix", p->nodes.size() * (size_t)p->nq);
   if (reinterpret_cast<uintptr_t>(ws) & 15) return fail(SC_EINVAL, "workspace must be 16-byte aligned");
   const sc_cache_desc& d = c->d;
   LseGeom g = attn_geom(p, c, layer, scale);

@@ -299,6 +299,7 @@ int sc::block_forward(const sc_block_weights* w, sc_cache* c, int32_t layer, con
     ahead.passed(2);  // w_o and w_q: their GEMMs are behind this attention
     {
       TimerAlias alias(TK_ATTENTION, TK_CROSS_ATTENTION);
+      const Weighing none(nullptr, nullptr, nullptr);  // only the self-attention's keys are weighed
       if ((rc = launch_attention(cr->plan, cr->cache, layer, qb, ob, 1.0f / std::sqrt((float)d.head_dim),
                                  attn_ws, attention_workspace_bound(), stream)) != SC_OK)
         return rc;

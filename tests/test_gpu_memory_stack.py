@@ -6,7 +6,6 @@ against single blocks and sc_attention_weigh on their queries; the pipeline with
 memory: as long as the memory holds one chunk whole, a window of W and the memory
 are a window of W + 1, and later it is a fold.
 """
-import numpy as np
 import pytest
 
 import paper_2609_22283_amd as sc
@@ -56,8 +55,8 @@ def _rope_table():
 
 
 def test_block_over_a_shared_prefix():
-    """Two nodes reading chunks 0 and 1 as a shared prefix beside a window of two, and as
-    part of a window of four (clean history: the same keys)."""
+    """Two nodes that read chunk 1 as a shared prefix beside a window of two, and by a sparse
+    window of four (clean history: the same keys)."""
     torch = torch_mod()
     w = _layers(1)[0]
     nodes = [(4, 1), (5, 2)]
@@ -67,9 +66,8 @@ def test_block_over_a_shared_prefix():
     got = []
     for shared in (True, False):
         cache = _cache(1, [(c, 0) for c in range(5)], 8)
-        # node (4, 1) reads 2 and 3, or 0 .. 3; node (5, 2) reads 3 and 4, or 1 .. 4
-        plan = sc.sc_plan_build(sc.sc_selection_build("clean", 4, 2 if shared else 4, nodes), cache)
         if shared:
+            plan = sc.sc_plan_build(sc.sc_selection_build("clean", 4, 2, nodes), cache)
             plan = sc.sc_plan_share(plan, [(1, 0)])
         else:
             mask = [[1, 1, 0, 0]] * 5

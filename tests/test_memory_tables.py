@@ -140,3 +140,16 @@ def test_condense_refusals():
     states = [(c, 0) for c in range(801)]
     _reserve(wide, states)
     assert _code(wide.condense, 0, 1, states[:800], states[800], PTR, PTR) == sc.SC_EUNSUPPORTED
+
+
+def test_share_own_lists_longer_than_the_prefix():
+    """Rows for which two partials each have room and three do not, lists of more than 800
+    pages, and own lists twice the prefix's length: one piece of each."""
+    cache = _cache(n_slots=400, ppc=40, layers=1, heads=10)
+    pack = [(c, 0) for c in range(3, 7)]
+    _reserve(cache, [(c, 0) for c in range(9)])
+    plan = sc.sc_plan_build(sc.sc_selection_build("clean", 4, 3, pack), cache)
+    plan = sc.sc_plan_share(plan, [(7, 0), (8, 0)])
+    queries, _, pieces = sc.sc_attention_form(plan, cache)
+    assert queries > 0 and pieces == -1
+    assert sc.sc_attention_workspace_bytes(plan, cache) == 2 * 4 * 2560 * 10 * 130 * 4
