@@ -22,6 +22,7 @@
 #include <cstring>
 #include <map>
 #include <mutex>
+#include <new>
 
 #include "attention_core.h"
 
@@ -520,11 +521,21 @@ static ShareSchedule find_share_schedule(const sc_plan* p, const sc_cache* c, si
   return best;
 }
 
-// Found once per plan, for the few rooms that its calls ask for.
+// Found once per plan, for the few rooms that its calls ask for.  Where host memory
+// runs out, one that fits no call (its bytes exceed any workspace).
 static const ShareSchedule& share_schedule(const sc_plan* p, const sc_cache* c, size_t room, bool lse) {
   for (const auto& s : p->share)
     if (s->room == room && s->lse == lse) return *s;
-  p->share.push_back(std::make_shared<ShareSchedule>(find_share_schedule(p, c, room, lse)));
+  try {
+    p->share.push_back(std::make_shared<ShareSchedule>(find_share_schedule(p, c, room, lse)));
+  } catch (const std::bad_alloc&) {
+    static const ShareSchedule none = [] {
+      ShareSchedule s;
+      s.bytes = SIZE_MAX / 2;
+      return s;
+    }();
+    return none;
+  }
   return *p->share.back();
 }
 

@@ -176,7 +176,8 @@ __global__ __launch_bounds__(CG_T) void condense_gather_kernel(CondenseGeom g, C
   const auto page_of = [&](int32_t i) { return (int32_t)fast_div((uint32_t)i, g.tpp_div); };
   if ((int32_t)blockIdx.x < k_blocks) {
     constexpr int U = HD * sizeof(E) / 16;  // 16-byte units of a K row
-    const int32_t i = (int32_t)blockIdx.x * CG_T + (int32_t)threadIdx.x, row = i / U, u = i % U;
+    static_assert(CG_T % U == 0, "a work-group copies whole rows");
+    const int32_t row = (int32_t)blockIdx.x * (CG_T / U) + (int32_t)threadIdx.x / U, u = (int32_t)threadIdx.x % U;
     if (row >= g.n) return;
     const int32_t from = kept[row], p = page_of(from), t = from - p * g.tpp, f = page_of(row), to = row - f * g.tpp;
     const int32_t src = slots.slot[p], dst = slots.slot[g.n_src + f];

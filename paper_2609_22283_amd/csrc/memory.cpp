@@ -89,8 +89,13 @@ extern "C" int sc_cache_weights_clear(const sc_cache* c, sc_node st, float* weig
 }
 
 extern "C" size_t sc_attention_weigh_workspace_bytes(const sc_plan* p, const sc_cache* c) {
-  if (!p || !c || p->cache != c || p->nodes.empty() || attention_check(p, c) != SC_OK) return 0;
-  return weigh_attention_bytes(p, c);
+  size_t need = 0;
+  guarded([&]() -> int {
+    if (!p || !c || p->cache != c || p->nodes.empty() || attention_check(p, c) != SC_OK) return SC_EINVAL;
+    need = weigh_attention_bytes(p, c);
+    return SC_OK;
+  });
+  return need;
 }
 
 // What the weighing of a plan needs besides the attention itself.

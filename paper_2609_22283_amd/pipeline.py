@@ -60,7 +60,7 @@ class StackPipeline:
         self.weights = None  # accumulated attention weight of every cached key
         if memory:
             d = cache.desc
-            self.weights = torch.zeros((d.n_layers, d.n_slots, d.n_heads, d.tokens_per_page),
+            self.weights = torch.empty((d.n_layers, d.n_slots, d.n_heads, d.tokens_per_page),
                                        dtype=torch.float32, device=xs.device)
             self.kept = torch.empty((d.n_layers, d.n_heads, self.n_tok), dtype=torch.int32, device=xs.device)
             self.weigh_ws = [torch.empty(0, dtype=torch.uint8, device=xs.device)]
