@@ -1,6 +1,6 @@
 """Cache.condense against a sort: the numbers each head keeps, and the pages and
 weights gathered by them, bit for bit.  Ties, zeros, infinities and NaN among the
-weights, one source and many, sources in any order, layers of their own, the three
+weights, one source and many, sources in any order, layers of their own, the
 ways a head's weights are held, and rolling one memory state forward."""
 import pytest
 import torch
@@ -60,8 +60,10 @@ CASES = [  # dtype, heads, head dim, tokens per page, pages per state, sources, 
     ("bf16", 2, 64, 104, 3, 5, 1),
     ("f32", 2, 64, 104, 3, 2, 1),
     ("f32", 1, 128, 40, 1, 7, 2),
-    ("bf16", 2, 128, 1560, 3, 3, 1),      # weights in the larger LDS array
-    ("bf16", 1, 128, 1560, 3, 8, 1),      # 37440 tokens: read again in each pass
+    ("bf16", 2, 128, 1560, 3, 1, 1),      # 4680 tokens: 8 of a thread's of 1024
+    ("bf16", 2, 128, 1560, 3, 3, 1),      # 14040 tokens: 16
+    ("bf16", 1, 128, 1560, 3, 8, 1),      # 37440 tokens: 40
+    ("bf16", 1, 128, 1560, 3, 9, 1),      # 42120 tokens: read again in each pass
 ]
 
 
@@ -102,6 +104,31 @@ def test_condense_some_layers_then_the_rest():
     assert e.value.code == sc.SC_EEXIST
     _check(case, w, states, (5, 0), 0, 1)
     _check(case, w, states, (5, 0), 3, 1)
+
+
+def test_condense_captured():
+    """Captured and replayed: each replay folds by the weights that it finds."""
+    states = [(c, 0) for c in range(3)]
+    case = MemCache("bf16", 2, 128, 72, 2, states, layers=2, seed=105)
+    w = case.weights()
+    kept = torch.empty((2, 2, case.n), dtype=torch.int32, device="cuda")
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g, stream=torch.cuda.Stream()):
+        case.cache.condense(0, 2, states, (3, 0), w, kept)
+    for _ in range(3):
+        w.copy_(torch.exp(case.normal(w.shape)))
+        before = w.clone()
+        g.replay()
+        torch.cuda.synchronize()
+        for l in range(2):
+            want = _want(case, before, states, l)
+            assert torch.equal(kept[l].long(), want)
+            k, v = (torch.cat([case.kv[s][l][i] for s in states]).transpose(0, 1) for i in (0, 1))
+            pick = want[..., None].expand(-1, -1, 128)
+            gk, gv = case.pages((3, 0), l)
+            assert torch.equal(gk, torch.gather(k, 1, pick).transpose(0, 1))
+            assert torch.equal(gv, torch.gather(v, 1, pick).transpose(0, 1))
 
 
 def test_rolling_memory():
