@@ -8,9 +8,9 @@
 // second Q K^T is all that is computed; the probabilities are never stored.  A
 // work-group owns keys, holds them in registers and streams through the rows of
 // every node that reads them.  Keys read by the same nodes are taken together, page
-// after page.  Where that leaves CUs idle, the rows are split over work-groups, whose
-// sums a second launch adds in their order: no atomics, so equal calls give equal
-// bits.
+// after page.  Their rows are cut into items of about one length, a work-group each
+// (keys that more nodes read are cut into more), whose sums a second launch adds in
+// their order: no atomics, so equal calls give equal bits.
 #include <algorithm>
 #include <climits>
 #include <cmath>
@@ -21,13 +21,13 @@
 
 namespace sc {
 
-constexpr int kWeighPages = 512, kWeighGroups = 64;
+constexpr int kWeighPages = 512, kWeighGroups = 64, kWeighSplits = 32;
 
 // Pages in groups with the same readers (bit i: node i).
 struct WeighPlan {
   uint64_t readers[kWeighGroups];
   int32_t page0[kWeighGroups + 1];  // a group's pages are page_slot[page0[g] .. page0[g + 1])
-  int32_t block0[kWeighGroups];     // its first key block (INT32_MAX past the last group)
+  int32_t item0[kWeighGroups];      // its first item of a head (INT32_MAX past the last group)
   int32_t page_slot[kWeighPages];
 };
 
@@ -35,31 +35,45 @@ struct WeighGeom {
   const char* layer_base;
   uint64_t slot_bytes;
   float* weights;    // this layer's
-  float* part;       // [split][head][key of the launch] sums of the splits' rows, if splits > 1
+  float* part;       // [split][head][key of the launch] sums of the splits' rows, where a group has several
   const float* lse;  // [head][row]
-  int32_t n_heads, tpp, nq, rows, blocks, splits, keys;  // keys: of the launch
+  int32_t n_heads, tpp, nq, rows, items, len, keys;  // items of a head, row tiles of one at most, keys of the launch
   DivMagic tpp_div, nq_div;
   float unit;       // bf16: |scale| log2(e)
   float scale;      // fp32
   uint32_t q_flip;  // bf16: sign bits of a negative scale
 };
 
-// A work-group's keys: those of block `blk` of KB keys, and the rows that read them.
+// Tiles of QB rows of a group's readers.
+template <int QB>
+__host__ __device__ __forceinline__ int32_t weigh_tiles(uint64_t readers, int32_t nq) {
+  return (__builtin_popcountll(readers) * nq + QB - 1) / QB;
+}
+
+// A work-group's work: KB keys of a group, and tiles [t, t_end) of QB rows of those that
+// read them (split `split` of `splits`).
 struct WeighItem {
-  int32_t head, split, key0, n_keys, page0;  // key0: first key within the group's n_keys
+  int32_t head, split, splits, key0, n_keys, page0;  // key0: first key within the group's n_keys
+  int32_t n_rows, t, t_end;
   uint64_t readers;
 };
-__device__ __forceinline__ WeighItem weigh_item(const WeighPlan& plan, const WeighGeom& g, int32_t kb) {
+template <int KB, int QB>
+__device__ __forceinline__ WeighItem weigh_item(const WeighPlan& plan, const WeighGeom& g) {
   const int32_t i = (int32_t)xcd_remap(blockIdx.x, gridDim.x);  // an XCD's work-groups share the rows of a few heads
   WeighItem it;
-  it.head = i / (g.blocks * g.splits);
-  it.split = i / g.blocks % g.splits;
-  const int32_t blk = i % g.blocks;
-  const int32_t grp = __builtin_popcountll(__builtin_amdgcn_ballot_w64(plan.block0[threadIdx.x & 63] <= blk)) - 1;
+  it.head = i / g.items;
+  const int32_t at = i % g.items;
+  const int32_t grp = __builtin_popcountll(__builtin_amdgcn_ballot_w64(plan.item0[threadIdx.x & 63] <= at)) - 1;
   it.readers = plan.readers[grp];
   it.page0 = plan.page0[grp];
   it.n_keys = (plan.page0[grp + 1] - it.page0) * g.tpp;
-  it.key0 = (blk - plan.block0[grp]) * kb;
+  it.n_rows = __builtin_popcountll(it.readers) * g.nq;
+  const int32_t blocks = (it.n_keys + KB - 1) / KB, tiles = weigh_tiles<QB>(it.readers, g.nq);
+  it.splits = (tiles + g.len - 1) / g.len;
+  it.split = (at - plan.item0[grp]) / blocks;  // the keys of a split side by side: they share its rows
+  it.key0 = (at - plan.item0[grp]) % blocks * KB;
+  it.t = (int32_t)((int64_t)it.split * tiles / it.splits);
+  it.t_end = (int32_t)((int64_t)(it.split + 1) * tiles / it.splits);
   return it;
 }
 
@@ -98,7 +112,7 @@ typedef float f32x4a __attribute__((ext_vector_type(4), aligned(4)));
 __device__ __forceinline__ void add_weights(const WeighPlan& plan, const WeighGeom& g, const WeighItem& it, int32_t key,
                                             const f32x4& w) {
   if (key >= it.n_keys) return;
-  if (g.splits > 1) {
+  if (it.splits > 1) {
     float* p = g.part + ((size_t)it.split * g.n_heads + it.head) * g.keys + it.page0 * g.tpp + key;
     *reinterpret_cast<f32x4a*>(p) = w;
     return;
@@ -124,7 +138,13 @@ __device__ __forceinline__ void dma16_at(const char* p, uint32_t lds) {
 
 // bf16: four waves of 16 KW keys each, which stay in registers as the A operand of
 // S^T = K Q^T; tiles of 64 rows of q go through LDS (two buffers, 16-byte columns
-// swizzled by the row), shared by the waves.
+// swizzled by the row), shared by the waves.  The keys are what stays because the sums
+// are theirs: they grow in registers over all rows, where a work-group that kept rows
+// would have to add its part of every key's sum to memory.  Bound by the MFMAs under
+// the power cap, exponentials beside them: four nodes of 4680 rows over windows of 21
+// frames of 1560 keys, 12 heads (1.9 TFLOP), 1.69 ms, 1.1 PFLOP/s where a large
+// library product reaches 1.23; three of 792 rows over seven states of 792 keys
+// 60 us (0.68 PFLOP/s: last round, ragged tiles).
 constexpr int WG_NW = 4, WG_QB = 64;
 template <int KW>
 __global__ __launch_bounds__(64 * WG_NW, 2) void weigh_bf16_kernel(const uint16_t* __restrict__ q, WeighGeom g,
@@ -133,7 +153,7 @@ __global__ __launch_bounds__(64 * WG_NW, 2) void weigh_bf16_kernel(const uint16_
   __shared__ int32_t nodes[kMaxNodes];
   const int32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int32_t lg = lane >> 4, c = lane & 15;
-  const WeighItem it = weigh_item(plan, g, 16 * KW * WG_NW);
+  const WeighItem it = weigh_item<16 * KW * WG_NW, WG_QB>(plan, g);
   if (wave == 0) list_readers(it.readers, lane, nodes);
   const int32_t key0 = it.key0 + 16 * KW * wave;
   bf16x8 kf[KW][4];
@@ -150,7 +170,7 @@ __global__ __launch_bounds__(64 * WG_NW, 2) void weigh_bf16_kernel(const uint16_
     }
   }
   __syncthreads();
-  const int32_t n_rows = __builtin_popcountll(it.readers) * g.nq;
+  const int32_t n_rows = it.n_rows;
   const char* qh = reinterpret_cast<const char*>(q) + (size_t)it.head * (HDB * 2);
   const size_t row_bytes = (size_t)g.n_heads * (HDB * 2);
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(tiles[0])) + 4096 * wave;
@@ -170,9 +190,8 @@ __global__ __launch_bounds__(64 * WG_NW, 2) void weigh_bf16_kernel(const uint16_
   f32x4 w[KW];
 #pragma unroll
   for (int b = 0; b < KW; ++b) w[b] = f32x4{};
-  const int32_t tiles_in_all = (n_rows + WG_QB - 1) / WG_QB;
-  int32_t t = (int32_t)((int64_t)it.split * tiles_in_all / g.splits);
-  const int32_t t_end = (int32_t)((int64_t)(it.split + 1) * tiles_in_all / g.splits);
+  int32_t t = it.t;
+  const int32_t t_end = it.t_end;
   float lse = 0.f;
   if (t < t_end) lse = fetch(t, t & 1);
   for (; t < t_end; ++t) {
@@ -216,7 +235,7 @@ __global__ __launch_bounds__(64 * WF_NW) void weigh_f32_kernel(const float* __re
   __shared__ int32_t nodes[kMaxNodes];
   const int32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int32_t lg = lane >> 4, c = lane & 15;
-  const WeighItem it = weigh_item(plan, g, WF_KB);
+  const WeighItem it = weigh_item<WF_KB, WF_QB>(plan, g);
   if (wave == 0) list_readers(it.readers, lane, nodes);
   const int32_t key0 = it.key0 + 16 * wave;
   const WeighKey k = weigh_key(plan, g, it, key0 + c);
@@ -226,7 +245,7 @@ __global__ __launch_bounds__(64 * WF_NW) void weigh_f32_kernel(const float* __re
 #pragma unroll
   for (int j = 0; j < NJ; ++j) kf[j] = *reinterpret_cast<const f32x4u*>(kp + 16 * j) * g.scale;
   __syncthreads();
-  const int32_t n_rows = __builtin_popcountll(it.readers) * g.nq;
+  const int32_t n_rows = it.n_rows;
   const char* qh = reinterpret_cast<const char*>(q) + (size_t)it.head * ROW;
   const size_t row_bytes = (size_t)g.n_heads * ROW;
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(tiles[0])) + 1024 * CP * wave;
@@ -242,9 +261,8 @@ __global__ __launch_bounds__(64 * WF_NW) void weigh_f32_kernel(const float* __re
     return r < n_rows ? l : INFINITY;
   };
   f32x4 w = {};
-  const int32_t tiles_in_all = (n_rows + WF_QB - 1) / WF_QB;
-  int32_t t = (int32_t)((int64_t)it.split * tiles_in_all / g.splits);
-  const int32_t t_end = (int32_t)((int64_t)(it.split + 1) * tiles_in_all / g.splits);
+  int32_t t = it.t;
+  const int32_t t_end = it.t_end;
   float lse = 0.f;
   if (t < t_end) lse = fetch(t, t & 1);
   for (; t < t_end; ++t) {
@@ -277,16 +295,24 @@ __global__ __launch_bounds__(64 * WF_NW) void weigh_f32_kernel(const float* __re
   if (c == 0) add_weights(plan, g, it, key0 + 4 * lg, w);
 }
 
-// Adds the splits' sums, in their order: four keys of a head to a thread.
+// Adds the splits' sums, in their order: four keys of a head to a thread.  QB: the
+// rows of a tile.
+template <int QB>
 __global__ __launch_bounds__(256) void weigh_add_kernel(WeighGeom g, WeighPlan plan) {
   const int32_t key = 4 * (int32_t)(blockIdx.x * 256 + threadIdx.x), head = blockIdx.y;
   if (key >= g.keys) return;
   const int32_t p = (int32_t)fast_div((uint32_t)key, g.tpp_div);
+  int32_t grp = 0;
+#pragma unroll
+  for (int step = kWeighGroups / 2; step; step /= 2)
+    if (plan.page0[grp + step] <= p) grp += step;
+  const int32_t splits = (weigh_tiles<QB>(plan.readers[grp], g.nq) + g.len - 1) / g.len;
+  if (splits == 1) return;
   const float* part = g.part + (size_t)head * g.keys + key;
   const size_t stride = (size_t)g.n_heads * g.keys;
   f32x4 w = *reinterpret_cast<const f32x4a*>(part);
 #pragma unroll 4
-  for (int32_t s = 1; s < g.splits; ++s) w += *reinterpret_cast<const f32x4a*>(part + s * stride);
+  for (int32_t s = 1; s < splits; ++s) w += *reinterpret_cast<const f32x4a*>(part + s * stride);
   f32x4a* to = reinterpret_cast<f32x4a*>(g.weights + ((size_t)plan.page_slot[p] * g.n_heads + head) * g.tpp + (key - p * g.tpp));
   *to = *to + w;
 }
@@ -300,67 +326,69 @@ __global__ __launch_bounds__(256) void weights_clear_kernel(float* weights, size
   for (size_t i = threadIdx.x; i < slot_floats; i += 256) p[i] = 0.f;
 }
 
-// A plan's distinct pages by their readers, most readers first (the longest
-// work-groups start first), in launches of bounded argument size.  A property of
-// the plan alone: found on its first use and kept in it.
-// How a launch runs: 16-key blocks per wave (bf16) and splits of the rows.
+// How a launch runs: 16-key blocks per wave (bf16), row tiles of an item at most,
+// items of a head, keys, and the most splits of a group.
 struct WeighForm {
-  int32_t kw, splits, blocks, keys;
+  int32_t kw, len, items, keys, splits;
 };
+// A plan's distinct pages by their readers, most readers first, in launches of
+// bounded argument size.  A property of the plan alone: found on its first use and
+// kept in it.
 struct WeighLaunches {
   std::vector<WeighPlan> plans;
   std::vector<WeighForm> forms;
   size_t part_bytes;  // the most that a launch's splits leave
 };
 
-// Key blocks of kb keys of a launch; block0 of its groups is set.
-static int32_t key_blocks(WeighPlan& plan, int32_t tpp, int32_t kb) {
-  int64_t n = 0;
-  for (int32_t i = 0; i < kWeighGroups; ++i) {
-    const int64_t keys = (int64_t)(plan.page0[i + 1] - plan.page0[i]) * tpp;
-    plan.block0[i] = keys ? (int32_t)n : INT32_MAX;
-    n += (keys + kb - 1) / kb;
-  }
-  return (int32_t)n;
-}
-
-// The cheapest form by estimated time.  Measured, per 64-row tile and work-group with
-// two of them to a CU: 2.1 us with 256 keys (1.07 PFLOP/s), 1.2 with 128, 0.8 with
-// 64, whose rows feed fewer products per LDS read; 4.5, 3 and 2.5 us to bring the
-// keys; fp32: 2.9 us per 32 rows and 128 keys, one to a CU, and 3.  All
-// work-groups' time over the slots, half of the longest one's tiles, and 5 us for
-// the launch that adds splits.  (Three nodes of 792 rows over windows of seven, 12
-// heads: 256 keys 93 us whole, 70 + 5 in halves, 64 + 5 in thirds, 71 + 5 in
-// sixths; 128 keys 74 and 67 + 5; 64 keys 96.  Four of 4680: 2010 whole, 1780 in
-// halves or quarters.  fp32, four of 312 rows, 2 heads: 114 us whole, 24 in
-// sixths, 21 in twelfths.)
+// The cheapest form by estimated time.  A CU's time per 64-row tile of an item is 1.05
+// us with 256 keys (1.07 PFLOP/s), 0.6 with 128 and 0.4 with 64, whose rows feed fewer
+// products per LDS read, and 2.2, 1.5 and 1.2 to bring the keys; fp32 2.9 us per 32
+// rows and 128 keys of 128 channels, and 3.  Items in rounds over the CUs (a work-group by
+// itself takes 1.6 times its share), what the longest one is longer than the mean, and 5 us for
+// the launch that adds splits.  Measured with the attention before it: three nodes of
+// 792 rows over windows of seven, 12 heads: 159 us with 128 keys in whole rows, 154 with
+// 256 in items of 8 to 12 tiles, 160 of 3; four of 4680: 5168 whole, 4970 in
+// items of 74, 5060 of 16; fp32, four of 312 rows, 2 heads: 76 us in items of 12, 59
+// of 4, 65 of 3.
 static WeighForm weigh_form(WeighPlan& plan, const sc_cache* c, int32_t nq) {
   const bool f32 = c->d.dtype == SC_DTYPE_F32;
   const int32_t tpp = c->d.tokens_per_page, H = c->d.n_heads;
-  WeighForm best{1, 1, 0, 0};
+  const auto tiles_of = [&](int32_t i) {
+    return f32 ? weigh_tiles<WF_QB>(plan.readers[i], nq) : weigh_tiles<WG_QB>(plan.readers[i], nq);
+  };
+  int32_t most = 1;
+  for (int32_t i = 0; i < kWeighGroups; ++i) most = std::max(most, tiles_of(i));
+  WeighForm best{1, most, 0, 0, 1};
   double best_us = 1e30;
   for (int32_t kw = f32 ? 1 : 4; kw >= 1; kw /= 2) {
-    const int32_t kb = f32 ? WF_KB : 16 * kw * WG_NW, rows = f32 ? WF_QB : WG_QB;
-    const double t = f32 ? 2.9 : kw == 4 ? 2.1 : kw == 2 ? 1.2 : 0.8, slots = f32 ? kCUs : 2 * kCUs;
-    const double f = f32 ? 3.0 : kw == 4 ? 4.5 : kw == 2 ? 3.0 : 2.5;
-    double tiles = 0.0, most = 0.0;
-    int64_t blocks = 0, keys = 0;
-    for (int32_t i = 0; i < kWeighGroups; ++i) {
-      const int64_t k = (int64_t)(plan.page0[i + 1] - plan.page0[i]) * tpp, b = (k + kb - 1) / kb;
-      const double r = std::ceil((double)__builtin_popcountll(plan.readers[i]) * nq / rows);
-      keys += k;
-      blocks += b;
-      tiles += (double)b * r;
-      if (b) most = std::max(most, r);
-    }
-    for (int32_t s = 1; s <= 16 && s <= most; ++s) {
-      const double per = std::ceil(most / s);
-      const double us = H * (tiles * t + (double)blocks * s * f) / slots + 0.5 * per * t + (s > 1 ? 5.0 : 0.0);
-      if (us < best_us * 0.97 && blocks * H * s < INT32_MAX) {
+    const int32_t kb = f32 ? WF_KB : 16 * kw * WG_NW;
+    const double t = f32 ? 2.9 * c->d.head_dim / 128 : kw == 4 ? 1.05 : kw == 2 ? 0.6 : 0.4;
+    const double f = f32 ? 3.0 : kw == 4 ? 2.2 : kw == 2 ? 1.5 : 1.2;
+    for (int32_t s = 1; s <= kWeighSplits && s <= most; ++s) {
+      const int32_t len = (most + s - 1) / s;
+      double tiles = 0.0;
+      int64_t items = 0, keys = 0;
+      for (int32_t i = 0; i < kWeighGroups; ++i) {
+        const int64_t k = (int64_t)(plan.page0[i + 1] - plan.page0[i]) * tpp, b = (k + kb - 1) / kb;
+        keys += k;
+        tiles += (double)b * tiles_of(i);
+        items += b * ((tiles_of(i) + len - 1) / len);
+      }
+      const double rounds = std::max(std::ceil((double)items * H / kCUs), f32 ? 1.0 : 1.6);
+      const double mean = tiles / (double)items;
+      const double us = rounds * (mean * t + f) + (len - mean) * (f32 ? t : 2.0 * t) + (len < most ? 5.0 : 0.0);
+      if (us < best_us * 0.99 && items * H < INT32_MAX) {
         best_us = us;
-        best = WeighForm{kw, s, (int32_t)blocks, (int32_t)keys};
+        best = WeighForm{kw, len, (int32_t)items, (int32_t)keys, (most + len - 1) / len};
       }
     }
+  }
+  int64_t items = 0;
+  for (int32_t i = 0; i < kWeighGroups; ++i) {
+    const int32_t kb = f32 ? WF_KB : 16 * best.kw * WG_NW;
+    const int64_t b = ((int64_t)(plan.page0[i + 1] - plan.page0[i]) * tpp + kb - 1) / kb;
+    plan.item0[i] = b ? (int32_t)items : INT32_MAX;
+    items += b * ((tiles_of(i) + best.len - 1) / best.len);
   }
   return best;
 }
@@ -400,7 +428,6 @@ static const WeighLaunches* weigh_launches(const sc_plan* p, const sc_cache* c) 
   out->part_bytes = 0;
   for (WeighPlan& w : out->plans) {
     const WeighForm f = weigh_form(w, c, p->nq);
-    key_blocks(w, c->d.tokens_per_page, c->d.dtype == SC_DTYPE_F32 ? WF_KB : 16 * f.kw * WG_NW);
     out->forms.push_back(f);
     if (f.splits > 1)
       out->part_bytes = std::max(out->part_bytes, (size_t)f.splits * c->d.n_heads * f.keys * sizeof(float));
@@ -433,10 +460,10 @@ static int launch_weigh(const sc_plan* p, const sc_cache* c, int32_t layer, cons
   for (size_t i = 0; i < all->plans.size(); ++i) {
     const WeighPlan& plan = all->plans[i];
     const WeighForm& f = all->forms[i];
-    g.blocks = f.blocks;
-    g.splits = f.splits;
+    g.items = f.items;
+    g.len = f.len;
     g.keys = f.keys;
-    const dim3 grid((uint32_t)(f.blocks * d.n_heads * f.splits));
+    const dim3 grid((uint32_t)(f.items * d.n_heads));
     timer_begin(TK_ATTN_WEIGH, stream);
     if (d.dtype == SC_DTYPE_F32) {
       const float* qf = static_cast<const float*>(q);
@@ -453,9 +480,13 @@ static int launch_weigh(const sc_plan* p, const sc_cache* c, int32_t layer, cons
       else
         hipLaunchKernelGGL((weigh_bf16_kernel<1>), grid, dim3(64 * WG_NW), 0, stream, qb, g, plan);
     }
-    if (f.splits > 1)
-      hipLaunchKernelGGL(weigh_add_kernel, dim3((uint32_t)((f.keys / 4 + 255) / 256), (uint32_t)d.n_heads), dim3(256), 0,
-                         stream, g, plan);
+    if (f.splits > 1) {
+      const dim3 adds((uint32_t)((f.keys / 4 + 255) / 256), (uint32_t)d.n_heads);
+      if (d.dtype == SC_DTYPE_F32)
+        hipLaunchKernelGGL(weigh_add_kernel<WF_QB>, adds, dim3(256), 0, stream, g, plan);
+      else
+        hipLaunchKernelGGL(weigh_add_kernel<WG_QB>, adds, dim3(256), 0, stream, g, plan);
+    }
     timer_end(TK_ATTN_WEIGH, stream);
     SC_HIP(hipGetLastError());
   }
