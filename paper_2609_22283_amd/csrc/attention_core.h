@@ -1732,7 +1732,9 @@ __global__ __launch_bounds__(256) void attn_combine_kernel(uint16_t* __restrict_
 // Merges the partials of a SharePlan's rows: the prefix's pieces, then those of the
 // row's own node, in that order.  GR groups of 32 lanes share a row (and each
 // holds 4 of its HD outputs per lane, or 2): one group where the partials are
-// few, eight where there are many and the chain of loads would set the time.
+// few, eight where there are many and the chain of loads would set the time.  Bound
+// by launch and latency: 32 rows of 12 heads and 18 partials 4 us, 2048 and 4 (50 MB)
+// 11 us.
 template <int HD, int GR, int KH>
 __global__ __launch_bounds__(256) void attn_share_combine_kernel(void* __restrict__ o, LseGeom g, SharePlan plan) {
   constexpr int V = HD / 32;
