@@ -26,17 +26,19 @@ static void launch_main(const AttnShape& sh, uint32_t items, const typename M::G
   }
   const uint16_t* qb = static_cast<const uint16_t*>(q);
   uint16_t* ob = static_cast<uint16_t*>(o);
-  if (sh.bq == WV_BQ)
+  if (sh.bq == WV_BQ) {
     hipLaunchKernelGGL((attn_waves_kernel<NoAhead, M>), dim3(items), dim3(64 * WV_NW), 0, stream, qb, ob, g, plan,
                        NoAhead{});
-  else if (sh.bq == BQ_TINY && sh.ring == 4)
+  } else if (sh.bq == BQ_TINY && (M::kShare || sh.ring == 4)) {  // a SharePlan's ring is 4 always
     hipLaunchKernelGGL((attn_bf16_kernel<2, 1, 4, M>), dim3(items), dim3(128), 0, stream, qb, ob, g, plan);
-  else if (sh.bq == BQ_TINY)
-    hipLaunchKernelGGL((attn_bf16_kernel<2, 1, 3, M>), dim3(items), dim3(128), 0, stream, qb, ob, g, plan);
-  else if (sh.bq == BQ_SMALL)
+  } else if (sh.bq == BQ_TINY) {
+    if constexpr (!M::kShare)
+      hipLaunchKernelGGL((attn_bf16_kernel<2, 1, 3, M>), dim3(items), dim3(128), 0, stream, qb, ob, g, plan);
+  } else if (sh.bq == BQ_SMALL) {
     hipLaunchKernelGGL((attn_bf16_kernel<4, 2, 2, M>), dim3(items), dim3(256), 0, stream, qb, ob, g, plan);
-  else
+  } else {
     hipLaunchKernelGGL((attn_bf16_kernel<8, 2, 2, M>), dim3(items), dim3(512), 0, stream, qb, ob, g, plan);
+  }
   timer_end(TK_ATTENTION, stream);
 }
 
