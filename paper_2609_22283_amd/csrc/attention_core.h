@@ -667,7 +667,11 @@ __device__ __forceinline__ void probs_tile(const STile<KH>& s, bf16x8 (&pb)[KH][
 // p ^ swizzle(row).  K rows of keys past the node's end fetch its last key,
 // V^T columns the tile's first key (valid memory; their probabilities are
 // zero).
-template <int NW, int KH>
+// KEPT: every copy's lane offsets stay in registers, for the plain forms, which have
+// room for them (four nodes of 4680 queries over 32760 keys, 12 heads: 2.899 ms so, 2.922
+// otherwise).  The exact forms have none to spare and derive them from the first
+// copies'.
+template <int NW, int KH, bool KEPT>
 struct KvTiles {
   static constexpr int BK = Tile<KH>::BK;
   static constexpr int KCP = BK / (4 * NW), VCP = BK / (4 * NW);
@@ -689,6 +693,8 @@ struct KvTiles {
   uint32_t kl0;      // K: the first row's bytes and the swizzled column
   uint32_t vl[KH];   // V^T: rows of even and odd copies (their swizzles alternate), with the key's bytes
   int32_t vk0;       // key offset in the tile, of even copies
+  uint32_t klane[KEPT ? KCP : 1], vlane[KEPT ? VCP : 1];  // KEPT: of every copy
+  int32_t vkeys[KEPT ? VCP : 1];
 
   template <class Plan>
   __device__ __forceinline__ KvTiles(const Plan& plan, const AttnGeom& g, int32_t node, int32_t head,
@@ -711,10 +717,23 @@ struct KvTiles {
     vk0 = 8 * (vp ^ (int32_t)vswz<KH>(vrow0));
 #pragma unroll
     for (int j = 0; j < KH; ++j) vl[j] = (uint32_t)vrow0 * tpp * 2 + (uint32_t)vkey(j) * 2;  // plus key t0 * 2
+    if constexpr (KEPT) {
+#pragma unroll
+      for (int j = 0; j < KCP; ++j) {
+        const int32_t row = krow0 + 4 * j;
+        klane[j] = (uint32_t)row * 256 + ((kp ^ kswz(row)) << 4);
+      }
+#pragma unroll
+      for (int j = 0; j < VCP; ++j) {
+        const int32_t d = vrow0 + RPI * j;
+        vkeys[j] = 8 * (vp ^ (int32_t)vswz<KH>(d));
+        vlane[j] = (uint32_t)d * tpp * 2 + (uint32_t)vkeys[j] * 2;
+      }
+    }
   }
   __device__ __forceinline__ int32_t vkey(int j) const { return KH == 2 ? vk0 ^ (32 * (j & 1)) : vk0; }
   // Offset of K copy j from that of the first (kl: kl0).
-  static __device__ __forceinline__ uint32_t klane(uint32_t kl, int j) { return kl ^ (kswz(4 * j) << 4); }
+  static __device__ __forceinline__ uint32_t kxor(uint32_t kl, int j) { return kl ^ (kswz(4 * j) << 4); }
   // Page slots of the tile starting at key t0 >= 0 (two scalar loads),
   // fetched ahead of the copy that uses them so their latency overlaps other
   // work (a step, or the barrier wait before the copy).  Clamped to the
@@ -736,14 +755,23 @@ struct KvTiles {
     const uint32_t lo = sl.lo + khead + (uint32_t)(t0 - sl.plo * tpp) * 256;
     const uint32_t hi = sl.hi + khead + (uint32_t)(t0 - bkey) * 256;
     const int32_t lim = nk - t0, split = bkey - t0;
+    if constexpr (KEPT) {
+#pragma unroll
+      for (int j = 0; j < KCP; ++j) {
+        const int32_t rg = 4 * KCP * wave + 4 * j;  // first tile row of this copy (wave-uniform)
+        const uint32_t src = rg >= lim ? kbad + (klane[j] & 255u) : (rg >= split ? hi : lo) + klane[j];
+        dma16(lbase, src, kl + rg * 256);
+      }
+      return;
+    }
     uint32_t k = kl0;
     asm volatile("" : "+v"(k));  // the offsets are made here, not kept
 #pragma unroll
     for (int j = 0; j < KCP; ++j) {
-      const int32_t rg = 4 * KCP * wave + 4 * j;  // first tile row of this copy (wave-uniform)
+      const int32_t rg = 4 * KCP * wave + 4 * j;
       const bool past = rg >= lim;
       const uint32_t base = past ? kbad : (rg >= split ? hi : lo) + 1024u * j;
-      dma16(lbase, base + (klane(k, j) & (past ? 255u : ~0u)), kl + rg * 256);
+      dma16(lbase, base + (kxor(k, j) & (past ? 255u : ~0u)), kl + rg * 256);
     }
   }
   // A V^T row holds the tile's BK keys; a page boundary or the node's end
@@ -758,18 +786,18 @@ struct KvTiles {
       for (int j = 0; j < VCP; ++j) {
         // opaque, so the offset stays one add of the scalar base (the
         // compiler otherwise re-derives it with a per-lane multiply)
-        uint32_t off = vl[j % KH];
+        uint32_t off = KEPT ? vlane[KEPT ? j : 0] : vl[j % KH];
         asm volatile("" : "+v"(off));
-        dma16(lbase, lo + (uint32_t)(RPI * 2 * j) * tpp + off, vt + (RPI * VCP * wave + RPI * j) * 2 * BK);
+        dma16(lbase, lo + (KEPT ? 0u : (uint32_t)(RPI * 2 * j) * tpp) + off, vt + (RPI * VCP * wave + RPI * j) * 2 * BK);
       }
       return;
     }
     const uint32_t hi = sl.hi + vhead + (uint32_t)(t0 - bkey) * 2;
 #pragma unroll
     for (int j = 0; j < VCP; ++j) {
-      const int32_t rk = vkey(j);
+      const int32_t rk = KEPT ? vkeys[KEPT ? j : 0] : vkey(j);
       const bool in = rk < lim;
-      const uint32_t at = vl[j % KH] + (uint32_t)(RPI * 2 * j) * tpp, off = in ? at : at - (uint32_t)rk * 2;
+      const uint32_t at = KEPT ? vlane[KEPT ? j : 0] : vl[j % KH] + (uint32_t)(RPI * 2 * j) * tpp, off = in ? at : at - (uint32_t)rk * 2;
       const uint32_t base = (in && rk >= split) ? hi : lo;
       dma16(lbase, base + off, vt + (RPI * VCP * wave + RPI * j) * 2 * BK);
     }
@@ -1010,10 +1038,6 @@ __device__ __forceinline__ void attn_step(char* smem, const AttnLane& L, const b
     for (int i = 0; i < NF; ++i) {
       const bf16x8 f = ring[i % PF];
       if (i + PF < NF) ring[i % PF] = frag(i + PF);
-      if (i < NE) {
-#pragma unroll
-        for (int x = i * 32 / NE; x < (i + 1) * 32 / NE; ++x) prob(x);
-      }
       if (i < NKF) {  // K fragment (ds, h, b) = (i / 4, i / 2 mod 2, i mod 2), as in qk_tile
         const int ds = i >> 2, h = (i >> 1) & 1, b = i & 1;
         sn[h][b][0] = mfma16(f, qreg[0][ds], sn[h][b][0]);
@@ -1022,6 +1046,10 @@ __device__ __forceinline__ void attn_step(char* smem, const AttnLane& L, const b
         const int j = i - NKF, h = j >> 3, db = j & 7;
         oacc[0][db] = mfma16(f, pb[h][0], oacc[0][db]);
         oacc[1][db] = mfma16(f, pb[h][1], oacc[1][db]);
+      }
+      if (i < NE) {
+#pragma unroll
+        for (int x = i * 32 / NE; x < (i + 1) * 32 / NE; ++x) prob(x);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -1074,7 +1102,7 @@ __device__ __forceinline__ void attn_step(char* smem, const AttnLane& L, const b
 // that maximum (every p <= 1).  Single-buffered K and V tiles; slow, and
 // taken only for logits far above the first tile's maximum.
 template <class M, int NW, int KH>
-__device__ __forceinline__ void attn_exact(char* smem, const KvTiles<NW, KH>& kv, const AttnLane& L,
+__device__ __forceinline__ void attn_exact(char* smem, const KvTiles<NW, KH, !M::kLse>& kv, const AttnLane& L,
                                            const bf16x8 (&qreg)[2][4], f32x4 (&oacc)[2][8], float (&m)[2],
                                            float (&l)[2], int32_t ta, int32_t ntiles, int32_t lg, float unit) {
   constexpr int BK = Tile<KH>::BK;
@@ -1104,7 +1132,7 @@ __device__ __forceinline__ void attn_exact(char* smem, const KvTiles<NW, KH>& kv
     for (int db = 0; db < 8; ++db) oacc[qb][db] = f32x4{};
   }
   for (int32_t t = ta; t < ntiles; ++t) {
-    const typename KvTiles<NW, KH>::Slots sl = kv.slots(t * BK);
+    const typename KvTiles<NW, KH, !M::kLse>::Slots sl = kv.slots(t * BK);
     kv.copy_k(t * BK, kl, sl);
     kv.copy_v(t * BK, vl, sl);
     landed();
@@ -1153,7 +1181,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 || D == 4 ? 1 : 2) void attn_bf16_
   const int32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);  // wave-uniform: LDS copy addresses stay scalar
   const int32_t lg = lane >> 4, c = lane & 15;
   if (tid == 0) any_bad = 0;
-  const KvTiles<NW, KH> kv(plan, g, it.node, it.head, wave, lane);
+  const KvTiles<NW, KH, !M::kLse> kv(plan, g, it.node, it.head, wave, lane);
   const int32_t nk = kv.nk;
   const bool ragged = it.tb == it.ntiles && (nk % BK) != 0;
   bf16x8 qreg[2][4];
@@ -1178,7 +1206,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 || D == 4 ? 1 : 2) void attn_bf16_
     constexpr bool ACT = decltype(act)::value;
     // prologue: K(ta), V(ta), K(ta+1) in flight; S(ta) = K(ta) Q^T; m = its exact column maxima
     {
-      const typename KvTiles<NW, KH>::Slots s0 = kv.slots(ta * BK);
+      const typename KvTiles<NW, KH, !M::kLse>::Slots s0 = kv.slots(ta * BK);
       kv.copy_k(ta * BK, smem, s0);
       kv.copy_v(ta * BK, smem + 2 * KT_BYTES, s0);
       if (ta + 1 < ntiles) kv.copy_k((ta + 1) * BK, smem + KT_BYTES, kv.slots((ta + 1) * BK));
@@ -1207,8 +1235,8 @@ __global__ __launch_bounds__(64 * NW, NW == 8 || D == 4 ? 1 : 2) void attn_bf16_
     // iteration t (buffer parity counted from ta): copy K(t+2) over K(t) and
     // V(t+1) over V(t-1), then step t
     int32_t t = ta;
-    typename KvTiles<NW, KH>::Slots sk = kv.slots(min(ta + 2, it.ntiles - 1) * BK);
-    typename KvTiles<NW, KH>::Slots sv = kv.slots(min(ta + 1, it.ntiles - 1) * BK);
+    typename KvTiles<NW, KH, !M::kLse>::Slots sk = kv.slots(min(ta + 2, it.ntiles - 1) * BK);
+    typename KvTiles<NW, KH, !M::kLse>::Slots sv = kv.slots(min(ta + 1, it.ntiles - 1) * BK);
     for (; t + 2 < ntiles; t += 2) {
       kv.copy_k((t + 2) * BK, smem, sk);
       kv.copy_v((t + 1) * BK, smem + 2 * KT_BYTES + VT_BYTES, sv);
@@ -1274,7 +1302,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 || D == 4 ? 1 : 2) void attn_bf16_
   // in flight, counted exactly (a pair past the item's end issues nothing).
   auto run_ring = [&](auto act) __attribute__((always_inline)) {
     constexpr bool ACT = decltype(act)::value;
-    using KV = KvTiles<NW, KH>;
+    using KV = KvTiles<NW, KH, !M::kLse>;
     constexpr int32_t KC = KV::KCP, VC = KV::VCP;
     static_assert(KC % 2 == 0 && VC % 2 == 0 && (D - 2) * (KC + VC) <= 16, "wait counts of landed_but");
     const int32_t n = ntiles - ta;
@@ -1395,8 +1423,8 @@ static_assert(WV_NW * (Tile<1>::KT_BYTES + Tile<1>::VT_BYTES) <= WV_RED, "the wa
 // A tile of one wave's own: the copies of KvTiles<1, 1>, four to an M0 setting.
 // (The biased offsets stay below 2^32: a group's first rows lie at least
 // kCopyBias bytes before the end of the slot.)
-struct WaveTiles : KvTiles<1, 1> {
-  using Base = KvTiles<1, 1>;
+struct WaveTiles : KvTiles<1, 1, false> {
+  using Base = KvTiles<1, 1, false>;
   const char* biased;
   template <class Plan>
   __device__ __forceinline__ WaveTiles(const Plan& plan, const AttnGeom& g, int32_t node, int32_t head,
@@ -1413,7 +1441,7 @@ struct WaveTiles : KvTiles<1, 1> {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int32_t rg = 16 * h + 4 * j;
-        const uint32_t k = klane(kl0, 4 * h + j);
+        const uint32_t k = kxor(kl0, 4 * h + j);
         off[j] = (rg >= lim ? kbad + (k & 255u) : (rg >= split ? hi : lo) + 1024u * (4 * h + j) + k) +
                  (kCopyBias - 1024 * j);
       }
