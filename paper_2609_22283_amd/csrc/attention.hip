@@ -453,7 +453,7 @@ static double makespan(int64_t slots, const double* count, const double* us, int
 }
 
 // The cheapest way within `room` bytes of partials, by estimated time in us: the
-// items' times as in attn_schedule (fp32: 0.36 us per 16-key tile of 128 channels and
+// items' times as in attn_schedule (fp32: 0.32 us per 16-key tile of 128 channels and
 // 6), dealt out in their order; no less than the
 // pages take from HBM, at 5 MB per us and 25 KB per us of a CU (what the copies in
 // flight of a work-group fetch); the partials written at the same rate and read by
@@ -475,7 +475,7 @@ static ShareSchedule find_share_schedule(const sc_plan* p, const sc_cache* c, si
     best.whole_lists = true;
     if (f32) {
       const double tiles = (double)share_tiles(c, {}, (int64_t)p->page_slot.size()) / n;
-      best.us = std::ceil((double)n * H * ((p->nq + F32_BQ - 1) / F32_BQ) / kCUs) * (6.0 + 0.36 * d.head_dim / 128 * tiles);
+      best.us = std::ceil((double)n * H * ((p->nq + F32_BQ - 1) / F32_BQ) / kCUs) * (6.0 + 0.32 * d.head_dim / 128 * tiles);
     } else {
       best.lists = attn_schedule(p, c, std::min(room, workspace_schedule(p, c).partial_bytes()));
       best.bytes = best.lists.partial_bytes();
@@ -490,7 +490,7 @@ static ShareSchedule find_share_schedule(const sc_plan* p, const sc_cache* c, si
     if (f32) sh = AttnShape{F32_BQ, 0, 1};
     if (!f32 && d.tokens_per_page < 32 * sh.kh) continue;
     const int32_t bq = sh.bq, per = f32 || bq == WV_BQ ? 1 : per_cu(sh), slots = kCUs * per;
-    const double a = f32 ? 0.36 * d.head_dim / 128 : (bq == BQ_MAX ? 1.5 : bq == BQ_SMALL ? 1.6 : bq == BQ_TINY ? 2.0 : 0.44) * sh.kh / 2;
+    const double a = f32 ? 0.32 * d.head_dim / 128 : (bq == BQ_MAX ? 1.5 : bq == BQ_SMALL ? 1.6 : bq == BQ_TINY ? 2.0 : 0.44) * sh.kh / 2;
     const double f = f32 ? 6.0 : bq == BQ_MAX ? 6.0 : bq == BQ_SMALL ? 8.0 : bq == BQ_TINY ? 2.5 : 6.5;
     const int64_t pt = p->shared ? share_tiles(c, sh, p->shared) : 0, ot_max = share_tiles(c, sh, own_max);
     const double p_units = p->shared ? (double)H * ((rows + bq - 1) / bq) : 0.0;

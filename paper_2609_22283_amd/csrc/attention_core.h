@@ -43,7 +43,7 @@ struct AttnGeom {
 
 // What the forms that give the rows' logarithmic sums (LseAttn, ShareAttn) need beside.
 struct LseGeom : AttnGeom {
-  float* lse;             // [head][row] log2 (fp32 caches: natural log) of the row's sum, or null
+  float* lse;             // [head][row] log2 of the row's sum, or null
   float unit;             // |scale| log2(e); fp32 caches: 1
   uint32_t q_flip;        // bf16: sign bits of a negative scale
   int32_t rows;           // rows of the pack, n_nodes * nq
@@ -219,7 +219,10 @@ __device__ __forceinline__ void reads_done() { asm volatile("s_waitcnt lgkmcnt(0
 // over K(t) once that has been read and V(t + 1) likewise, and takes the operands from
 // there.  The loads above put adjacent lanes on adjacent rows, so each of their 16
 // bytes is a cache access of its own.  16 x 100 rows over 12384 keys, 12 heads of 64:
-// 669 us (91 TFLOP/s of 154), 834 without.
+// 582 us (105 TFLOP/s of 154), 834 without.  Of the vector instructions between the
+// products (the products of 16 queries leave little room for them) those forms take the
+// exponentials to base 2 (one instruction; the plain form calls expf) and the copies'
+// addresses from lane offsets that no tile changes: 695 us before.
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 constexpr int F32_NW = 8, F32_BQ = 16, F32_BK = 16;
 
@@ -255,7 +258,7 @@ __global__ __launch_bounds__(64 * F32_NW) void attn_f32_kernel(const float* __re
   f32x4 qr[NJ], acc[NJ];
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
-    qr[j] = *reinterpret_cast<const f32x4u*>(q + qoff + 16 * j) * g.scale;
+    qr[j] = *reinterpret_cast<const f32x4u*>(q + qoff + 16 * j) * (M::kLse ? g.scale_log2 : g.scale);
     acc[j] = f32x4{};
   }
   const int32_t p0 = plan.page_off[node], npages = plan.page_off[node + 1] - p0;
@@ -280,104 +283,189 @@ __global__ __launch_bounds__(64 * F32_NW) void attn_f32_kernel(const float* __re
   char* const kl = smem + wave * 2 * TILE;
   char* const vl = kl + TILE;
   const auto slot_base = [&](int32_t pg) { return g.layer_base + (size_t)plan.page_slot[p0 + pg] * g.slot_bytes; };
-  const auto stage_k = [&]() __attribute__((always_inline)) {
-    constexpr int LPR = ROW / 16;  // lanes per row
-    const char* base = slot_base(page) + (size_t)head * g.tpp * ROW;
+  // A lane's part of the addresses is the same in every tile that lies whole in its
+  // page.  Copies go out in fours, with one M0 (copy_group): K copy j adds 1024 j to both
+  // addresses and its own bits of the swizzle, V^T copy j 16 rows.
+  constexpr int LPR = ROW / 16, RPC = 64 / LPR;  // lanes of a K row, K rows of a copy
+  const int32_t kr0 = lane / LPR, kcol0 = (lane % LPR) ^ kr0, vkey0 = 4 * ((lane & 3) ^ (lane >> 4));
+  const uint32_t klane0 = (uint32_t)kr0 * ROW + 16 * kcol0;
+  uint32_t vlane[STAGED ? CP : 1];
+  if constexpr (STAGED)
 #pragma unroll
-    for (int j = 0; j < CP; ++j) {
-      const int32_t r = (64 / LPR) * j + lane / LPR, col = (lane % LPR) ^ r;
-      dma16(base, (uint32_t)min(F32_BK * tt + r, g.tpp - 1) * ROW + 16 * col, kl + 1024 * j);
+    for (int j = 0; j < CP; ++j)
+      vlane[j] = ((uint32_t)(16 * j + (lane >> 2)) * g.tpp + vkey0) * 4 + (kCopyBias - 1024 * (j & 3));
+  const auto stage_k = [&](int32_t page, int32_t tt) __attribute__((always_inline)) {
+    const char* base = slot_base(page) + ((size_t)head * g.tpp + F32_BK * tt) * ROW;
+    const int32_t past = g.tpp - F32_BK * tt;  // rows from here on lie past the page's end
+#pragma unroll
+    for (int h = 0; h < CP / 4; ++h) {
+      uint32_t off[4];
+      if (past >= F32_BK) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) off[j] = klane0 ^ (16 * RPC * (4 * h + j));
+        copy_group<4>(base + 4096 * h, off, lds_addr(kl) + 4096 * h);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int32_t r = RPC * (4 * h + j) + kr0;
+          off[j] = (uint32_t)min(r, past - 1) * ROW + 16 * (kcol0 ^ (RPC * (4 * h + j))) + (kCopyBias - 1024 * j);
+        }
+        copy_group<4>(base - kCopyBias, off, lds_addr(kl) + 4096 * h);
+      }
     }
   };
-  const auto stage_v = [&]() __attribute__((always_inline)) {
-    const char* base = slot_base(page) + g.kv_half + (size_t)head * g.tpp * ROW;
+  const auto stage_v = [&](int32_t page, int32_t tt) __attribute__((always_inline)) {
+    const char* base = slot_base(page) + g.kv_half + (size_t)head * g.tpp * ROW - kCopyBias;
+    const int32_t key = F32_BK * tt;
 #pragma unroll
-    for (int j = 0; j < CP; ++j) {
-      const int32_t d = 16 * j + (lane >> 2), key = F32_BK * tt + 4 * ((lane & 3) ^ (d >> 2 & 3));
-      dma16(base, ((uint32_t)d * g.tpp + (key < g.tpp ? key : 0)) * 4, vl + 1024 * j);
+    for (int h = 0; h < CP / 4; ++h) {
+      if (key + F32_BK <= g.tpp) {
+        copy_group<4>(base + 4 * key, vlane + 4 * h, lds_addr(vl) + 4096 * h);
+      } else {
+        uint32_t off[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) off[j] = vlane[4 * h + j] + (key + vkey0 < g.tpp ? 4 * key : -4 * vkey0);
+        copy_group<4>(base, off, lds_addr(vl) + 4096 * h);
+      }
     }
   };
+  const auto ex = [](float x) { return M::kLse ? __builtin_amdgcn_exp2f(x) : expf(x); };
   float m = -INFINITY, l = 0.f;
   f32x4 kf[NJ];
-  if (t < t_end) {
-    if constexpr (STAGED) {
-      stage_k();
-      stage_v();
-    } else {
-      load_k(kf);
-    }
-  }
-  while (t < t_end) {
-    const int32_t k0 = F32_BK * tt + 4 * lg;  // this lane's first key of the tile, within the page
-    f32x4 vf[NJ];
-    if constexpr (STAGED) {
-      copies_landed<CP>();  // K(t); V(t) may still be under way
+  if constexpr (STAGED) {
+    // fragments are read out of LDS ahead of the products that need them: V^T(t) while the
+    // softmax runs, K(t + 1) while V^T(t) is multiplied
+    int32_t kpage = page, ktt = tt;  // of the next K tile to copy
+    const auto next = [&](int32_t& pg, int32_t& tl) __attribute__((always_inline)) {
+      if (++tl == tp) {
+        tl = 0;
+        ++pg;
+      }
+    };
+    const auto read_k = [&]() __attribute__((always_inline)) {
 #pragma unroll
       for (int j = 0; j < NJ; ++j) kf[j] = *reinterpret_cast<const f32x4*>(kl + c * ROW + (((4 * j + lg) ^ c) << 4));
+    };
+    if (t < t_end) {
+      stage_k(kpage, ktt);
+      stage_v(page, tt);
+      copies_landed<CP>();  // K(t); V^T(t) may still be under way
+      read_k();
       reads_done();
-    } else {
+      next(kpage, ktt);
+      if (t + 1 < t_end) stage_k(kpage, ktt);
+    }
+    for (; t < t_end; ++t) {
+      const bool more = t + 1 < t_end;
+      f32x4 s0 = {}, s1 = {};
+#pragma unroll
+      for (int j = 0; j < NJ; j += 2)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[j][e], qr[j][e], s0, 0, 0, 0);
+          s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[j + 1][e], qr[j + 1][e], s1, 0, 0, 0);
+        }
+      if (more)
+        copies_landed<CP>();  // V^T(t); K(t + 1) may still be under way
+      else
+        copies_landed<0>();
+      f32x4 vf[NJ];
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) vf[j] = *reinterpret_cast<const f32x4*>(vl + (16 * j + c) * 64 + ((lg ^ (c >> 2)) << 4));
+      const int32_t k0 = F32_BK * tt + 4 * lg;  // this lane's first key of the tile, within the page
+      f32x4 s = s0 + s1;
+      if (k0 + 4 > g.tpp) s = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};  // pages hold whole runs of 8 keys
+      float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+      mx = fmaxf(mx, __shfl_xor(mx, 16));
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      const float mn = fmaxf(m, mx);
+      if (__builtin_amdgcn_ballot_w64(mn > m)) {
+        const float alpha = mn == -INFINITY ? 1.f : ex(m - mn);
+        l *= alpha;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[j] *= alpha;
+        m = mn;
+      }
+      const float ms = m == -INFINITY ? 0.f : m;  // every logit so far -inf: no weight yet
+      f32x4 p;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) p[e] = ex(s[e] - ms);
+      l += (p[0] + p[1]) + (p[2] + p[3]);
+      reads_done();
+      if (F32_BK * tt + F32_BK > g.tpp) {  // the page ends in this tile
+        asm volatile("");  // a branch, not a selection in every tile
+        if (k0 >= g.tpp)
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) vf[j] = f32x4{};
+      }
+      if (more) {
+        next(page, tt);
+        stage_v(page, tt);
+        copies_landed<CP>();  // K(t + 1)
+        read_k();
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[j][e], p[e], acc[j], 0, 0, 0);
+      if (more) {
+        reads_done();
+        next(kpage, ktt);
+        if (t + 2 < t_end) stage_k(kpage, ktt);
+      }
+    }
+  } else {
+    if (t < t_end) load_k(kf);
+    while (t < t_end) {
+      const int32_t k0 = F32_BK * tt + 4 * lg;  // this lane's first key of the tile, within the page
+      f32x4 vf[NJ];
       const float* vb = reinterpret_cast<const float*>(g.layer_base + (size_t)plan.page_slot[p0 + page] * g.slot_bytes +
                                                        g.kv_half) +
                         ((size_t)head * HD + c) * g.tpp + (k0 < g.tpp ? k0 : 0);
 #pragma unroll
       for (int j = 0; j < NJ; ++j) vf[j] = *reinterpret_cast<const f32x4u*>(vb + (size_t)16 * j * g.tpp);
-    }
-    const bool page_end = F32_BK * tt + F32_BK > g.tpp;
-    f32x4 s0 = {}, s1 = {};
+      const bool page_end = F32_BK * tt + F32_BK > g.tpp;
+      f32x4 s0 = {}, s1 = {};
 #pragma unroll
-    for (int j = 0; j < NJ; j += 2)
+      for (int j = 0; j < NJ; j += 2)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[j][e], qr[j][e], s0, 0, 0, 0);
-        s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[j + 1][e], qr[j + 1][e], s1, 0, 0, 0);
+        for (int e = 0; e < 4; ++e) {
+          s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[j][e], qr[j][e], s0, 0, 0, 0);
+          s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[j + 1][e], qr[j + 1][e], s1, 0, 0, 0);
+        }
+      ++t;
+      if (++tt == tp) {
+        tt = 0;
+        ++page;
       }
-    ++t;
-    if (++tt == tp) {
-      tt = 0;
-      ++page;
+      const bool more = t < t_end;
+      if (more) load_k(kf);
+      f32x4 s = s0 + s1;
+      if (k0 + 4 > g.tpp) s = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};  // pages hold whole runs of 8 keys
+      float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+      mx = fmaxf(mx, __shfl_xor(mx, 16));
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      const float mn = fmaxf(m, mx);
+      if (__builtin_amdgcn_ballot_w64(mn > m)) {
+        const float alpha = mn == -INFINITY ? 1.f : ex(m - mn);
+        l *= alpha;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[j] *= alpha;
+        m = mn;
+      }
+      const float ms = m == -INFINITY ? 0.f : m;  // every logit so far -inf: no weight yet
+      f32x4 p;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) p[e] = ex(s[e] - ms);
+      l += (p[0] + p[1]) + (p[2] + p[3]);
+      if (page_end && k0 >= g.tpp)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) vf[j] = f32x4{};
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[j][e], p[e], acc[j], 0, 0, 0);
     }
-    const bool more = t < t_end;
-    if (more) {
-      if constexpr (STAGED)
-        stage_k();
-      else
-        load_k(kf);
-    }
-    f32x4 s = s0 + s1;
-    if (k0 + 4 > g.tpp) s = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};  // pages hold whole runs of 8 keys
-    float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
-    mx = fmaxf(mx, __shfl_xor(mx, 16));
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
-    const float mn = fmaxf(m, mx);
-    if (__builtin_amdgcn_ballot_w64(mn > m)) {
-      const float alpha = mn == -INFINITY ? 1.f : expf(m - mn);
-      l *= alpha;
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) acc[j] *= alpha;
-      m = mn;
-    }
-    const float ms = m == -INFINITY ? 0.f : m;  // every logit so far -inf: no weight yet
-    f32x4 p;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) p[e] = expf(s[e] - ms);
-    l += (p[0] + p[1]) + (p[2] + p[3]);
-    if constexpr (STAGED) {
-      if (more)
-        copies_landed<CP>();  // V(t); K(t + 1) may still be under way
-      else
-        copies_landed<0>();
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) vf[j] = *reinterpret_cast<const f32x4*>(vl + (16 * j + c) * 64 + ((lg ^ (c >> 2)) << 4));
-      reads_done();
-      if (more) stage_v();
-    }
-    if (page_end && k0 >= g.tpp)
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) vf[j] = f32x4{};
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[j][e], p[e], acc[j], 0, 0, 0);
   }
   // merge: every wave scales its part to the common maximum, then a tree of
   // LDS additions (a wave without tiles adds zeros), over the tiles
@@ -394,8 +482,8 @@ __global__ __launch_bounds__(64 * F32_NW) void attn_f32_kernel(const float* __re
   // a piece without a finite logit adds zeros to its row
   const float base = M::kShare && mt == -INFINITY ? 0.f : mt;
 #pragma unroll
-  for (int w = 0; w < F32_NW; ++w) lt += ml[1][w][c] * expf(ml[0][w][c] - base);
-  const float f = expf(m - base);
+  for (int w = 0; w < F32_NW; ++w) lt += ml[1][w][c] * ex(ml[0][w][c] - base);
+  const float f = ex(m - base);
 #pragma unroll
   for (int j = 0; j < NJ; ++j) acc[j] *= f;
 #pragma unroll
@@ -424,7 +512,7 @@ __global__ __launch_bounds__(64 * F32_NW) void attn_f32_kernel(const float* __re
   if (wave == 0 && row < g.nq) {
     const float inv = 1.f / lt;
     if constexpr (M::kLse)
-      if (g.lse && lg == 0) g.lse[(size_t)head * g.rows + row0 + row] = mt + logf(lt);
+      if (g.lse && lg == 0) g.lse[(size_t)head * g.rows + row0 + row] = mt + __builtin_amdgcn_logf(lt);
 #pragma unroll
     for (int j = 0; j < NJ; ++j) *reinterpret_cast<f32x4u*>(o + qoff + 16 * j) = acc[j] * inv;
   }
@@ -1775,7 +1863,7 @@ __global__ __launch_bounds__(256) void attn_share_combine_kernel(void* __restric
   const int32_t node = 1 + (int32_t)fast_div((uint32_t)row, g.nq_div);
   const int32_t n = g.p_pieces + (g.own_waves ? 1 : (share_tiles<KH>(plan, g, node) + g.o_tiles - 1) / g.o_tiles);
   const auto at = [&](int32_t p) { return ((size_t)p * g.n_heads + head) * g.rows + row; };
-  const auto ex = [](float x) { return F32 ? expf(x) : __builtin_amdgcn_exp2f(x); };
+  const auto ex = [](float x) { return __builtin_amdgcn_exp2f(x); };
   // the first partials are on their way while the maximum is found
   constexpr int AHEAD = 4;
   const int32_t p0 = GR == 8 ? grp : 0;
@@ -1808,7 +1896,7 @@ __global__ __launch_bounds__(256) void attn_share_combine_kernel(void* __restric
     for (int w = 1; w < 8; ++w) acc += red[w][dl];
   }
   const float inv = 1.f / l;
-  if (g.lse && dl == 0) g.lse[(size_t)head * g.rows + row] = m + (F32 ? logf(l) : __builtin_amdgcn_logf(l));
+  if (g.lse && dl == 0) g.lse[(size_t)head * g.rows + row] = m + __builtin_amdgcn_logf(l);
   const size_t out = ((size_t)row * g.n_heads + head) * HD + V * dl;
   if constexpr (F32) {
     float* op = static_cast<float*>(o) + out;

@@ -108,8 +108,7 @@ int attention_check(const sc_plan* plan, const sc_cache* cache);
 int launch_attention(const sc_plan* plan, const sc_cache* cache, int32_t layer,
                      const void* q, void* o, float scale, void* ws, size_t ws_bytes,
                      hipStream_t stream);
-// The same with the rows' logarithmic sums, fp32 [head][row] (log2; fp32 caches:
-// natural), where lse is not NULL.
+// The same with the rows' logarithmic sums, fp32 [head][row] (log2), where lse is not NULL.
 int launch_attention_lse(const sc_plan* plan, const sc_cache* cache, int32_t layer, const void* q, void* o, float* lse,
                          float scale, void* ws, size_t ws_bytes, hipStream_t stream);
 // Workspace of the attention for a plan (0 for fp32 caches and plans whose units
