@@ -39,11 +39,12 @@ class StackPipeline:
                  xs, noise, policy: str, K: int, W: int, B: int, t_sched: Sequence[float],
                  refresh: bool = True, stream=None, condition=None, memory: bool = False):
         """``memory``: keep one memory state of what leaves the window, of as
-        many tokens as a chunk (the cache needs room for two states more; the
-        modes and hooks are the same).  ``condition``: optional dict with ``cache`` (an sc.Cache holding the
-        condition K/V of every layer), ``cross`` (per layer: (w_q, w_o,
-        q_norm or None)) and ``condition_of`` (chunk -> cached condition
-        state; default (0, 0))."""
+        many tokens as a chunk.  The cache needs room for two states more; the
+        modes are the same, layer hooks are refused, and states cached before
+        the run are left where they are.  ``condition``: optional dict with
+        ``cache`` (an sc.Cache holding the condition K/V of every layer),
+        ``cross`` (per layer: (w_q, w_o, q_norm or None)) and ``condition_of``
+        (chunk -> cached condition state; default (0, 0))."""
         import torch
         self.torch = torch
         self.layers, self.cache, self.rope = list(layers), cache, rope
@@ -60,7 +61,7 @@ class StackPipeline:
         self.weights = None  # accumulated attention weight of every cached key
         if memory:
             d = cache.desc
-            self.weights = torch.empty((d.n_layers, d.n_slots, d.n_heads, d.tokens_per_page),
+            self.weights = torch.zeros((d.n_layers, d.n_slots, d.n_heads, d.tokens_per_page),
                                        dtype=torch.float32, device=xs.device)
             self.kept = torch.empty((d.n_layers, d.n_heads, self.n_tok), dtype=torch.int32, device=xs.device)
             self.weigh_ws = [torch.empty(0, dtype=torch.uint8, device=xs.device)]
@@ -194,8 +195,9 @@ class StackPipeline:
                 e1.record()
                 times.append((e0, e1))
             if kernel_timer_rounds and g == kernel_timer_rounds[1]:
+                folds = () if self.weights is None else ("attention_weigh", "condense")
                 for kind in ("attention", "attention_combine", "gemm_qkv", "gemm_out", "gemm_up",
-                             "gemm_down", "qk_norm", "cross_attention", "gemm_cross_q", "gemm_cross_out"):
+                             "gemm_down", "qk_norm", "cross_attention", "gemm_cross_q", "gemm_cross_out") + folds:
                     self.kernel_times[kind] = sc.sc_timer_read(kind)
                 sc.sc_timer_enable(False)
             if stop_after is not None and g == stop_after:

@@ -187,3 +187,12 @@ def test_pipeline_memory_refuses_layer_hooks():
     p = _pipe(make, memory=True)
     with pytest.raises(ValueError):
         p.run("serial", layer_hooks={0: lambda *a: None})
+
+
+def test_pipeline_memory_times_its_launches():
+    make, _, _, keep = _setup(SMALL, 2, 6, 2, "prog", seed=28, n_slots=100)
+    p = _pipe(make, memory=True)
+    p.run("packed", kernel_timer_rounds=(0, len(p.rounds()) - 1))
+    layers = len(p.layers)
+    assert p.kernel_times["attention_weigh"][0] >= layers * len(p.rounds())
+    assert p.kernel_times["condense"][0] >= 1
