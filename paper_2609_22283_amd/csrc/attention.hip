@@ -565,8 +565,9 @@ static int share_check(const sc_plan* p, const sc_cache* c) {
   return SC_OK;
 }
 
+// left: where not NULL the pieces' partials are left as they are (and o unwritten).
 static int launch_share(const sc_plan* p, const sc_cache* c, int32_t layer, const void* q, void* o, float* lse,
-                        float scale, void* ws, const ShareSchedule& s, hipStream_t stream) {
+                        float scale, void* ws, const ShareSchedule& s, ShareMerge* left, hipStream_t stream) {
   if (s.whole_lists) return launch_scheduled(p, c, layer, q, o, true, lse, scale, ws, s.lists, stream);
   if (!s.sh.bq) return fail(SC_EUNSUPPORTED, "no way to run %zu rows over a shared prefix", p->nodes.size() * (size_t)p->nq);
   if (reinterpret_cast<uintptr_t>(ws) & 15) return fail(SC_EINVAL, "workspace must be 16-byte aligned");
@@ -597,9 +598,27 @@ static int launch_share(const sc_plan* p, const sc_cache* c, int32_t layer, cons
                         (s.own_waves ? (o_units + WV_NW - 1) / WV_NW : o_units * g.o_pieces);
   g.part_o = static_cast<float*>(ws);
   g.part_ml = g.part_o + (size_t)(g.p_pieces + g.o_pieces) * d.n_heads * g.rows * d.head_dim;
-  launch_form<ShareAttn>(s.sh, (uint32_t)items, g, plan, q, o, d.dtype, d.head_dim, stream);
+  if (left) {
+    left->g = g;
+    for (int32_t i = 0; i < g.n_nodes; ++i)
+      left->pieces[i] = (uint8_t)(g.p_pieces + (s.own_waves ? 1 : (share_tiles(c, s.sh, own_pages(p, i)) + g.o_tiles - 1) / g.o_tiles));
+    launch_share_pieces(s.sh, (uint32_t)items, g, plan, q, d.dtype, d.head_dim, stream);
+  } else {
+    launch_form<ShareAttn>(s.sh, (uint32_t)items, g, plan, q, o, d.dtype, d.head_dim, stream);
+  }
   SC_HIP(hipGetLastError());
   return SC_OK;
+}
+
+bool attention_leaves_partials(const sc_plan* p, const sc_cache* c) {
+  const ShareSchedule& s = share_schedule(p, c, attention_workspace_bound(), true);
+  return c->d.dtype == SC_DTYPE_BF16 && !s.whole_lists && s.sh.bq && s.p_pieces + s.o_pieces <= kMergePieces;
+}
+
+int launch_attention_partials(const sc_plan* p, const sc_cache* c, int32_t layer, const void* q, float scale, void* ws,
+                              ShareMerge* left, hipStream_t stream) {
+  return launch_share(p, c, layer, q, nullptr, nullptr, scale, ws, share_schedule(p, c, attention_workspace_bound(), true),
+                      left, stream);
 }
 
 int launch_attention_lse(const sc_plan* p, const sc_cache* c, int32_t layer, const void* q, void* o, float* lse,
@@ -611,7 +630,7 @@ int launch_attention_lse(const sc_plan* p, const sc_cache* c, int32_t layer, con
     return fail(SC_EINVAL, "attention workspace of %zu bytes, need %zu", ws_bytes, need);
   if (p->shared || lse)
     return launch_share(p, c, layer, q, o, lse, scale, ws, share_schedule(p, c, attention_workspace_bound(), lse),
-                        stream);
+                        nullptr, stream);
   const AttnSchedule ts = c->d.dtype == SC_DTYPE_F32 ? AttnSchedule{} : attn_schedule(p, c, need);
   return launch_scheduled(p, c, layer, q, o, false, nullptr, scale, ws, ts, stream);
 }
@@ -702,7 +721,7 @@ extern "C" int sc_attention_noalloc(const sc_plan* p, const sc_cache* c, int32_t
   if (p->shared) {
     const ShareSchedule& s = share_schedule(p, c, kNoAllocScratchBytes, false);
     if (s.us >= 1e30) return fail(SC_ECAPACITY, "the rows sharing a prefix need more partials than the scratch holds");
-    return launch_share(p, c, layer, q, o, nullptr, scale, ptr, s, static_cast<hipStream_t>(stream));
+    return launch_share(p, c, layer, q, o, nullptr, scale, ptr, s, nullptr, static_cast<hipStream_t>(stream));
   }
   AttnSchedule ts{};
   if (ptr) ts = attn_schedule(p, c, std::min(kNoAllocScratchBytes, attention_workspace_bytes(p, c)));

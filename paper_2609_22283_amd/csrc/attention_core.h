@@ -1851,17 +1851,17 @@ __global__ __launch_bounds__(256) void attn_combine_kernel(uint16_t* __restrict_
 // few, eight where there are many and the chain of loads would set the time.  Bound
 // by launch and latency: 32 rows of 12 heads and 18 partials 4 us, 2048 and 4 (50 MB)
 // 11 us.
-template <int HD, int GR, int KH>
-__global__ __launch_bounds__(256) void attn_share_combine_kernel(void* __restrict__ o, LseGeom g, SharePlan plan) {
+// pieces(node): the partials of a row of that node.
+template <int HD, int GR, bool F32, class Pieces>
+__device__ __forceinline__ void share_combine(void* __restrict__ o, const LseGeom& g, int32_t block, int32_t head,
+                                              const Pieces& pieces) {
   constexpr int V = HD / 32;
-  constexpr bool F32 = KH == 0;
   typedef float fv __attribute__((ext_vector_type(V)));
   __shared__ fv red[8][32];
   const int32_t grp = threadIdx.x >> 5, dl = threadIdx.x & 31;
-  const int32_t row = GR == 8 ? (int32_t)blockIdx.x : (int32_t)blockIdx.x * 8 + grp, head = blockIdx.y;
+  const int32_t row = GR == 8 ? block : block * 8 + grp;
   if (row >= g.rows) return;  // the whole work-group where its lanes share a row
-  const int32_t node = 1 + (int32_t)fast_div((uint32_t)row, g.nq_div);
-  const int32_t n = g.p_pieces + (g.own_waves ? 1 : (share_tiles<KH>(plan, g, node) + g.o_tiles - 1) / g.o_tiles);
+  const int32_t n = pieces((int32_t)fast_div((uint32_t)row, g.nq_div));
   const auto at = [&](int32_t p) { return ((size_t)p * g.n_heads + head) * g.rows + row; };
   const auto ex = [](float x) { return __builtin_amdgcn_exp2f(x); };
   // the first partials are on their way while the maximum is found
@@ -1909,6 +1909,19 @@ __global__ __launch_bounds__(256) void attn_share_combine_kernel(void* __restric
     *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(o) + out) = r;
   }
 }
+template <int HD, int GR, int KH>
+__global__ __launch_bounds__(256) void attn_share_combine_kernel(void* __restrict__ o, LseGeom g, SharePlan plan) {
+  share_combine<HD, GR, KH == 0>(o, g, (int32_t)blockIdx.x, (int32_t)blockIdx.y, [&](int32_t node) {
+    return g.p_pieces + (g.own_waves ? 1 : (share_tiles<KH>(plan, g, 1 + node) + g.o_tiles - 1) / g.o_tiles);
+  });
+}
+
+// What is left to merge after a SharePlan's pieces: where their partials lie, and how
+// many of them a row of each node has.
+struct ShareMerge {
+  LseGeom g;
+  uint8_t pieces[kMaxNodes];
+};
 
 // ---------------------------------------------------------------- launches
 // A form of the unit kernel (attn_shape in attention.hip).
@@ -1931,6 +1944,15 @@ struct AttnSchedule {
 template <class M>
 void launch_form(const AttnShape& sh, uint32_t items, const typename M::Geom& g, const typename M::Plan& plan, const void* q,
                  void* o, int32_t dtype, int32_t head_dim, hipStream_t stream);
+// The pieces of a SharePlan alone (attention_lse.hip).
+void launch_share_pieces(const AttnShape& sh, uint32_t items, const LseGeom& g, const SharePlan& plan, const void* q,
+                         int32_t dtype, int32_t head_dim, hipStream_t stream);
+// Whether a row of a plan leaves few partials (bf16, at most kMergePieces), which launch_weigh can
+// merge on its way; and the launch that leaves them (attention.hip).
+constexpr int32_t kMergePieces = 16;
+bool attention_leaves_partials(const sc_plan* p, const sc_cache* c);
+int launch_attention_partials(const sc_plan* p, const sc_cache* c, int32_t layer, const void* q, float scale, void* ws,
+                              ShareMerge* left, hipStream_t stream);
 template <>  // attention_lse.hip
 void launch_form<LseAttn>(const AttnShape&, uint32_t, const LseGeom&, const AttnPlan&, const void*, void*, int32_t,
                           int32_t, hipStream_t);

@@ -59,6 +59,11 @@ void launch_form<LseAttn>(const AttnShape& sh, uint32_t items, const LseGeom& g,
   timer_end(TK_ATTN_COMBINE, stream);
 }
 
+void launch_share_pieces(const AttnShape& sh, uint32_t items, const LseGeom& g, const SharePlan& plan, const void* q,
+                         int32_t dtype, int32_t head_dim, hipStream_t stream) {
+  launch_main<ShareAttn>(sh, items, g, plan, q, nullptr, dtype, head_dim, stream);
+}
+
 template <>
 void launch_form<ShareAttn>(const AttnShape& sh, uint32_t items, const LseGeom& g, const SharePlan& plan,
                             const void* q, void* o, int32_t dtype, int32_t head_dim, hipStream_t stream) {

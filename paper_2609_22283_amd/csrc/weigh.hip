@@ -58,8 +58,8 @@ struct WeighItem {
   uint64_t readers;
 };
 template <int KB, int QB>
-__device__ __forceinline__ WeighItem weigh_item(const WeighPlan& plan, const WeighGeom& g) {
-  const int32_t i = (int32_t)xcd_remap(blockIdx.x, gridDim.x);  // an XCD's work-groups share the rows of a few heads
+__device__ __forceinline__ WeighItem weigh_item(const WeighPlan& plan, const WeighGeom& g, uint32_t block, uint32_t of) {
+  const int32_t i = (int32_t)xcd_remap(block, of);  // an XCD's work-groups share the rows of a few heads
   WeighItem it;
   it.head = i / g.items;
   const int32_t at = i % g.items;
@@ -146,14 +146,15 @@ __device__ __forceinline__ void dma16_at(const char* p, uint32_t lds) {
 // library product reaches 1.23; three of 792 rows over seven states of 792 keys
 // 60 us (0.68 PFLOP/s: last round, ragged tiles).
 constexpr int WG_NW = 4, WG_QB = 64;
-template <int KW>
-__global__ __launch_bounds__(64 * WG_NW, 2) void weigh_bf16_kernel(const uint16_t* __restrict__ q, WeighGeom g,
-                                                                   WeighPlan plan) {
+// lse_of(head, row): a row's logarithmic sum.
+template <int KW, class Lse>
+__device__ __forceinline__ void weigh_bf16(const uint16_t* __restrict__ q, const WeighGeom& g, const WeighPlan& plan,
+                                           uint32_t block, uint32_t of, const Lse& lse_of) {
   __shared__ __attribute__((aligned(1024))) char tiles[2][WG_QB * HDB * 2];
   __shared__ int32_t nodes[kMaxNodes];
   const int32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int32_t lg = lane >> 4, c = lane & 15;
-  const WeighItem it = weigh_item<16 * KW * WG_NW, WG_QB>(plan, g);
+  const WeighItem it = weigh_item<16 * KW * WG_NW, WG_QB>(plan, g, block, of);
   if (wave == 0) list_readers(it.readers, lane, nodes);
   const int32_t key0 = it.key0 + 16 * KW * wave;
   bf16x8 kf[KW][4];
@@ -184,7 +185,7 @@ __global__ __launch_bounds__(64 * WG_NW, 2) void weigh_bf16_kernel(const uint16_
       const int32_t src = __shfl(row, tr);
       dma16_at(qh + (size_t)src * row_bytes + ((c ^ (tr & 15)) << 4), lds0 + buf * (WG_QB * HDB * 2) + 1024 * j);
     }
-    const float l = g.lse[(size_t)it.head * g.rows + row];
+    const float l = lse_of(it.head, row);
     return r < n_rows ? l : INFINITY;
   };
   f32x4 w[KW];
@@ -225,6 +226,47 @@ __global__ __launch_bounds__(64 * WG_NW, 2) void weigh_bf16_kernel(const uint16_
   }
 }
 
+template <int KW>
+__global__ __launch_bounds__(64 * WG_NW, 2) void weigh_bf16_kernel(const uint16_t* __restrict__ q, WeighGeom g,
+                                                                   WeighPlan plan) {
+  weigh_bf16<KW>(q, g, plan, blockIdx.x, gridDim.x,
+                 [&](int32_t head, int32_t row) { return g.lse[(size_t)head * g.rows + row]; });
+}
+
+// The same after an attention that left few partials per row and has not merged them: the
+// first work-groups do that, the others take the rows' sums from the partials themselves.
+// One launch less, where a row tile or two are all that a work-group streams.  12 heads,
+// with the attention: 64 rows over 21 x 64 keys 14.5 us, 17.3 apart; 128 over 11 x 128
+// 19.6 against 22.1; 64 over 7 x 64 12.9 against 15.2.  (Up to 32 partials, taken eight at
+// a time, cost more than the launch: 23.8 for the second.)
+template <int KW>
+__global__ __launch_bounds__(64 * WG_NW, 2) void weigh_merge_kernel(const uint16_t* __restrict__ q,
+                                                                    uint16_t* __restrict__ o, WeighGeom g, WeighPlan plan,
+                                                                    ShareMerge left, int32_t merges) {
+  if ((int32_t)blockIdx.x < merges) {
+    const int32_t per = (left.g.rows + 7) / 8;
+    share_combine<HDB, 1, false>(o, left.g, (int32_t)blockIdx.x % per, (int32_t)blockIdx.x / per,
+                                 [&](int32_t node) { return (int32_t)left.pieces[node]; });
+    return;
+  }
+  weigh_bf16<KW>(q, g, plan, blockIdx.x - merges, gridDim.x - merges, [&](int32_t head, int32_t row) {
+    const float* ml = left.g.part_ml + 2 * ((size_t)head * g.rows + row);
+    const size_t stride = 2 * (size_t)g.n_heads * g.rows;
+    const int32_t n = left.pieces[fast_div((uint32_t)row, g.nq_div)];
+    float m[kMergePieces], l[kMergePieces], top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int p = 0; p < kMergePieces; ++p) {
+      m[p] = p < n ? ml[p * stride] : -INFINITY;
+      l[p] = p < n ? ml[p * stride + 1] : 0.f;
+    }
+#pragma unroll
+    for (int p = 0; p < kMergePieces; ++p) top = fmaxf(top, m[p]);
+#pragma unroll
+    for (int p = 0; p < kMergePieces; ++p) sum += __builtin_amdgcn_exp2f(m[p] - top) * l[p];
+    return top + __builtin_amdgcn_logf(sum);
+  });
+}
+
 // fp32: the same with eight waves of 16 keys, 32-row tiles and fp32 MFMAs, whose
 // contraction index of product (j, e) in lane group g is channel 16 j + 4 g + e.
 // Bound by the fp32 MFMAs: four nodes of 312 rows over windows of four, 12 heads of 128
@@ -237,7 +279,7 @@ __global__ __launch_bounds__(64 * WF_NW) void weigh_f32_kernel(const float* __re
   __shared__ int32_t nodes[kMaxNodes];
   const int32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int32_t lg = lane >> 4, c = lane & 15;
-  const WeighItem it = weigh_item<WF_KB, WF_QB>(plan, g);
+  const WeighItem it = weigh_item<WF_KB, WF_QB>(plan, g, blockIdx.x, gridDim.x);
   if (wave == 0) list_readers(it.readers, lane, nodes);
   const int32_t key0 = it.key0 + 16 * wave;
   const WeighKey k = weigh_key(plan, g, it, key0 + c);
@@ -438,9 +480,16 @@ static const WeighLaunches* weigh_launches(const sc_plan* p, const sc_cache* c) 
   return out.get();
 }
 
-// Adds the weights to the whole array `weights`; part: the launches' part_bytes.
+// Whether the weighing merges the attention's partials on its way (weigh_merge_kernel).
+static bool weigh_merges(const sc_plan* p, const sc_cache* c) {
+  const WeighLaunches* all = weigh_launches(p, c);
+  return all->plans.size() == 1 && all->forms[0].splits == 1 && all->forms[0].len <= 2 && attention_leaves_partials(p, c);
+}
+
+// Adds the weights to the whole array `weights`; part: the launches' part_bytes.  left:
+// the partials to merge into o, or NULL.
 static int launch_weigh(const sc_plan* p, const sc_cache* c, int32_t layer, const void* q, const float* lse, float scale,
-                 float* weights, float* part, hipStream_t stream) {
+                        float* weights, float* part, void* o, const ShareMerge* left, hipStream_t stream) {
   const sc_cache_desc& d = c->d;
   WeighGeom g;
   std::memset(&g, 0, sizeof g);
@@ -475,7 +524,16 @@ static int launch_weigh(const sc_plan* p, const sc_cache* c, int32_t layer, cons
         hipLaunchKernelGGL((weigh_f32_kernel<128>), grid, dim3(64 * WF_NW), 0, stream, qf, g, plan);
     } else {
       const uint16_t* qb = static_cast<const uint16_t*>(q);
-      if (f.kw == 4)
+      uint16_t* ob = static_cast<uint16_t*>(o);
+      const int32_t merges = left ? (g.rows + 7) / 8 * d.n_heads : 0;
+      const dim3 both(grid.x + (uint32_t)merges);
+      if (left && f.kw == 4)
+        hipLaunchKernelGGL((weigh_merge_kernel<4>), both, dim3(64 * WG_NW), 0, stream, qb, ob, g, plan, *left, merges);
+      else if (left && f.kw == 2)
+        hipLaunchKernelGGL((weigh_merge_kernel<2>), both, dim3(64 * WG_NW), 0, stream, qb, ob, g, plan, *left, merges);
+      else if (left)
+        hipLaunchKernelGGL((weigh_merge_kernel<1>), both, dim3(64 * WG_NW), 0, stream, qb, ob, g, plan, *left, merges);
+      else if (f.kw == 4)
         hipLaunchKernelGGL((weigh_bf16_kernel<4>), grid, dim3(64 * WG_NW), 0, stream, qb, g, plan);
       else if (f.kw == 2)
         hipLaunchKernelGGL((weigh_bf16_kernel<2>), grid, dim3(64 * WG_NW), 0, stream, qb, g, plan);
@@ -508,9 +566,16 @@ size_t weigh_attention_bytes(const sc_plan* p, const sc_cache* c) {
 int launch_attention_weigh(const sc_plan* p, const sc_cache* c, int32_t layer, const void* q, void* o, float scale,
                            float* weights, void* ws, hipStream_t stream) {
   const size_t part = partial_bytes(p, c);
+  if (weigh_merges(p, c)) {
+    ShareMerge left;
+    std::memset(static_cast<void*>(&left), 0, sizeof left);
+    const int rc = launch_attention_partials(p, c, layer, q, scale, ws, &left, stream);
+    return rc != SC_OK ? rc : launch_weigh(p, c, layer, q, nullptr, scale, weights, nullptr, o, &left, stream);
+  }
   float* lse = reinterpret_cast<float*>(static_cast<char*>(ws) + part);
   const int rc = launch_attention_lse(p, c, layer, q, o, lse, scale, ws, part, stream);
-  return rc != SC_OK ? rc : launch_weigh(p, c, layer, q, lse, scale, weights, static_cast<float*>(ws), stream);
+  return rc != SC_OK ? rc
+                     : launch_weigh(p, c, layer, q, lse, scale, weights, static_cast<float*>(ws), nullptr, nullptr, stream);
 }
 
 int launch_weights_clear(const sc_cache* c, const int32_t* slots, int32_t n, float* weights, hipStream_t stream) {

@@ -227,3 +227,29 @@ def test_weigh_workspace_is_checked():
     sc.sc_attention_weigh(plan, case.cache, 0, q, o, 0.1, w, ws, nb)
     torch.cuda.synchronize()
     assert (ws[nb:] == 0x5A).all()
+
+
+@pytest.mark.parametrize("heads,tpp,prefix,nodes,nq", [
+    (12, 64, 20, 1, 64), (12, 128, 10, 1, 128), (12, 40, 6, 1, 40), (12, 64, 8, 8, 1), (12, 64, 24, 4, 16),
+    (24, 64, 16, 2, 33), (12, 72, 5, 64, 1), (7, 264, 3, 3, 20),
+])
+def test_weigh_few_rows(heads, tpp, prefix, nodes, nq):
+    """Few rows over a prefix and pages of their own, where the weighing merges the
+    attention's partials itself, or the attention does."""
+    states = [(c, 0) for c in range(prefix + nodes)]
+    case = MemCache("bf16", heads, 128, tpp, 1, states, seed=83)
+    own = states[prefix:]
+    plan = sc.sc_plan_share(sc.sc_plan_condition(case.cache, own, nq), states[:prefix])
+    _check(case, plan, [states[:prefix] + [s] for s in own], nq)
+
+
+def test_weigh_merges_few_partials():
+    """One frame of 64 tokens over its window leaves few partials: no launch merges them."""
+    case = MemCache("bf16", 12, 128, 64, 1, [(c, 0) for c in range(21)], seed=84)
+    plan, reads = _pack("clean", 4, 20, [(20, 0)], case)
+    sc.sc_timer_enable(True)
+    try:
+        _check(case, plan, reads, 64)
+        assert sc.sc_timer_read("attention_weigh")[0] == 2 and sc.sc_timer_read("attention_combine")[0] == 0
+    finally:
+        sc.sc_timer_enable(False)
