@@ -27,7 +27,7 @@ extern "C" {
  * "cross_attention", "gemm_cross_q", "gemm_cross_out", "gemm_condition"
  * (the projections of sc_condition_append), "row_scale" (no launch of its
  * own any more: always 0), "attention_weigh" (the keys' weights, after the
- * attention, and in small calls the merge of its partials), "condense" (both launches
+ * attention, and in small calls the merge of its partials), "condense" (the launches
  * of a fold).  A projection's time includes the launch that adds
  * the parts of a split contraction.  Enabling clears earlier records.  Events
  * are created lazily and reused; the cost is two event records per launch. */

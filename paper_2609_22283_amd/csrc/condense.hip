@@ -2,7 +2,7 @@
 // with the largest weights (of equal ones the first), in their order, gathered into
 // the new state's pages.
 //
-// Two launches.  condense_select_kernel finds each head's tokens: the n-th largest
+// Two launches, or one for few tokens.  condense_select_kernel finds each head's tokens: the n-th largest
 // weight by radix selection over the weights' bits (11 + 11 + 10), then one pass
 // that gives every kept token its place.  One work-group per layer and head: a
 // selection is a chain of counts over all of a head's tokens, which stay in
@@ -17,6 +17,7 @@
 // tokens in three, fp32: 21 against 39), with no rule on sizes that told them apart.
 #include <algorithm>
 #include <cstring>
+#include <type_traits>
 
 #include "device.h"
 #include "internal.h"
@@ -74,14 +75,16 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* sums, int32
 // T threads hold R tokens each, in order (R a multiple of 8: eight tokens lie in
 // one page); R 0: any number of tokens, read again in each pass.  C copies of a
 // counter: fewer lanes of a wave meet in one.
+// kept: where the numbers go (LDS or memory).
 template <int T, int R, int C>
-__global__ __launch_bounds__(T) void condense_select_kernel(CondenseGeom g, CondenseSlots slots) {
+__device__ __forceinline__ void select_tokens(const CondenseGeom& g, const CondenseSlots& slots, int32_t head, int32_t layer,
+                                              int32_t* kept) {
   constexpr int BPT = CS_BINS / T;    // bins of a thread, counted together by it:
   constexpr int ROW = BPT * C + 4;    // their counters, and a gap that spreads the threads over the banks
   __shared__ __attribute__((aligned(16))) uint32_t hist[T * ROW];
   __shared__ uint32_t sums[5][T / 64];
   __shared__ uint32_t found[3][2];
-  const int32_t tid = threadIdx.x, head = blockIdx.x, layer = blockIdx.y, N = g.n_src * g.tpp;
+  const int32_t tid = threadIdx.x, N = g.n_src * g.tpp;
   const float* w = g.weights + ((size_t)layer * g.n_slots * g.n_heads + head) * g.tpp;
   const int32_t per = R ? R : ((N + T - 1) / T + 7) / 8 * 8, i0 = tid * per;
   constexpr int RR = R ? R : 8;
@@ -164,7 +167,6 @@ __global__ __launch_bounds__(T) void condense_select_kernel(CondenseGeom g, Cond
   const uint32_t own_above = above, own_equal = equal;
   above = block_scan<T>(above, sums[3], tid) - own_above;
   equal = block_scan<T>(equal, sums[4], tid) - own_equal;
-  int32_t* kept = g.kept + ((size_t)layer * g.n_heads + head) * g.n;
   each([&](uint32_t k, int32_t i) __attribute__((always_inline)) {
     if (k > prefix || (k == prefix && equal < want)) kept[above + min(equal, want)] = i;
     above += k > prefix;
@@ -172,62 +174,112 @@ __global__ __launch_bounds__(T) void condense_select_kernel(CondenseGeom g, Cond
   });
 }
 
-// E: the elements' type (uint16_t or uint32_t), HD the head dim.
-constexpr int CG_T = 256, CG_D = 4;  // CG_D: V^T rows of a thread
+template <int T, int R, int C>
+__global__ __launch_bounds__(T) void condense_select_kernel(CondenseGeom g, CondenseSlots slots) {
+  const int32_t head = blockIdx.x, layer = blockIdx.y;
+  select_tokens<T, R, C>(g, slots, head, layer, g.kept + ((size_t)layer * g.n_heads + head) * g.n);
+}
+
+// The gather's units of a head and layer, E the elements' type (uint16_t or uint32_t), HD
+// the head dim: 16 bytes of a K row (its first unit the weight too), and CG_D rows of
+// eight V^T columns.
+constexpr int CG_T = 256, CG_D = 4;
 template <class E, int HD>
-__global__ __launch_bounds__(CG_T) void condense_gather_kernel(CondenseGeom g, CondenseSlots slots, int32_t k_blocks) {
-  const int32_t head = blockIdx.y % g.n_heads, layer = blockIdx.y / g.n_heads;
-  const int32_t* kept = g.kept + (size_t)blockIdx.y * g.n;
-  char* pool = g.pool + (size_t)layer * g.n_slots * g.slot_bytes;
-  const size_t head_off = (size_t)head * g.tpp * HD * sizeof(E);
-  const auto page_of = [&](int32_t i) { return (int32_t)fast_div((uint32_t)i, g.tpp_div); };
-  if ((int32_t)blockIdx.x < k_blocks) {
-    constexpr int U = HD * sizeof(E) / 16;  // 16-byte units of a K row
-    static_assert(CG_T % U == 0, "a work-group copies whole rows");
-    const int32_t row = (int32_t)blockIdx.x * (CG_T / U) + (int32_t)threadIdx.x / U, u = (int32_t)threadIdx.x % U;
-    if (row >= g.n) return;
+struct Gather {
+  static constexpr int U = HD * sizeof(E) / 16;  // units of a K row
+  const CondenseGeom& g;
+  const CondenseSlots& slots;
+  const int32_t* kept;
+  char* pool;
+  float* w;
+  size_t head_off;
+  __device__ __forceinline__ Gather(const CondenseGeom& g_, const CondenseSlots& s, int32_t head, int32_t layer,
+                                    const int32_t* k)
+      : g(g_), slots(s), kept(k), pool(g_.pool + (size_t)layer * g_.n_slots * g_.slot_bytes),
+        w(g_.weights + ((size_t)layer * g_.n_slots * g_.n_heads + head) * g_.tpp),
+        head_off((size_t)head * g_.tpp * HD * sizeof(E)) {}
+  __device__ __forceinline__ int32_t page_of(int32_t i) const { return (int32_t)fast_div((uint32_t)i, g.tpp_div); }
+  __device__ __forceinline__ void k_unit(int32_t row, int32_t u) const {
     const int32_t from = kept[row], p = page_of(from), t = from - p * g.tpp, f = page_of(row), to = row - f * g.tpp;
     const int32_t src = slots.slot[p], dst = slots.slot[g.n_src + f];
     *reinterpret_cast<u32x4u*>(pool + (size_t)dst * g.slot_bytes + head_off + (size_t)to * HD * sizeof(E) + 16 * u) =
         *reinterpret_cast<const u32x4u*>(pool + (size_t)src * g.slot_bytes + head_off + (size_t)t * HD * sizeof(E) + 16 * u);
     if (u == 0) {
-      float* w = g.weights + ((size_t)layer * g.n_slots * g.n_heads + head) * g.tpp;
       const size_t stride = (size_t)g.n_heads * g.tpp;
       w[dst * stride + to] = w[src * stride + t];
     }
+  }
+  __device__ __forceinline__ void v_unit(int32_t run, int32_t d0) const {
+    const char* src[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int32_t from = kept[8 * run + e], p = page_of(from);
+      src[e] = pool + (size_t)slots.slot[p] * g.slot_bytes + g.kv_half + head_off +
+               ((size_t)d0 * g.tpp + (from - p * g.tpp)) * sizeof(E);
+    }
+    const int32_t f = page_of(8 * run), to = 8 * run - f * g.tpp;
+    char* dst = pool + (size_t)slots.slot[g.n_src + f] * g.slot_bytes + g.kv_half + head_off +
+                ((size_t)d0 * g.tpp + to) * sizeof(E);
+    E v[CG_D][8];
+#pragma unroll
+    for (int d = 0; d < CG_D; ++d)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[d][e] = *reinterpret_cast<const E*>(src[e] + (size_t)d * g.tpp * sizeof(E));
+#pragma unroll
+    for (int d = 0; d < CG_D; ++d) {
+      u32x4u* out = reinterpret_cast<u32x4u*>(dst + (size_t)d * g.tpp * sizeof(E));
+      if constexpr (sizeof(E) == 2) {
+        u32x4 x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = (uint32_t)v[d][2 * e] | (uint32_t)v[d][2 * e + 1] << 16;
+        *out = x;
+      } else {
+        out[0] = u32x4{v[d][0], v[d][1], v[d][2], v[d][3]};
+        out[1] = u32x4{v[d][4], v[d][5], v[d][6], v[d][7]};
+      }
+    }
+  }
+};
+
+// A work-group's share of a head's gather: the first k_blocks work-groups have the K
+// units, the others the V^T ones.
+template <class E, int HD>
+__device__ __forceinline__ void gather_block(const Gather<E, HD>& gt, int32_t block, int32_t k_blocks) {
+  constexpr int U = Gather<E, HD>::U;
+  static_assert(CG_T % U == 0, "a work-group copies whole rows");
+  const CondenseGeom& g = gt.g;
+  if (block < k_blocks) {
+    const int32_t row = block * (CG_T / U) + (int32_t)threadIdx.x / U;
+    if (row < g.n) gt.k_unit(row, (int32_t)threadIdx.x % U);
     return;
   }
   const int32_t runs = g.n / 8;
-  const int32_t i = ((int32_t)blockIdx.x - k_blocks) * CG_T + (int32_t)threadIdx.x, run = i % runs, d0 = i / runs * CG_D;
-  if (d0 >= HD) return;
-  const char* src[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int32_t from = kept[8 * run + e], p = page_of(from);
-    src[e] = pool + (size_t)slots.slot[p] * g.slot_bytes + g.kv_half + head_off +
-             ((size_t)d0 * g.tpp + (from - p * g.tpp)) * sizeof(E);
-  }
-  const int32_t f = page_of(8 * run), to = 8 * run - f * g.tpp;
-  char* dst = pool + (size_t)slots.slot[g.n_src + f] * g.slot_bytes + g.kv_half + head_off +
-              ((size_t)d0 * g.tpp + to) * sizeof(E);
-  E v[CG_D][8];
-#pragma unroll
-  for (int d = 0; d < CG_D; ++d)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[d][e] = *reinterpret_cast<const E*>(src[e] + (size_t)d * g.tpp * sizeof(E));
-#pragma unroll
-  for (int d = 0; d < CG_D; ++d) {
-    u32x4u* out = reinterpret_cast<u32x4u*>(dst + (size_t)d * g.tpp * sizeof(E));
-    if constexpr (sizeof(E) == 2) {
-      u32x4 x;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = (uint32_t)v[d][2 * e] | (uint32_t)v[d][2 * e + 1] << 16;
-      *out = x;
-    } else {
-      out[0] = u32x4{v[d][0], v[d][1], v[d][2], v[d][3]};
-      out[1] = u32x4{v[d][4], v[d][5], v[d][6], v[d][7]};
-    }
-  }
+  const int32_t i = (block - k_blocks) * CG_T + (int32_t)threadIdx.x, d0 = i / runs * CG_D;
+  if (d0 < HD) gt.v_unit(i % runs, d0);
+}
+
+template <class E, int HD>
+__global__ __launch_bounds__(CG_T) void condense_gather_kernel(CondenseGeom g, CondenseSlots slots, int32_t k_blocks) {
+  gather_block(Gather<E, HD>(g, slots, (int32_t)blockIdx.y % g.n_heads, (int32_t)blockIdx.y / g.n_heads,
+                             g.kept + (size_t)blockIdx.y * g.n),
+               (int32_t)blockIdx.x, k_blocks);
+}
+
+// Both in one launch, for few tokens: every work-group of the gather selects for itself,
+// which costs nothing where all of them are resident at once (seven to a CU, 20 KB of
+// LDS each).  12 heads, apart against so: four states of 64 tokens in 12 layers 14.8 us
+// against 11.9, 21 in 29 layers (1740 work-groups) 37.9 against 36.2; fp32, two of 312
+// in three layers 15.2 against 13.2, two of 64 in 20 (2160) 16.1 against 19.3.
+constexpr int CS_FEW = 256 * 8;
+template <class E, int HD>
+__global__ __launch_bounds__(CG_T) void condense_few_kernel(CondenseGeom g, CondenseSlots slots, int32_t k_blocks) {
+  __shared__ int32_t kept[CS_FEW];
+  const int32_t head = (int32_t)blockIdx.y % g.n_heads, layer = (int32_t)blockIdx.y / g.n_heads;
+  select_tokens<CG_T, CS_FEW / CG_T, 1>(g, slots, head, layer, kept);
+  __syncthreads();
+  if (blockIdx.x == 0)
+    for (int32_t i = threadIdx.x; i < g.n; i += CG_T) g.kept[(size_t)blockIdx.y * g.n + i] = kept[i];
+  gather_block(Gather<E, HD>(g, slots, head, layer, kept), (int32_t)blockIdx.x, k_blocks);
 }
 
 int condense_check(const sc_cache* c, int32_t n_sources) {
@@ -267,6 +319,24 @@ int launch_condense(const sc_cache* c, int32_t layer, int32_t n_layers, const in
     g.kept = kept + (size_t)l * d.n_heads * g.n;
     const dim3 heads((uint32_t)d.n_heads, (uint32_t)m), grid((uint32_t)(k_blocks + v_blocks), (uint32_t)(m * d.n_heads));
     timer_begin(TK_CONDENSE, stream);
+    const auto by_type = [&](auto launch) {
+      if (d.dtype == SC_DTYPE_F32 && d.head_dim == 64)
+        launch(uint32_t{}, std::integral_constant<int, 64>{});
+      else if (d.dtype == SC_DTYPE_F32)
+        launch(uint32_t{}, std::integral_constant<int, 128>{});
+      else if (d.head_dim == 64)
+        launch(uint16_t{}, std::integral_constant<int, 64>{});
+      else
+        launch(uint16_t{}, std::integral_constant<int, 128>{});
+    };
+    if (N <= CS_FEW && (int64_t)grid.x * grid.y <= 7 * kCUs) {
+      by_type([&](auto e, auto hd) {
+        hipLaunchKernelGGL((condense_few_kernel<decltype(e), decltype(hd)::value>), grid, dim3(CG_T), 0, stream, g, s, k_blocks);
+      });
+      timer_end(TK_CONDENSE, stream);
+      SC_HIP(hipGetLastError());
+      continue;
+    }
     // few tokens: fewer waves meet at each barrier
     if (N <= 256 * 8)
       hipLaunchKernelGGL((condense_select_kernel<256, 8, 1>), heads, dim3(256), 0, stream, g, s);
@@ -278,14 +348,9 @@ int launch_condense(const sc_cache* c, int32_t layer, int32_t n_layers, const in
       hipLaunchKernelGGL((condense_select_kernel<1024, 40, 4>), heads, dim3(1024), 0, stream, g, s);
     else
       hipLaunchKernelGGL((condense_select_kernel<1024, 0, 4>), heads, dim3(1024), 0, stream, g, s);
-    if (d.dtype == SC_DTYPE_F32 && d.head_dim == 64)
-      hipLaunchKernelGGL((condense_gather_kernel<uint32_t, 64>), grid, dim3(CG_T), 0, stream, g, s, k_blocks);
-    else if (d.dtype == SC_DTYPE_F32)
-      hipLaunchKernelGGL((condense_gather_kernel<uint32_t, 128>), grid, dim3(CG_T), 0, stream, g, s, k_blocks);
-    else if (d.head_dim == 64)
-      hipLaunchKernelGGL((condense_gather_kernel<uint16_t, 64>), grid, dim3(CG_T), 0, stream, g, s, k_blocks);
-    else
-      hipLaunchKernelGGL((condense_gather_kernel<uint16_t, 128>), grid, dim3(CG_T), 0, stream, g, s, k_blocks);
+    by_type([&](auto e, auto hd) {
+      hipLaunchKernelGGL((condense_gather_kernel<decltype(e), decltype(hd)::value>), grid, dim3(CG_T), 0, stream, g, s, k_blocks);
+    });
     timer_end(TK_CONDENSE, stream);
     SC_HIP(hipGetLastError());
   }

@@ -57,6 +57,7 @@ CASES = [  # dtype, heads, head dim, tokens per page, pages per state, sources, 
     ("bf16", 2, 128, 8, 1, 2, 1),
     ("bf16", 3, 128, 72, 2, 1, 2),        # one source: a copy
     ("bf16", 12, 128, 64, 1, 21, 3),
+    ("bf16", 12, 128, 64, 1, 3, 30),      # few tokens, more work-groups than run at once
     ("bf16", 2, 64, 104, 3, 5, 1),
     ("f32", 2, 64, 104, 3, 2, 1),
     ("f32", 1, 128, 40, 1, 7, 2),
