@@ -266,7 +266,7 @@ static LseGeom attn_geom(const sc_plan* p, const sc_cache* c, int32_t layer, flo
   g.tpp_div = magic_div((uint32_t)d.tokens_per_page);
   g.scale = scale;
   g.scale_log2 = scale * 1.4426950408889634f;
-  g.unit = d.dtype == SC_DTYPE_F32 ? 1.f : std::fabs(scale) * 1.4426950408889634f;
+  g.unit = d.dtype == SC_DTYPE_F32 ? 1.f : logit_unit(scale);
   g.q_flip = std::signbit(scale) ? 0x80008000u : 0u;
   g.rows = g.n_nodes * p->nq;
   g.nq_div = magic_div((uint32_t)p->nq);

@@ -2,6 +2,9 @@
 // launches, and the pieces of them that other kernels over the same pages use.
 #pragma once
 
+#include <algorithm>
+#include <cfloat>
+#include <cmath>
 #include <type_traits>
 
 #include "device.h"
@@ -44,7 +47,7 @@ struct AttnGeom {
 // What the forms that give the rows' logarithmic sums (LseAttn, ShareAttn) need beside.
 struct LseGeom : AttnGeom {
   float* lse;             // [head][row] log2 of the row's sum, or null
-  float unit;             // |scale| log2(e); fp32 caches: 1
+  float unit;             // logit_unit(scale); fp32 caches: 1
   uint32_t q_flip;        // bf16: sign bits of a negative scale
   int32_t rows;           // rows of the pack, n_nodes * nq
   // ShareAttn: query tiles of the prefix; pieces and tiles per piece of the prefix, and
@@ -76,6 +79,10 @@ struct ShareAttn {
   using Geom = LseGeom;
   static constexpr bool kLse = true, kShare = true;
 };
+// |scale| log2(e) as the factor of the bf16 forms' logits.  Not below the smallest normal
+// number: a scale of zero would turn the -inf of a key past the end into NaN, and
+// products of q and k below 2^100 times 2^-126 have an exponential of 1 in every bit.
+inline float logit_unit(float scale) { return std::max(std::fabs(scale) * 1.4426950408889634f, FLT_MIN); }
 template <class M>
 __device__ __forceinline__ float unit_of(const typename M::Geom& g) {
   if constexpr (M::kLse) return g.unit;

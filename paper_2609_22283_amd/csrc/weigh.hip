@@ -39,7 +39,7 @@ struct WeighGeom {
   const float* lse;  // [head][row]
   int32_t n_heads, tpp, nq, rows, items, len, keys;  // items of a head, row tiles of one at most, keys of the launch
   DivMagic tpp_div, nq_div;
-  float unit;       // bf16: |scale| log2(e)
+  float unit;       // bf16: logit_unit(scale)
   float scale;      // fp32: scale log2(e)
   uint32_t q_flip;  // bf16: sign bits of a negative scale
 };
@@ -504,7 +504,7 @@ static int launch_weigh(const sc_plan* p, const sc_cache* c, int32_t layer, cons
   g.rows = (int32_t)p->nodes.size() * p->nq;
   g.tpp_div = magic_div((uint32_t)g.tpp);
   g.nq_div = magic_div((uint32_t)g.nq);
-  g.unit = std::fabs(scale) * 1.4426950408889634f;
+  g.unit = logit_unit(scale);
   g.scale = scale * 1.4426950408889634f;
   g.q_flip = std::signbit(scale) ? 0x80008000u : 0u;
   const WeighLaunches* all = weigh_launches(p, c);
