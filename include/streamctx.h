@@ -405,10 +405,11 @@ int sc_cache_weights_clear(const sc_cache* cache, sc_node state, float* weights,
  * follows from the same (sc_attention rounds a bf16 q times the scale): both
  * calls agree within bf16 rounding, not in bits.  Limits, arguments and errors
  * as sc_attention (layer, plan and workspace among them), and SC_EINVAL for
- * a scale that is not finite, a null array or a q off 16-byte boundaries.  ws:
- * 16-byte aligned, of sc_attention_weigh_workspace_bytes(plan, cache) bytes (0
- * for a plan that the call refuses).  Its contents are undefined on return; calls
- * sharing one workspace must be ordered on one stream. */
+ * a scale that is not finite, a null array, a q off 16-byte boundaries or an o
+ * that overlaps q (q is read again after o is written).  ws: 16-byte aligned, of
+ * sc_attention_weigh_workspace_bytes(plan, cache) bytes (0 for a plan that the call
+ * refuses).  Its contents are undefined on return; calls sharing one workspace must
+ * be ordered on one stream. */
 size_t sc_attention_weigh_workspace_bytes(const sc_plan* plan, const sc_cache* cache);
 int sc_attention_weigh(const sc_plan* plan, const sc_cache* cache, int32_t layer, const void* q,
                        void* o, float scale, float* weights, void* ws, size_t ws_bytes,

@@ -119,6 +119,10 @@ extern "C" int sc_attention_weigh(const sc_plan* p, const sc_cache* c, int32_t l
     int rc = plan_check(p, c, layer);
     if (rc != SC_OK || (rc = weigh_check(p, c, weights, ws, ws_bytes)) != SC_OK) return rc;
     if (p->nodes.empty()) return SC_OK;
+    // the keys are weighed by q after (or while) o is written
+    const uint64_t n = (uint64_t)p->nodes.size() * p->nq * c->d.n_heads * c->d.head_dim * dtype_size(c->d.dtype);
+    const uint64_t qa = reinterpret_cast<uintptr_t>(q), oa = reinterpret_cast<uintptr_t>(o);
+    if (qa < oa + n && oa < qa + n) return fail(SC_EINVAL, "o overlaps q, which is read after o is written");
     return launch_attention_weigh(p, c, layer, q, o, scale, weights, ws, static_cast<hipStream_t>(stream));
   });
 }
