@@ -63,7 +63,7 @@ class StackPipeline:
             d = cache.desc
             self.weights = torch.zeros((d.n_layers, d.n_slots, d.n_heads, d.tokens_per_page),
                                        dtype=torch.float32, device=xs.device)
-            self.kept = torch.empty((d.n_layers, d.n_heads, self.n_tok), dtype=torch.int32, device=xs.device)
+            self.kept = torch.empty((len(self.layers), d.n_heads, self.n_tok), dtype=torch.int32, device=xs.device)
             self.weigh_ws = [torch.empty(0, dtype=torch.uint8, device=xs.device)]
             self.cached = set()  # states of the nodes run so far that are still cached
 
@@ -150,7 +150,8 @@ class StackPipeline:
             self.memory = (old + leaving)[0]  # it fits whole
         elif leaving:
             into = (leaving[-1][0], self.K + 1)  # a level that no node has
-            self.cache.condense(0, self.cache.desc.n_layers, old + leaving, into, self.weights, self.kept,
+            # the stack's layers: a cache may hold more, which nothing writes
+            self.cache.condense(0, len(self.layers), old + leaving, into, self.weights, self.kept,
                                 self.stream)
             for st in old + leaving:
                 self.cache.release(st)

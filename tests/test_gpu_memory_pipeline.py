@@ -1,0 +1,38 @@
+"""The pipeline with a memory on the GPU: caches of more layers than the stack, streams,
+and a condition beside the memory."""
+import pytest
+
+import paper_2609_22283_amd as sc
+from paper_2609_22283_amd.pipeline import StackPipeline
+from synth.configs import SMALL
+
+from gpu_cases import from_device, torch_mod
+from test_gpu_pipeline import T_SCHED, _setup, _stack_gate
+
+pytestmark = pytest.mark.gpu
+
+
+def _pipe(make, cache=None, **kw):
+    p = make()
+    return StackPipeline(layers=p.layers, cache=cache or p.cache, rope=p.rope, xs=p.xs, noise=p.noise, policy=p.policy,
+                         K=p.K, W=kw.pop("W", p.W), B=p.B, t_sched=T_SCHED, refresh=True, **kw)
+
+
+def test_cache_of_more_layers_than_the_stack():
+    """Six chunks over a window of two, folded again and again: the same bits whether the cache
+    holds the stack's two layers or a third, which stays as it was."""
+    torch = torch_mod()
+    make, _, _, keep = _setup(SMALL, 2, 6, 2, "prog", seed=31, n_slots=90)
+    runs = []
+    for layers in (2, 3):
+        args = (layers, SMALL.heads, SMALL.head_dim, SMALL.tokens_per_page, SMALL.frames_per_chunk, 90)
+        pool = torch.full((sc.sc_cache_pool_bytes(*args),), 0xFF, dtype=torch.uint8, device="cuda")
+        p = _pipe(make, sc.sc_cache_create(pool, *args), memory=True)
+        p.run("packed")
+        torch.cuda.synchronize()
+        assert p.cache.free_slot_count() == 90 and p.memory is None
+        assert bool((pool.view(layers, -1)[2:] == 0xFF).all())
+        assert bool((p.weights[2:] == 0).all())
+        runs.append((p.xs.clone(), p.weights[:2].clone()))
+    assert torch.isfinite(runs[0][0].float()).all()
+    assert torch.equal(runs[0][0], runs[1][0]) and torch.equal(runs[0][1], runs[1][1])

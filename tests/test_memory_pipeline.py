@@ -1,0 +1,36 @@
+"""The pipeline with a memory on the CPU: what it folds, and what it does when a fold
+fails or is refused (no kernel runs: device pointers here are never read)."""
+import pytest
+import torch
+
+import paper_2609_22283_amd as sc
+from paper_2609_22283_amd.pipeline import StackPipeline
+
+PTR = 1 << 20  # stands for device memory, 16-byte aligned
+HEADS, TPP, PPC, D, MLP = 2, 40, 1, 256, 512
+
+
+def _pipe(layers=2, cache_layers=2, B=8, **kw):
+    cache = sc.sc_cache_create(PTR, cache_layers, HEADS, 128, TPP, PPC, 40)
+    ws = [sc.BlockWeights(D, HEADS, 128, MLP, PTR, PTR, PTR, PTR) for _ in range(layers)]
+    xs = torch.zeros((B, TPP * PPC, D), dtype=torch.bfloat16)
+    return StackPipeline(layers=ws, cache=cache, rope=None, xs=xs, noise=xs, policy="clean", K=4, W=2, B=B,
+                         t_sched=(0.0, 0.25, 0.5, 0.75, 1.0), memory=True, **kw)
+
+
+def _cached(p, states):
+    """States that the pipeline has run, with slots (unwritten)."""
+    sc.sc_plan_build(sc.sc_selection_build("clean", 4, 0, states), p.cache)
+    p.cached = set(states)
+
+
+def test_folds_the_stack_layers():
+    """A cache may hold more layers than the stack: the fold takes those of the stack."""
+    p = _pipe(layers=2, cache_layers=3)
+    _cached(p, [(0, 0), (1, 0), (2, 0)])
+    seen = []
+    p.cache.condense = lambda layer, n_layers, *a: seen.append((layer, n_layers))
+    p._fold_unread([(4, 4)])
+    assert seen == [(0, 2)]
+    assert tuple(p.kept.shape) == (2, HEADS, TPP * PPC)
+    assert tuple(p.weights.shape) == (3, 40, HEADS, TPP)
