@@ -136,26 +136,27 @@ class StackPipeline:
         off, chunk, level, _ = sc.sc_selection_build(self.policy, self.K, self.W, future).tables()
         needed = {(chunk[s], level[s]) for i in range(len(future)) for s in range(off[i], off[i + 1] - 1)}
         unread = sorted(self.cached - needed)
-        self.cached -= set(unread)
         leaving = [st for st in unread if st[1] == 0] if future else []
-        for st in unread:
-            if st not in leaving:
-                self.cache.release(st)
+        self._release([st for st in unread if st not in leaving])
         old = [] if self.memory is None else [self.memory]
         if not future:
-            for st in old:
-                self.cache.release(st)
+            self._release(old)
             self.memory = None
         elif len(old + leaving) == 1:
             self.memory = (old + leaving)[0]  # it fits whole
+            self.cached -= set(leaving)
         elif leaving:
             into = (leaving[-1][0], self.K + 1)  # a level that no node has
             # the stack's layers: a cache may hold more, which nothing writes
             self.cache.condense(0, len(self.layers), old + leaving, into, self.weights, self.kept,
                                 self.stream)
-            for st in old + leaving:
-                self.cache.release(st)
+            self._release(old + leaving)  # only now: a fold that fails can be tried again
             self.memory = into
+
+    def _release(self, states: Sequence[Tuple[int, int]]) -> None:
+        for st in states:
+            self.cache.release(st)
+            self.cached.discard(st)
 
     def run(self, mode: str = "packed", time_rounds: bool = False,
             kernel_timer_rounds: Tuple[int, int] = None, layer_hooks=None,

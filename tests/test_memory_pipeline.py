@@ -34,3 +34,24 @@ def test_folds_the_stack_layers():
     assert seen == [(0, 2)]
     assert tuple(p.kept.shape) == (2, HEADS, TPP * PPC)
     assert tuple(p.weights.shape) == (3, 40, HEADS, TPP)
+
+
+def test_a_failed_fold_keeps_its_states():
+    """A fold that fails leaves the memory and the states that were to join it as they are:
+    cached, known to the pipeline, and folded by the next attempt."""
+    p = _pipe()
+    _cached(p, [(0, 0), (1, 0), (1, 3), (2, 0)])
+    p.memory = (0, 0)
+    p.cached.discard((0, 0))
+    for _ in range(2):
+        with pytest.raises(sc.ScError) as e:  # nothing is written yet
+            p._fold_unread([(4, 4)])
+        assert e.value.code == sc.SC_EUNAVAILABLE
+        assert p.memory == (0, 0) and p.cached == {(1, 0), (2, 0)}
+        assert all(p.cache.contains(st) for st in [(0, 0), (1, 0), (2, 0)]) and not p.cache.contains((1, 3))
+    folds = []
+    p.cache.condense = lambda layer, n, sources, into, *a: folds.append((sources, into))
+    p._fold_unread([(4, 4)])
+    assert folds == [([(0, 0), (1, 0)], (1, 5))]
+    assert p.memory == (1, 5) and p.cached == {(2, 0)}
+    assert not p.cache.contains((0, 0)) and not p.cache.contains((1, 0))
