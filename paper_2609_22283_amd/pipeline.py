@@ -40,8 +40,9 @@ class StackPipeline:
                  refresh: bool = True, stream=None, condition=None, memory: bool = False):
         """``memory``: keep one memory state of what leaves the window, of as
         many tokens as a chunk.  The cache needs room for two states more; the
-        modes are the same, layer hooks are refused, and states cached before
-        the run are left where they are.  ``condition``: optional dict with
+        modes are the same, ``refresh`` is needed (the clean states that it
+        leaves are what the memory is made of), layer hooks are refused, and
+        states cached before the run are left where they are.  ``condition``: optional dict with
         ``cache`` (an sc.Cache holding the condition K/V of every layer),
         ``cross`` (per layer: (w_q, w_o, q_norm or None)) and ``condition_of``
         (chunk -> cached condition state; default (0, 0))."""
@@ -60,6 +61,8 @@ class StackPipeline:
         self.memory = None   # the cached state that holds it, once something has left the window
         self.weights = None  # accumulated attention weight of every cached key
         if memory:
+            if not refresh:
+                raise ValueError("a memory holds clean states, which only the refresh nodes leave: it needs refresh=True")
             d = cache.desc
             self.weights = torch.zeros((d.n_layers, d.n_slots, d.n_heads, d.tokens_per_page),
                                        dtype=torch.float32, device=xs.device)

@@ -55,3 +55,11 @@ def test_a_failed_fold_keeps_its_states():
     assert folds == [([(0, 0), (1, 0)], (1, 5))]
     assert p.memory == (1, 5) and p.cached == {(2, 0)}
     assert not p.cache.contains((0, 0)) and not p.cache.contains((1, 0))
+
+
+def test_memory_needs_the_refresh_node():
+    """Only clean states join the memory, and only the refresh node makes them: without it the
+    history would be lost in silence."""
+    with pytest.raises(ValueError):
+        _pipe(refresh=False)
+    assert _pipe(refresh=True).memory is None
