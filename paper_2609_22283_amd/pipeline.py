@@ -91,6 +91,7 @@ class StackPipeline:
         the same function of the inputs, equal up to the order of fp32 sums
         (a stack takes its layers' first RMSNorm factors from sums that the
         layer before stored)."""
+        self._refuse_hooks(layer_hook)
         n = self.n_tok
         sel = sc.sc_selection_build(self.policy, self.K, self.W, nodes)
         plan = sc.sc_plan_build(sel, self.cache)
@@ -110,8 +111,6 @@ class StackPipeline:
             layers = [w.with_cross(sc.CrossAttn(wq, wo, cond["cache"], plan_c, q_norm=qn))
                       for w, (wq, wo, qn) in zip(self.layers, cond["cross"])]
         if self.weights is not None:
-            if layer_hook is not None:
-                raise ValueError("layer hooks observe single blocks; a stack with a memory runs in one call")
             nb = sc.sc_attention_weigh_workspace_bytes(plan, self.cache)
             if self.weigh_ws[-1].numel() < nb:  # the smaller ones may still be in use
                 self.weigh_ws.append(self.torch.empty(nb, dtype=self.torch.uint8, device=x.device))
@@ -132,6 +131,10 @@ class StackPipeline:
                 sc.sc_sampler_step([(c, j)], self.t_sched, self.K, self.xs[c],
                                    self.stage[i * n:(i + 1) * n], self.noise[c, j],
                                    n * self.hidden, self.stream)
+
+    def _refuse_hooks(self, *hooks) -> None:
+        if self.weights is not None and any(h is not None for h in hooks):
+            raise ValueError("layer hooks observe single blocks; a stack with a memory runs in one call")
 
     def _fold_unread(self, future: Sequence[Tuple[int, int]]) -> None:
         """Release what no node of ``future`` selects, the clean states among it
@@ -172,6 +175,7 @@ class StackPipeline:
         serial mode) to a layer hook of its forwards (see ``forward``);
         ``stop_after`` ends the run after that round."""
         torch = self.torch
+        self._refuse_hooks(*(layer_hooks or {}).values())
         times = []
         self.kernel_times = {}
         if mode == "serial":

@@ -63,3 +63,16 @@ def test_memory_needs_the_refresh_node():
     with pytest.raises(ValueError):
         _pipe(refresh=False)
     assert _pipe(refresh=True).memory is None
+
+
+@pytest.mark.parametrize("mode", ["packed", "sequential", "serial"])
+def test_layer_hooks_are_refused_before_anything_runs(mode):
+    """In whichever round the hook is: no state has slots, no weight is cleared."""
+    p = _pipe()
+    for r in (0, 3, len(p.rounds()) - 1):
+        with pytest.raises(ValueError):
+            p.run(mode, layer_hooks={r: lambda *a: None})
+        assert p.cache.free_slot_count() == 40 and p.cached == set()
+    with pytest.raises(ValueError):
+        p.forward([(0, 4)], lambda *a: None)
+    assert p.cache.free_slot_count() == 40
