@@ -68,6 +68,8 @@ class StackPipeline:
                                        dtype=torch.float32, device=xs.device)
             self.kept = torch.empty((len(self.layers), d.n_heads, self.n_tok), dtype=torch.int32, device=xs.device)
             self.weigh_ws = [torch.empty(0, dtype=torch.uint8, device=xs.device)]
+            if xs.is_cuda:  # a run on another stream must not find the zeros still to come
+                torch.cuda.current_stream(xs.device).synchronize()
             self.cached = set()  # states of the nodes run so far that are still cached
 
     # ----------------------------------------------------------- schedules

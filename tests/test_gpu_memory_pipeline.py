@@ -36,3 +36,27 @@ def test_cache_of_more_layers_than_the_stack():
         runs.append((p.xs.clone(), p.weights[:2].clone()))
     assert torch.isfinite(runs[0][0].float()).all()
     assert torch.equal(runs[0][0], runs[1][0]) and torch.equal(runs[0][1], runs[1][1])
+
+
+def test_made_on_a_busy_stream_run_on_another():
+    """A pipeline made behind long work of one stream and run on another: its weights start from
+    zeros that have landed, and the run has the bits of one on a single stream."""
+    torch = torch_mod()
+    make, _, _, keep = _setup(SMALL, 2, 6, 2, "prog", seed=32, n_slots=90)
+    base = make()
+    p = _pipe(make, memory=True)
+    p.run("packed")
+    torch.cuda.synchronize()
+    want, weights = p.xs.clone(), p.weights.clone()
+    side = torch.cuda.Stream()
+    a = torch.randn((4096, 4096), device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(20):  # some tens of ms
+        a = (a @ a) * 1e-2
+    q = StackPipeline(layers=base.layers, cache=base.cache, rope=base.rope, xs=base.xs, noise=base.noise,
+                      policy=base.policy, K=base.K, W=base.W, B=base.B, t_sched=T_SCHED, refresh=True, memory=True)
+    assert torch.cuda.current_stream().query()  # the zeros have landed
+    with torch.cuda.stream(side):
+        q.run("packed")
+    torch.cuda.synchronize()
+    assert torch.equal(q.xs, want) and torch.equal(q.weights, weights)
