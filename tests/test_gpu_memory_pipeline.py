@@ -60,3 +60,30 @@ def test_made_on_a_busy_stream_run_on_another():
         q.run("packed")
     torch.cuda.synchronize()
     assert torch.equal(q.xs, want) and torch.equal(q.weights, weights)
+
+
+def test_memory_beside_a_condition():
+    """The full block form with a memory: serial clean history, a window of two and a memory of
+    one chunk against a window of three, as without a condition; and a packed stream
+    whose conditions change under it, twice with the same bits."""
+    torch = torch_mod()
+    switch = lambda c: 0 if c < 3 else 1  # noqa: E731
+    make, _, _, keep, _ = _setup(SMALL, 2, 4, 2, "clean", seed=33, n_slots=60, full=True, n_cond=2, cond_of=switch)
+    runs = []
+    for kw in (dict(memory=True), dict(W=3)):
+        p = _pipe(make, condition=make().condition, **kw)
+        p.run("serial")
+        torch.cuda.synchronize()
+        assert p.cache.free_slot_count() == 60 and p.memory is None
+        runs.append(from_device(p.xs))
+    for c in range(4):
+        _stack_gate(runs[0][c], runs[1][c], 2, ("memory beside a condition", c), runs=2)
+    make, _, _, keep2, _ = _setup(SMALL, 2, 8, 2, "prog", seed=34, n_slots=120, full=True, n_cond=2, cond_of=switch)
+    runs = []
+    for memory in (True, True, False):
+        p = _pipe(make, condition=make().condition, memory=memory)
+        p.run("packed")
+        torch.cuda.synchronize()
+        runs.append(p.xs.clone())
+    assert torch.isfinite(runs[0].float()).all()
+    assert torch.equal(runs[0], runs[1]) and not torch.equal(runs[0][-1], runs[2][-1])
