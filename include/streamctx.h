@@ -204,8 +204,9 @@ int sc_plan_condition(sc_cache* cache, const sc_node* conditions, int32_t n, int
  * 128 and pages of at least one key tile: 32 tokens when Nq <= 64, 64
  * otherwise (else SC_EUNSUPPORTED).  ws: device scratch, 16-byte aligned, of at least
  * sc_attention_workspace_bytes(plan, cache) bytes (may be NULL when that is
- * 0, as for fp32 caches); the bf16 kernel splits long key ranges across
- * work-groups and merges their partial softmax sums there.  Its contents are
+ * 0, as for fp32 caches unless the nodes share a prefix); the bf16 kernel splits
+ * long key ranges across work-groups and merges their partial softmax sums
+ * there, and so does any that reads a shared prefix once.  Its contents are
  * undefined on return; calls sharing one workspace must be ordered on one
  * stream.  Errors: SC_ESTALE, SC_EUNAVAILABLE (a page's state not written at
  * this layer), SC_EINVAL (workspace too small or misaligned), SC_EUNSUPPORTED,
@@ -449,13 +450,14 @@ int sc_cache_condense(sc_cache* cache, int32_t layer, int32_t n_layers, const sc
  * itself (`plan` may be freed) and goes wherever a plan of `plan`'s kind goes:
  * sc_attention, sc_attention_noalloc, sc_attention_weigh, and as the plan of a
  * block or stack or of its cross-attention.  The attention reads the prefix once
- * for the rows of all nodes where that pays.  Limits: at most 64 nodes and 800
- * pages with the prefix counted once; at least 32 tokens per page for bf16; and
- * where the nodes' lists hold more than 800 pages together, or pages of fewer
- * than 64 tokens are read by more than 64 queries a node, no more rows than
- * 136 MB of partials hold (two of head_dim + 2 fp32 values per row and head);
- * else SC_EUNSUPPORTED when the plan is used (SC_ECAPACITY if it is the
- * smaller scratch of sc_attention_noalloc that does not hold them).
+ * for the rows of all nodes where that pays; its logits are sc_attention_weigh's, so
+ * that it agrees with sc_attention over the same pages within rounding, not in bits.
+ * Limits: at most 64 nodes and 800 pages with the prefix counted once; at least 32
+ * tokens per page for bf16; and where the nodes' lists hold more than 800 pages
+ * together, or pages of fewer than 64 tokens are read by more than 64 queries a
+ * node, no more rows than 136 MB of partials hold (two of head_dim + 2 fp32 values
+ * per row and head); else SC_EUNSUPPORTED when the plan is used (SC_ECAPACITY if it
+ * is the smaller scratch of sc_attention_noalloc that does not hold them).
  * A plan that shares a prefix already gets the new states before it.
  * Errors: SC_EINVAL (null argument, n < 1, a state that would be read twice:
  * named twice, or read by a node of `plan`), SC_ENOTFOUND, SC_EUNSUPPORTED. */

@@ -707,7 +707,12 @@ __device__ __forceinline__ void probs(const STile<KH>& s, bf16x8 (&pb)[KH][2]) {
         pb[h][qb][e] = static_cast<__bf16>(__builtin_amdgcn_exp2f(s[h][e >> 2][qb][e & 3]));
 }
 
-// p = exp2(unit s): this lane's sums of the unrounded values are added to l.
+// p = exp2(unit s): this lane's sums of the unrounded values are added to l.  Rounded
+// to bf16 is p only as the operand of PV, which fp32 MFMAs would do at an eighth of the
+// rate (154 TFLOP/s against 1234): at most 2^-8 of each p, independent of each other,
+// which in the 2-norm adds as much as the output's own rounding (0.0023 from the exact
+// output; 0.0017 for fp32 products rounded once), and less where a row's largest p,
+// exactly 1, makes most of it.
 // (Taking the maximum off here, by an fma, instead of in the products' accumulators
 // was 1 % slower.)
 template <int KH>
