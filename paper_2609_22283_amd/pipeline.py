@@ -22,7 +22,9 @@ states that no later node selects are folded into one memory state that every
 node reads beside its window.  The stack weighs the keys that it reads
 (``sc_stack_forward_weigh``), each head keeps the heaviest tokens of the memory
 and the states that join it (``Cache.condense``), and the packs' plans get the
-memory as a shared prefix (``sc_plan_share``).
+memory as a shared prefix (``sc_plan_share``).  Weights accumulate and do not age:
+a token of the memory has gained weight in every forward since it was cached, so
+on long streams early tokens hold their places.
 
 Every computation runs in the library; this module sequences calls and moves
 device buffers.
