@@ -263,7 +263,7 @@ def prepare(case, seed):
 
     import paper_2609_22283_amd as sc
     s.sc = sc
-    states = _cached(case)
+    states = [] if kind == "rotate" else _cached(case)
     if kind == "rotate":
         F_, h, w = _grid(case)
         dims = (case["dim_t"], case["dim_h"], case["dim_w"])
@@ -322,7 +322,7 @@ def run(s):
     if not own:
         return {"attend": _plain_attend, "hold": _plain_hold, "park": _plain_park, "move": _plain_move,
                 "rotate": _plain_rotate}[kind](s)
-    sc, states = s.sc, _cached(case)
+    sc, states = s.sc, [] if kind == "rotate" else _cached(case)
     if kind == "attend":
         sc.sc_attention(s.plan, s.cache, 0, t["q"], s.o, s.scale, s.ws, s.ws_bytes)
         return {"o": s.o}
