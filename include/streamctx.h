@@ -47,7 +47,7 @@ enum {
 };
 
 enum { SC_POLICY_CLEAN = 0, SC_POLICY_SAME = 1, SC_POLICY_PROG = 2, SC_POLICY_TABLE = 3 };
-enum { SC_DTYPE_BF16 = 0, SC_DTYPE_F32 = 1 };
+enum { SC_DTYPE_BF16 = 0, SC_DTYPE_F32 = 1, SC_DTYPE_FP4 = 2 };
 
 typedef void* sc_stream; /* hipStream_t */
 
@@ -117,7 +117,18 @@ void sc_selection_free(sc_selection* sel);
  * (V is stored transposed: the attention kernel reads it as the A operand of
  * O^T = V^T P^T).  Slots are handed out lowest-free-first.  Requirements:
  * tokens_per_page a positive multiple of 8, head_dim 64 or 128 (bf16: 128).
- * The pool must outlive the cache handle. */
+ * The pool must outlive the cache handle.
+ *
+ * SC_DTYPE_FP4 (head_dim 128, a 16-byte aligned pool) holds keys and values in 4 bits:
+ * e2m1 codes (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) times a power of two
+ * shared by 32 of them, 4.25 bits a value.  A group is 32 channels of a key, or a
+ * channel of V over 32 tokens of its page (tokens 32 b .. 32 b + 31; fewer at the
+ * page's end).  The shared exponent is floor(log2 of the largest magnitude) - 2, at least
+ * -127; values are rounded to the nearest code, ties to the even one, and magnitudes above 6
+ * become 6.  A group with an infinity or a NaN reads as NaN throughout.  Everything
+ * beside the pages (k and v of an append, q and o) is bf16.  Blocks, stacks, weighing,
+ * folding and sc_condition_append take no 4-bit cache (SC_EUNSUPPORTED), but the
+ * condition that a block's cross-attention reads may be one. */
 typedef struct {
   int32_t n_layers, n_heads, head_dim, tokens_per_page, pages_per_chunk, n_slots, dtype;
 } sc_cache_desc;
@@ -131,8 +142,9 @@ int sc_cache_contains(const sc_cache* cache, sc_node state, int32_t layer);
 /* Copies the state's pages_per_chunk slot ids to slots[]. SC_ENOTFOUND. */
 int sc_cache_slots(const sc_cache* cache, sc_node state, int32_t* slots);
 int sc_cache_free_slot_count(const sc_cache* cache);
-/* Frees the state's slots in every layer and bumps their generation, so a
- * plan that still names them fails with SC_ESTALE.  SC_ENOTFOUND. */
+/* Frees the state's slots in every layer (those that no fork of the cache holds) and
+ * bumps their generation, so a plan of this handle that still names them fails with
+ * SC_ESTALE.  SC_ENOTFOUND. */
 int sc_cache_release(sc_cache* cache, sc_node state);
 
 /* ---- 3D RoPE table ------------------------------------------------------
@@ -154,15 +166,95 @@ typedef struct {
 size_t sc_rope_table_bytes(const sc_rope_desc* desc);
 int sc_rope_table_build(const sc_rope_desc* desc, void* dev_table, sc_stream stream);
 
+/* The same table with the time axis scaled for histories longer than `original` frames
+ * of training; it goes wherever an sc_rope goes.  With f_i = theta^(-2 i / dim_t):
+ *   SC_ROPE_UNSCALED  f_i
+ *   SC_ROPE_LINEAR    f_i / factor (positions are interpolated)
+ *   SC_ROPE_NTK       theta * factor^(dim_t / (dim_t - 2)) in place of theta (dim_t > 2)
+ *   SC_ROPE_YARN      f_i (g_i + (1 - g_i) / factor), g_i = (r_i - beta_slow) / (beta_fast -
+ *                     beta_slow) clamped to [0, 1], r_i = original f_i / (2 pi): pairs that
+ *                     turn often in training keep their frequency, slow ones are interpolated
+ * Every cosine and sine of the table is multiplied by magnitude (1: a rotation).
+ * Errors: SC_EINVAL (null argument, a bad descriptor, an unknown kind, factor < 1,
+ * magnitude <= 0, original <= 0 or beta_fast <= beta_slow, values that are not finite). */
+enum { SC_ROPE_UNSCALED = 0, SC_ROPE_LINEAR = 1, SC_ROPE_NTK = 2, SC_ROPE_YARN = 3 };
+typedef struct {
+  int32_t kind;
+  double factor, original, beta_fast, beta_slow, magnitude; /* read where the kind uses them */
+} sc_rope_scaling;
+int sc_rope_table_build_scaled(const sc_rope_desc* desc, const sc_rope_scaling* scaling, void* dev_table,
+                               sc_stream stream);
+
+/* Rotates the rows of a tensor [n_rows][n_heads][head_dim] at positions of their own: the
+ * queries of sc_attention, keys whose cache does not rotate them, or (transpose) their
+ * gradients.  The first R = dim_t + dim_h + dim_w channels of a head (R <= head_dim) are R / 2
+ * pairs, those of the time axis first, then height, then width; pair p is the channels
+ *   SC_ROPE_INTERLEAVED  (2 p, 2 p + 1)        SC_ROPE_HALF  (p, p + R / 2)
+ * and becomes (x0 c - x1 s, x0 s + x1 c), in fp32, c and s the table's at the row's
+ * position; with transpose (x0 c + x1 s, -x0 s + x1 c), which takes a gradient back and,
+ * at magnitude 1, undoes the rotation.  Channels behind the R are copied.
+ * x, y: device, of `dtype` (bf16 or fp32), element-aligned; strides between rows and between
+ * heads in elements (channels are adjacent), so that a slice of a wider tensor is taken as it
+ * is; x may repeat rows or heads (a stride of 0).  y is x itself with the same strides, or
+ * lies apart from it.  positions: device int32 [n_rows][3] (t, h, w), read asynchronously; a
+ * row whose position is outside the table (a negative one marks padding) is left as it is
+ * in y.  n_rows may be 0.  Errors: SC_EINVAL (null argument, a bad shape, layout or
+ * descriptor, R < 2 or R > head_dim, a misaligned or overlapping tensor), SC_EUNSUPPORTED,
+ * SC_EDEVICE. */
+enum { SC_ROPE_INTERLEAVED = 0, SC_ROPE_HALF = 1 };
+typedef struct {
+  int32_t n_rows, n_heads, head_dim, dtype, layout, transpose;
+  int64_t x_row, x_head, y_row, y_head;
+} sc_rotate_desc;
+int sc_rope_rotate(const sc_rope* rope, const sc_rotate_desc* desc, const void* x, void* y,
+                   const int32_t* positions, sc_stream stream);
+
 /* Writes the K/V of one state for one layer into its page slots (allocating
  * them, lowest free first, unless a plan reserved them).  k, v: device
- * [pages_per_chunk * tokens_per_page, n_heads, head_dim] in the cache dtype,
+ * [pages_per_chunk * tokens_per_page, n_heads, head_dim] in the cache dtype (4-bit
+ * caches: bf16, held as the states that sc_cache_copy takes out of a bf16 cache),
  * read asynchronously on the stream.  With rope != NULL the keys are rotated
  * at the state's absolute positions first (grid_h * grid_w must equal
  * tokens_per_page).  Errors: SC_EEXIST (layer already written),
  * SC_ECAPACITY, SC_EINVAL, SC_EDEVICE. */
 int sc_cache_append(sc_cache* cache, int32_t layer, sc_node state, const void* k,
                     const void* v, const sc_rope* rope, sc_stream stream);
+
+/* ---- Pages: copied, shared, gathered and moved ----------------------------
+ * Writes copies of n cached states of `from` into states of `to` (which may be the same
+ * cache), in layers [layer, layer + n_layers) of both: into[i] becomes states[i].  The
+ * caches have the same heads and page geometry, and one dtype (the pages as they are) or one
+ * of them is bf16 and the other SC_DTYPE_FP4: states go into 4 bits, and come back as
+ * the bf16 values that their codes stand for.  `into` gets slots as by sc_cache_append.
+ * Errors (both caches unchanged): SC_EINVAL (null argument, n < 1, layers out of range, caches
+ * that do not match, overlapping pools, a state of `into` named twice), SC_ENOTFOUND,
+ * SC_EUNAVAILABLE (a source not written at one of the layers), SC_EEXIST (a state of `into`
+ * written at one of them), SC_ECAPACITY, SC_EUNSUPPORTED, SC_EDEVICE. */
+int sc_cache_copy(const sc_cache* from, const sc_node* states, int32_t n, sc_cache* to, const sc_node* into,
+                  int32_t layer, int32_t n_layers, sc_stream stream);
+/* A second handle over the cache's pool that holds the same states, for a stream that
+ * branches: pages are shared, nothing is copied, and what either handle appends or releases
+ * from then on is its own (a slot is free once no handle holds it).  Every state must be
+ * written in every layer.  Plans belong to the handle that they were built with.  Handles
+ * over one pool are used by one thread at a time, like one handle; weights kept beside the
+ * cache go by slots, which the handles share.  Free it with sc_cache_free.
+ * Errors: SC_EINVAL, SC_EUNAVAILABLE (a state not written at some layer). */
+int sc_cache_fork(sc_cache* cache, sc_cache** out);
+/* Moves pages, in every layer, until the slots in use (of all handles over the pool) are the
+ * lowest ones.  Plans that name a moved page fail with SC_ESTALE from then on.  weights: the
+ * array kept beside the cache, whose rows move along, or NULL.  Errors: SC_EINVAL,
+ * SC_EDEVICE (nothing has moved). */
+int sc_cache_compact(sc_cache* cache, float* weights, sc_stream stream);
+/* Moves the pages to another pool, of n_slots slots (sc_cache_pool_bytes with that many), in
+ * the order of their slots from slot 0 on; every handle over the old pool is over the new
+ * one afterwards, and all plans are stale.  The old pool is read asynchronously on the
+ * stream and not used after that.  weights, moved_weights: the array kept beside the cache
+ * and the one that takes its place, or both NULL; rows of slots in use are moved.
+ * Errors (nothing has changed): SC_EINVAL (null argument, n_slots < 1, overlapping pools or
+ * weights, one of the weights without the other), SC_ECAPACITY (more slots in use),
+ * SC_EDEVICE. */
+int sc_cache_move(sc_cache* cache, void* dev_pool, int32_t n_slots, const float* weights, float* moved_weights,
+                  sc_stream stream);
 
 /* ---- Plan: availability and page lists (Eq. 6, Eq. 8) ------------------
  * Resolves every segment of the selection to page slots and checks
@@ -202,7 +294,9 @@ int sc_plan_condition(sc_cache* cache, const sc_node* conditions, int32_t n, int
  * no per-round host-to-device copy is needed); larger plans fail with
  * SC_EUNSUPPORTED before anything is launched.  bf16 caches need head_dim
  * 128 and pages of at least one key tile: 32 tokens when Nq <= 64, 64
- * otherwise (else SC_EUNSUPPORTED).  ws: device scratch, 16-byte aligned, of at least
+ * otherwise (else SC_EUNSUPPORTED).  4-bit caches: q and o are bf16, logits are products of q
+ * as it is and of the values that the codes stand for; q 16-byte aligned, a finite scale
+ * and at most 2^31 - 1 rows (else SC_EINVAL, SC_EUNSUPPORTED).  ws: device scratch, 16-byte aligned, of at least
  * sc_attention_workspace_bytes(plan, cache) bytes (may be NULL when that is
  * 0, as for fp32 caches unless the nodes share a prefix); the bf16 kernel splits
  * long key ranges across work-groups and merges their partial softmax sums

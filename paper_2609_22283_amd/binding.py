@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import weakref
 from typing import List, Optional, Sequence, Tuple
 
 __all__ = [
@@ -28,14 +29,16 @@ __all__ = [
     "sc_serial_steps", "sc_serial_step_node", "sc_block_workspace_views",
     "sc_attention_noalloc", "sc_attention_noalloc_scratch_bytes",
     "sc_cache_weights_bytes", "sc_attention_weigh_workspace_bytes", "sc_attention_weigh", "sc_plan_share",
-    "sc_stack_forward_weigh",
+    "sc_stack_forward_weigh", "SC_DTYPE_FP4", "sc_rope_rotate",
 ]
 
 SC_OK, SC_EINVAL, SC_EUNAVAILABLE, SC_ECAPACITY = 0, -1, -2, -3
 SC_EEXIST, SC_ENOTFOUND, SC_ESTALE, SC_EDEVICE, SC_EUNSUPPORTED = -4, -5, -6, -7, -8
 SC_POLICY_CLEAN, SC_POLICY_SAME, SC_POLICY_PROG, SC_POLICY_TABLE = 0, 1, 2, 3
-SC_DTYPE_BF16, SC_DTYPE_F32 = 0, 1
+SC_DTYPE_BF16, SC_DTYPE_F32, SC_DTYPE_FP4 = 0, 1, 2
 POLICY_KINDS = {"clean": 0, "same": 1, "prog": 2, "table": 3}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
+ROPE_LAYOUTS = {"interleaved": 0, "half": 1}
 
 # Every function the headers under include/ declare (checked by the CPU tests).
 EXPORTED_SYMBOLS = [
@@ -55,6 +58,8 @@ EXPORTED_SYMBOLS = [
     "sc_attention_noalloc", "sc_attention_noalloc_scratch_bytes",
     "sc_cache_weights_bytes", "sc_cache_weights_clear", "sc_attention_weigh_workspace_bytes",
     "sc_attention_weigh", "sc_cache_condense", "sc_plan_share", "sc_stack_forward_weigh",
+    "sc_cache_copy", "sc_cache_fork", "sc_cache_compact", "sc_cache_move", "sc_rope_table_build_scaled",
+    "sc_rope_rotate",
 ]
 
 # The library and PyTorch must share one HIP runtime: torch ships its own
@@ -104,6 +109,16 @@ class sc_rope_desc(C.Structure):
 
 class sc_rope(C.Structure):
     _fields_ = [("desc", sc_rope_desc), ("dev_table", C.c_void_p)]
+
+
+class sc_rope_scaling(C.Structure):
+    _fields_ = [("kind", C.c_int32)] + [(n, C.c_double) for n in
+                                        ("factor", "original", "beta_fast", "beta_slow", "magnitude")]
+
+
+class sc_rotate_desc(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("n_rows", "n_heads", "head_dim", "dtype", "layout", "transpose")] +
+                [(n, C.c_int64) for n in ("x_row", "x_head", "y_row", "y_head")])
 
 
 class sc_cross_attn(C.Structure):
@@ -178,6 +193,12 @@ _SIG = {
     "sc_attention_weigh": (C.c_int, [_P, _P, C.c_int32, _P, _P, C.c_float, _P, _P, C.c_size_t, _P]),
     "sc_cache_condense": (C.c_int, [_P, C.c_int32, C.c_int32, C.POINTER(sc_node), C.c_int32, sc_node, _P, _P, _P]),
     "sc_plan_share": (C.c_int, [_P, C.POINTER(sc_node), C.c_int32, C.POINTER(_P)]),
+    "sc_cache_copy": (C.c_int, [_P, C.POINTER(sc_node), C.c_int32, _P, C.POINTER(sc_node), C.c_int32, C.c_int32, _P]),
+    "sc_cache_fork": (C.c_int, [_P, C.POINTER(_P)]),
+    "sc_cache_compact": (C.c_int, [_P, _P, _P]),
+    "sc_cache_move": (C.c_int, [_P, _P, C.c_int32, _P, _P, _P]),
+    "sc_rope_table_build_scaled": (C.c_int, [C.POINTER(sc_rope_desc), C.POINTER(sc_rope_scaling), _P, _P]),
+    "sc_rope_rotate": (C.c_int, [C.POINTER(sc_rope), C.POINTER(sc_rotate_desc), _P, _P, _P, _P]),
     "sc_stack_forward_weigh": (C.c_int, [C.POINTER(sc_block_weights), C.c_int32, _P, _P, _P,
                                          C.POINTER(sc_rope), _P, C.c_size_t, _P, _P, C.c_size_t, _P]),
 }
@@ -295,6 +316,10 @@ def sc_selection_build(kind, K, W, nodes: Sequence[Tuple[int, int]], phi_table=N
 
 
 # ---------------------------------------------------------------------- cache
+def _nodes(states):
+    return (sc_node * max(1, len(states)))(*[sc_node(int(c), int(j)) for c, j in states])
+
+
 def _desc(n_layers, n_heads, head_dim, tokens_per_page, pages_per_chunk, n_slots, dtype):
     return sc_cache_desc(n_layers, n_heads, head_dim, tokens_per_page, pages_per_chunk, n_slots, dtype)
 
@@ -312,6 +337,7 @@ class Cache:
         self._h = C.c_void_p(handle)
         self.desc = desc
         self.pool = pool  # keeps the caller's buffer alive
+        self._family = weakref.WeakSet([self])  # the handles over this pool
 
     def __del__(self):
         if getattr(self, "_h", None) and self._h.value:
@@ -350,9 +376,40 @@ class Cache:
         [layer, layer + n_layers): each head keeps its heaviest tokens (``weights``:
         fp32 [n_layers][n_slots][heads][tokens] of the whole cache).  ``kept``
         (device int32 [n_layers, heads, tokens of a state]) receives their numbers."""
-        arr = (sc_node * max(1, len(sources)))(*[sc_node(int(c), int(j)) for c, j in sources])
+        arr = _nodes(sources)
         _check(lib.sc_cache_condense(self._h, layer, n_layers, arr, len(sources), sc_node(*into),
                                      _ptr(weights), _ptr(kept), _stream(stream)))
+
+
+    def copy(self, states, to: "Cache", into, layer: int, n_layers: int, stream=None) -> None:
+        """Write copies of ``states`` into the states ``into`` of the cache ``to`` (this one, or
+        another of the same geometry: of the same dtype, or one bf16 and one in 4 bits)."""
+        if len(states) != len(into):
+            raise ScError(SC_EINVAL, f"SC_EINVAL: {len(states)} states into {len(into)}")
+        _check(lib.sc_cache_copy(self._h, _nodes(states), len(states), to._h, _nodes(into), layer, n_layers,
+                                 _stream(stream)))
+
+    def fork(self) -> "Cache":
+        """A second handle over the same pool that holds the same states, whose pages it shares."""
+        out = C.c_void_p()
+        _check(lib.sc_cache_fork(self._h, C.byref(out)))
+        f = Cache(out.value, self.desc, self.pool)
+        f._family = self._family
+        self._family.add(f)
+        return f
+
+    def compact(self, weights=None, stream=None) -> None:
+        """Move pages until the slots in use are the lowest ones (and the rows of ``weights`` along)."""
+        _check(lib.sc_cache_compact(self._h, _ptr(weights), _stream(stream)))
+
+    def move(self, pool, n_slots: int, weights=None, moved_weights=None, stream=None) -> None:
+        """Move the pages of this cache and its forks to ``pool``, of ``n_slots`` slots, in the order
+        of their slots (and the rows of ``weights`` to ``moved_weights``)."""
+        _check(lib.sc_cache_move(self._h, _ptr(pool), n_slots, _ptr(weights), _ptr(moved_weights), _stream(stream)))
+        for c in self._family:
+            d = c.desc
+            c.pool = pool
+            c.desc = _desc(d.n_layers, d.n_heads, d.head_dim, d.tokens_per_page, d.pages_per_chunk, n_slots, d.dtype)
 
 
 def sc_cache_create(pool, n_layers, n_heads, head_dim, tokens_per_page, pages_per_chunk, n_slots,
@@ -379,10 +436,39 @@ def sc_rope_table_bytes(grid_h, grid_w, dims, max_frames, theta=10000.0) -> int:
     return lib.sc_rope_table_bytes(C.byref(d))
 
 
-def sc_rope_table_build(table, grid_h, grid_w, dims, max_frames, theta=10000.0, stream=None) -> Rope:
+def sc_rope_table_build(table, grid_h, grid_w, dims, max_frames, theta=10000.0, stream=None, scaling=None) -> Rope:
+    """``scaling``: None, or a dict for a scaled time axis (sc_rope_table_build_scaled): ``kind``
+    ("none", "linear", "ntk" or "yarn"), ``factor``, ``original``, ``beta_fast`` (32), ``beta_slow`` (1)
+    and ``magnitude`` (1)."""
     d = _rope_desc(grid_h, grid_w, dims, max_frames, theta)
-    _check(lib.sc_rope_table_build(C.byref(d), _ptr(table), _stream(stream)))
+    if scaling is None:
+        _check(lib.sc_rope_table_build(C.byref(d), _ptr(table), _stream(stream)))
+        return Rope(d, table)
+    known = {"kind": "none", "factor": 1.0, "original": 0.0, "beta_fast": 32.0, "beta_slow": 1.0, "magnitude": 1.0}
+    if set(scaling) - set(known) or scaling.get("kind", "none") not in ROPE_SCALINGS:
+        raise ScError(SC_EINVAL, f"SC_EINVAL: unknown scaling {scaling}")
+    v = {**known, **scaling}
+    s = sc_rope_scaling(ROPE_SCALINGS[v["kind"]], *[float(v[n]) for n in list(known)[1:]])
+    _check(lib.sc_rope_table_build_scaled(C.byref(d), C.byref(s), _ptr(table), _stream(stream)))
     return Rope(d, table)
+
+
+def sc_rope_rotate(rope: Rope, x, y, positions, layout: str = "interleaved", transpose: bool = False,
+                   stream=None) -> None:
+    """Rotate the rows of ``x`` [rows, heads, head_dim] (bf16 or fp32, any strides between rows
+    and heads) at ``positions`` (int32 [rows, 3]) into ``y``, of the same shape and dtype; ``y``
+    may be ``x``."""
+    import torch
+    codes = {torch.bfloat16: SC_DTYPE_BF16, torch.float32: SC_DTYPE_F32}
+    if (x.dim() != 3 or y.shape != x.shape or x.dtype not in codes or y.dtype != x.dtype or
+            (x.numel() and (x.stride(2) != 1 or y.stride(2) != 1) and x.shape[2] != 1) or layout not in ROPE_LAYOUTS):
+        raise ScError(SC_EINVAL, "SC_EINVAL: x and y are [rows, heads, head_dim] of one dtype (bf16, fp32) with adjacent "
+                                 f"channels, the layout one of {sorted(ROPE_LAYOUTS)}")
+    if tuple(positions.shape) != (x.shape[0], 3) or positions.dtype != torch.int32 or not positions.is_contiguous():
+        raise ScError(SC_EINVAL, "SC_EINVAL: positions are contiguous int32 [rows, 3]")
+    d = sc_rotate_desc(x.shape[0], x.shape[1], x.shape[2], codes[x.dtype], ROPE_LAYOUTS[layout], 1 if transpose else 0,
+                       x.stride(0), x.stride(1), y.stride(0), y.stride(1))
+    _check(lib.sc_rope_rotate(C.byref(rope.struct), C.byref(d), _ptr(x), _ptr(y), _ptr(positions), _stream(stream)))
 
 
 # ----------------------------------------------------------------------- plan

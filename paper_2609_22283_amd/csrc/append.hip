@@ -5,6 +5,7 @@
 // chunk * pages_per_chunk + frame, height = n / grid_w, width = n % grid_w)
 // with interleaved channel pairs split over the three axes.
 #include "device.h"
+#include "fp4.h"
 #include "internal.h"
 
 namespace sc {
@@ -193,6 +194,7 @@ int launch_append(const sc_cache* c, int32_t layer, const int32_t* slots, int32_
                   const void* k, const void* v, const sc_rope* rope, hipStream_t stream) {
   const sc_cache_desc& d = c->d;
   if (d.pages_per_chunk > 32) return fail(SC_EUNSUPPORTED, "pages_per_chunk > 32");
+  if (d.dtype == SC_DTYPE_FP4) return launch_fp4_append(c, layer, slots, chunk, k, v, rope, stream);
   SlotList sl;
   for (int i = 0; i < d.pages_per_chunk; ++i) sl.slot[i] = slots[i];
   RopeArgs ra{};

@@ -101,6 +101,7 @@ static AttnSchedule workspace_schedule(const sc_plan* p, const sc_cache* c) {
 static size_t share_workspace_bytes(const sc_plan* p, const sc_cache* c, bool lse);
 size_t attention_workspace_bytes(const sc_plan* p, const sc_cache* c) {
   if (p->nodes.empty()) return 0;
+  if (c->d.dtype == SC_DTYPE_FP4) return fp4_attention_workspace_bytes(p, c);
   if (p->shared) return share_workspace_bytes(p, c, false);
   return c->d.dtype == SC_DTYPE_BF16 ? workspace_schedule(p, c).partial_bytes() : 0;
 }
@@ -197,6 +198,7 @@ int attention_check(const sc_plan* p, const sc_cache* c) {
   if (n > kMaxNodes) return fail(SC_EUNSUPPORTED, "pack of %d nodes exceeds %d", n, kMaxNodes);
   const size_t pages = p->page_slot.size() - (size_t)std::max(n - 1, 0) * p->shared;  // shared ones once
   if (pages > (size_t)kMaxPages) return fail(SC_EUNSUPPORTED, "plan of %zu pages exceeds %d", pages, kMaxPages);
+  if (d.dtype == SC_DTYPE_FP4) return SC_OK;
   if (p->shared) {
     const int rc = share_check(p, c);
     if (rc != SC_OK) return rc;
@@ -625,6 +627,7 @@ int launch_attention_lse(const sc_plan* p, const sc_cache* c, int32_t layer, con
                          float scale, void* ws, size_t ws_bytes, hipStream_t stream) {
   const int rc = attention_check(p, c);
   if (rc != SC_OK) return rc;
+  if (c->d.dtype == SC_DTYPE_FP4) return launch_fp4_attention(p, c, layer, q, o, scale, ws, ws ? ws_bytes : 0, stream);
   const size_t need = lse ? attention_lse_workspace_bytes(p, c) : attention_workspace_bytes(p, c);
   if (ws_bytes < need || (need && !ws))
     return fail(SC_EINVAL, "attention workspace of %zu bytes, need %zu", ws_bytes, need);
@@ -652,6 +655,7 @@ extern "C" int sc_attention_form(const sc_plan* p, const sc_cache* c, int32_t* q
   if (p->nodes.empty()) return fail(SC_EINVAL, "a plan without nodes launches nothing");
   const int rc = attention_check(p, c);
   if (rc != SC_OK) return rc;
+  if (c->d.dtype == SC_DTYPE_FP4) return fp4_attention_form(p, c, queries, ring, pieces);
   *queries = F32_BQ;
   *ring = *pieces = 1;
   AttnSchedule ts{};
@@ -717,7 +721,9 @@ extern "C" int sc_attention_noalloc(const sc_plan* p, const sc_cache* c, int32_t
   if (p->nodes.empty()) return SC_OK;
   if ((rc = attention_check(p, c)) != SC_OK) return rc;
   void* ptr = nullptr;
-  if ((p->shared || c->d.dtype == SC_DTYPE_BF16) && (rc = scratch_address(&ptr)) != SC_OK) return rc;
+  if ((p->shared || c->d.dtype != SC_DTYPE_F32) && (rc = scratch_address(&ptr)) != SC_OK) return rc;
+  if (c->d.dtype == SC_DTYPE_FP4)
+    return launch_fp4_attention(p, c, layer, q, o, scale, ptr, kNoAllocScratchBytes, static_cast<hipStream_t>(stream));
   if (p->shared) {
     const ShareSchedule& s = share_schedule(p, c, kNoAllocScratchBytes, false);
     if (s.us >= 1e30) return fail(SC_ECAPACITY, "the rows sharing a prefix need more partials than the scratch holds");

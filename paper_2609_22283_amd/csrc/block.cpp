@@ -44,7 +44,7 @@ static int cross_check(const sc_cross_attn* cr, const sc_cache* c, const sc_plan
   if (!cr->w_q || !cr->w_o || !cr->cache || !cr->plan)
     return fail(SC_EINVAL, "cross-attention needs w_q, w_o, a condition cache and its plan");
   const sc_cache_desc& e = cr->cache->d;
-  if (e.dtype != SC_DTYPE_BF16 || e.n_heads != c->d.n_heads || e.head_dim != c->d.head_dim)
+  if ((e.dtype != SC_DTYPE_BF16 && e.dtype != SC_DTYPE_FP4) || e.n_heads != c->d.n_heads || e.head_dim != c->d.head_dim)
     return fail(SC_EINVAL, "condition cache (%d heads x %d, dtype %d) does not match the block",
                 e.n_heads, e.head_dim, e.dtype);
   if (cr->plan->nodes.size() != p->nodes.size() || cr->plan->nq != p->nq)
@@ -113,13 +113,13 @@ int sc::block_check(const sc_block_weights* w, const sc_cache* c, int32_t layer,
   }
   for (size_t q = 0; q < p->page_slot.size(); ++q) {
     int32_t s = p->page_slot[q];
-    if (!c->used[s] || c->gen[s] != p->page_gen[q])
+    if (!page_current(c, s, p->page_gen[q]))
       return fail(SC_ESTALE, "slot %d was released after the plan was built", s);
     const StateKey& key = p->page_state[q];
     bool in_pack = false;
     for (int32_t i = 0; i < n; ++i)
       if (p->nodes[i].chunk == key.first && p->nodes[i].level == key.second) in_pack = true;
-    if (!in_pack && !c->states.at(key).written[layer])
+    if (!in_pack && !c->table->written[(size_t)layer * d.n_slots + s])
       return fail(SC_EUNAVAILABLE, "state (%d,%d) has no K/V at layer %d", key.first, key.second, layer);
   }
   return SC_OK;

@@ -37,11 +37,11 @@ int plan_check(const sc_plan* plan, const sc_cache* cache, int32_t layer) {
   for (int32_t i = 0; i < n; ++i)
     for (size_t p = first(i); p < (size_t)plan->page_off[i + 1]; ++p) {
       int32_t s = plan->page_slot[p];
-      if (!cache->used[s] || cache->gen[s] != plan->page_gen[p])
+      if (!page_current(cache, s, plan->page_gen[p]))
         return fail(SC_ESTALE, "slot %d was released after the plan was built", s);
     }
   // every slot is still the one planned (above), so its flag is its state's
-  const uint8_t* wr = cache->slot_written.data() + (size_t)layer * cache->d.n_slots;
+  const uint8_t* wr = cache->table->written.data() + (size_t)layer * cache->d.n_slots;
   for (int32_t i = 0; i < n; ++i)
     for (size_t p = first(i); p < (size_t)plan->page_off[i + 1]; ++p)
       if (!wr[plan->page_slot[p]])
@@ -50,9 +50,13 @@ int plan_check(const sc_plan* plan, const sc_cache* cache, int32_t layer) {
   return SC_OK;
 }
 
+int32_t free_slots(const sc_cache* cache) {
+  return (int32_t)std::count(cache->table->refs.begin(), cache->table->refs.end(), 0);
+}
+
 void set_written(sc_cache* cache, StateEntry& e, int32_t layer, uint8_t v) {
   e.written[layer] = v;
-  for (int32_t s : e.slots) cache->slot_written[(size_t)layer * cache->d.n_slots + s] = v;
+  for (int32_t s : e.slots) cache->table->written[(size_t)layer * cache->d.n_slots + s] = v;
 }
 
 int policy_check(const sc_policy* p) {
@@ -210,14 +214,17 @@ static int validate_desc(const sc_cache_desc* d) {
   if (d->tokens_per_page < 8 || d->tokens_per_page % 8 != 0)
     return fail(SC_EINVAL, "tokens_per_page must be a positive multiple of 8 (got %d)",
                 d->tokens_per_page);
-  if (d->dtype != SC_DTYPE_BF16 && d->dtype != SC_DTYPE_F32)
+  if (d->dtype != SC_DTYPE_BF16 && d->dtype != SC_DTYPE_F32 && d->dtype != SC_DTYPE_FP4)
     return fail(SC_EINVAL, "unknown dtype %d", d->dtype);
   if (d->head_dim != 64 && d->head_dim != 128)
     return fail(SC_EUNSUPPORTED, "head_dim must be 64 or 128 (got %d)", d->head_dim);
+  if (d->dtype == SC_DTYPE_FP4 && d->head_dim != 128)
+    return fail(SC_EUNSUPPORTED, "4-bit caches need head_dim 128 (got %d)", d->head_dim);
   return SC_OK;
 }
 
 static size_t slot_bytes(const sc_cache_desc* d) {
+  if (d->dtype == SC_DTYPE_FP4) return (size_t)d->n_heads * fp4_blocks(d->tokens_per_page) * kFp4Block;
   return 2ull * d->n_heads * d->tokens_per_page * d->head_dim * dtype_size(d->dtype);
 }
 
@@ -231,21 +238,43 @@ int sc_cache_create(const sc_cache_desc* d, void* pool, sc_cache** out) {
   *out = nullptr;
   int rc = validate_desc(d);
   if (rc != SC_OK) return rc;
-  sc_cache* c = new (std::nothrow) sc_cache;
-  if (!c) return fail(SC_EINVAL, "out of host memory");
-  c->d = *d;
-  c->pool = static_cast<char*>(pool);
-  c->slot_bytes = slot_bytes(d);
-  c->kv_half = c->slot_bytes / 2;
-  c->used.assign(d->n_slots, 0);
-  c->gen.assign(d->n_slots, 0);
-  c->owner.assign(d->n_slots, StateKey(-1, -1));
-  c->slot_written.assign((size_t)d->n_layers * d->n_slots, 0);
-  *out = c;
+  if (d->dtype == SC_DTYPE_FP4 && reinterpret_cast<uintptr_t>(pool) & 15)
+    return fail(SC_EINVAL, "the pool of a 4-bit cache must be 16-byte aligned");
+  try {
+    std::unique_ptr<sc_cache> c(new sc_cache);
+    c->d = *d;
+    c->pool = static_cast<char*>(pool);
+    c->slot_bytes = slot_bytes(d);
+    c->kv_half = d->dtype == SC_DTYPE_FP4 ? 0 : c->slot_bytes / 2;
+    c->table = std::make_shared<SlotTable>();
+    c->table->refs.assign(d->n_slots, 0);
+    c->gen.assign(d->n_slots, 0);
+    c->table->written.assign((size_t)d->n_layers * d->n_slots, 0);
+    c->table->handles.push_back(c.get());
+    *out = c.release();
+  } catch (const std::bad_alloc&) {
+    return fail(SC_EINVAL, "out of host memory");
+  }
   return SC_OK;
 }
 
-void sc_cache_free(sc_cache* c) { delete c; }
+// A handle gives up a state's slots; those that no fork holds are free.
+static void drop_slots(sc_cache* c, const StateEntry& e) {
+  SlotTable& t = *c->table;
+  for (int32_t s : e.slots) {
+    c->gen[s] += 1;
+    if (--t.refs[s]) continue;
+    for (int32_t l = 0; l < c->d.n_layers; ++l) t.written[(size_t)l * c->d.n_slots + s] = 0;
+  }
+}
+
+void sc_cache_free(sc_cache* c) {
+  if (!c) return;
+  for (const auto& kv : c->states) drop_slots(c, kv.second);
+  auto& all = c->table->handles;
+  all.erase(std::find(all.begin(), all.end(), c));
+  delete c;
+}
 
 int sc_cache_contains(const sc_cache* c, sc_node st, int32_t layer) {
   if (!c) return fail(SC_EINVAL, "null cache");
@@ -266,25 +295,24 @@ int sc_cache_slots(const sc_cache* c, sc_node st, int32_t* slots) {
 
 int sc_cache_free_slot_count(const sc_cache* c) {
   if (!c) return fail(SC_EINVAL, "null cache");
-  return (int)std::count(c->used.begin(), c->used.end(), 0);
+  return free_slots(c);
 }
 
 // Lowest-free-first allocation of one state's pages (frames ascending).
 static int allocate_state(sc_cache* c, StateKey key) {
   std::vector<int32_t> got;
   for (int32_t s = 0; s < c->d.n_slots && (int32_t)got.size() < c->d.pages_per_chunk; ++s)
-    if (!c->used[s]) got.push_back(s);
+    if (!c->table->refs[s]) got.push_back(s);
   if ((int32_t)got.size() < c->d.pages_per_chunk)
     return fail(SC_ECAPACITY, "no free slots for state (%d,%d)", key.first, key.second);
-  for (int32_t s : got) {
-    c->used[s] = 1;
-    c->owner[s] = key;
-    for (int32_t l = 0; l < c->d.n_layers; ++l) c->slot_written[(size_t)l * c->d.n_slots + s] = 0;
-  }
   StateEntry e;
   e.slots = got;
   e.written.assign(c->d.n_layers, 0);
   c->states.emplace(key, std::move(e));
+  for (int32_t s : got) {
+    c->table->refs[s] = 1;
+    for (int32_t l = 0; l < c->d.n_layers; ++l) c->table->written[(size_t)l * c->d.n_slots + s] = 0;
+  }
   return SC_OK;
 }
 
@@ -292,12 +320,7 @@ int sc_cache_release(sc_cache* c, sc_node st) {
   if (!c) return fail(SC_EINVAL, "null cache");
   auto it = c->states.find(StateKey(st.chunk, st.level));
   if (it == c->states.end()) return fail(SC_ENOTFOUND, "state (%d,%d) not cached", st.chunk, st.level);
-  for (int32_t s : it->second.slots) {
-    c->used[s] = 0;
-    c->gen[s] += 1;
-    c->owner[s] = StateKey(-1, -1);
-    for (int32_t l = 0; l < c->d.n_layers; ++l) c->slot_written[(size_t)l * c->d.n_slots + s] = 0;
-  }
+  drop_slots(c, it->second);
   c->states.erase(it);
   return SC_OK;
 }
@@ -453,6 +476,11 @@ int sc_attention(const sc_plan* p, const sc_cache* c, int32_t layer, const void*
   int rc = plan_check(p, c, layer);
   if (rc != SC_OK) return rc;
   if (p->nodes.empty()) return SC_OK;
+  if (c->d.dtype == SC_DTYPE_FP4) {  // a block's launches may give it less, and it cuts less finely
+    if ((rc = attention_check(p, c)) != SC_OK) return rc;
+    const size_t need = attention_workspace_bytes(p, c);
+    if (ws_bytes < need || (need && !ws)) return fail(SC_EINVAL, "attention workspace of %zu bytes, need %zu", ws_bytes, need);
+  }
   return launch_attention(p, c, layer, q, o, scale, ws, ws_bytes, static_cast<hipStream_t>(stream));
 }
 

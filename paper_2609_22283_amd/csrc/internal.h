@@ -32,10 +32,30 @@ struct StateEntry {
   std::vector<uint8_t> written;  // per layer
 };
 
+// The page slots of a pool.  A cache and its forks (sc_cache_fork) have one table
+// between them; their states name its slots.
+struct SlotTable {
+  std::vector<int32_t> refs;  // handles whose states hold the slot; 0: free
+  // [layer * n_slots + slot]: the written flag of the slot's state at that
+  // layer (a flat copy of StateEntry::written, so that checking a plan's
+  // pages costs no map lookups); kept by set_written
+  std::vector<uint8_t> written;
+  std::vector<sc_cache*> handles;
+};
+
 struct ShareSchedule;  // attention.hip
 struct WeighLaunches;  // weigh.hip
+struct Fp4Schedule;    // attention_fp4.hip
 
+// Bytes of an element of q, k, v and o beside a cache of this type (pages of 4-bit
+// caches hold blocks: fp4.h).
 inline size_t dtype_size(int32_t dtype) { return dtype == SC_DTYPE_F32 ? 4 : 2; }
+
+// Pages of 4-bit caches: blocks of 32 tokens of a head (head_dim 128), a page's last one
+// padded; a slot is [head][block].
+constexpr int32_t kFp4Tokens = 32;    // tokens of a block
+constexpr int32_t kFp4Block = 4352;   // bytes of a block
+inline int32_t fp4_blocks(int32_t tokens_per_page) { return (tokens_per_page + kFp4Tokens - 1) / kFp4Tokens; }
 
 }  // namespace sc
 
@@ -50,15 +70,10 @@ struct sc_cache {
   sc_cache_desc d;
   char* pool;
   size_t slot_bytes;    // bytes of one slot in one layer (K and V)
-  size_t kv_half;       // offset of V within a slot
-  std::vector<uint8_t> used;
-  std::vector<uint32_t> gen;
-  std::vector<sc::StateKey> owner;  // slot -> state (valid when used)
+  size_t kv_half;       // offset of V within a slot (4-bit caches: 0, a block holds both)
+  std::shared_ptr<sc::SlotTable> table;
+  std::vector<uint32_t> gen;  // per slot: raised when this handle gives it up, or its page moves
   std::map<sc::StateKey, sc::StateEntry> states;
-  // [layer * n_slots + slot]: the written flag of the slot's state at that
-  // layer (a flat copy of StateEntry::written, so that checking a plan's
-  // pages costs no map lookups); kept by set_written
-  std::vector<uint8_t> slot_written;
 };
 
 struct sc_plan {
@@ -75,6 +90,8 @@ struct sc_plan {
   mutable std::vector<std::shared_ptr<const sc::ShareSchedule>> share;
   // its pages by the nodes that read them (built on first use)
   mutable std::shared_ptr<const sc::WeighLaunches> weigh;
+  // how it runs over a 4-bit cache (attention_fp4.hip; found on first use)
+  mutable std::vector<std::shared_ptr<const sc::Fp4Schedule>> fp4;
 };
 
 namespace sc {
@@ -86,6 +103,14 @@ int plan_check(const sc_plan* plan, const sc_cache* cache, int32_t layer);
 // The entry of a state about to be written at `layer`, its slots allocated if it
 // is new (*fresh: release it if the write fails).
 int state_for_append(sc_cache* cache, int32_t layer, StateKey key, StateEntry** e, bool* fresh);
+
+// Slots of `table` that nothing holds.
+int32_t free_slots(const sc_cache* cache);
+
+// Whether a page that a plan names is still the one it was built over.
+inline bool page_current(const sc_cache* cache, int32_t slot, uint32_t gen) {
+  return slot < cache->d.n_slots && cache->table->refs[slot] && cache->gen[slot] == gen;
+}
 
 // Sets a state's written flag at `layer` and its slots' copies of it.
 void set_written(sc_cache* cache, StateEntry& e, int32_t layer, uint8_t v);
@@ -122,6 +147,7 @@ size_t attention_workspace_bound();
 int launch_append(const sc_cache* cache, int32_t layer, const int32_t* slots, int32_t chunk,
                   const void* k, const void* v, const sc_rope* rope, hipStream_t stream);
 int launch_rope_table(const sc_rope_desc* d, void* table, hipStream_t stream);
+int launch_rope_scaled_table(const sc_rope_desc* d, const sc_rope_scaling* s, void* table, hipStream_t stream);
 
 int launch_weights_clear(const sc_cache* cache, const int32_t* slots, int32_t n, float* weights, hipStream_t stream);
 // Whether a fold of so many states fits a launch: SC_OK or SC_EUNSUPPORTED; the
@@ -138,6 +164,34 @@ int block_check(const sc_block_weights* w, const sc_cache* c, int32_t layer, con
                 const sc_rope* rope, const void* ws, size_t ws_bytes);
 int block_forward(const sc_block_weights* w, sc_cache* c, int32_t layer, const sc_plan* p, void* x,
                   const sc_rope* rope, void* ws, bool sums_in, const sc_block_weights* next, sc_stream stream);
+
+// Launchers of fp4_pages.hip.
+
+// Slots of one pool whose pages go to slots of another, in layers that lie a fixed
+// distance apart.
+struct PagePairs {
+  const int32_t *src, *dst;
+  int32_t n;
+};
+struct PoolView {
+  char* base;            // first layer
+  uint64_t layer_bytes;  // from one layer to the next
+};
+// Pages as they are, `bytes` each (a multiple of 16; the pools may lie at any even address).
+int launch_page_moves(const PoolView& from, const PoolView& to, uint64_t bytes, const PagePairs& pairs, int32_t layers,
+                      hipStream_t stream);
+// bf16 pages to 4-bit ones (pack) or back.
+int launch_page_convert(bool pack, const PoolView& from, const PoolView& to, const sc_cache_desc& d,
+                        const PagePairs& pairs, int32_t layers, hipStream_t stream);
+int launch_fp4_append(const sc_cache* cache, int32_t layer, const int32_t* slots, int32_t chunk, const void* k,
+                      const void* v, const sc_rope* rope, hipStream_t stream);
+
+// Launchers of attention_fp4.hip (their meaning as of those without the name, internal.h).
+size_t fp4_attention_workspace_bytes(const sc_plan* plan, const sc_cache* cache);
+// The cheapest way within `room` bytes at ws.
+int launch_fp4_attention(const sc_plan* plan, const sc_cache* cache, int32_t layer, const void* q, void* o, float scale,
+                         void* ws, size_t room, hipStream_t stream);
+int fp4_attention_form(const sc_plan* plan, const sc_cache* cache, int32_t* queries, int32_t* ring, int32_t* pieces);
 
 // Memory that the launches after an attention will read first, in their order:
 // weights, which a model of many layers finds in HBM every time.  While an object
@@ -192,7 +246,7 @@ enum TimerKind {
   TK_SAMPLER, TK_ATTN_COMBINE, TK_QK_NORM, TK_CROSS_ATTENTION, TK_GEMM_CROSS_Q,
   TK_GEMM_CROSS_OUT, TK_GEMM_CONDITION,
   TK_ROW_SCALE,  // launched by nothing: its name stays readable
-  TK_ATTN_WEIGH, TK_CONDENSE,
+  TK_ATTN_WEIGH, TK_CONDENSE, TK_PAGES, TK_ROTATE,
   TK_COUNT
 };
 void timer_begin(int kind, hipStream_t stream);

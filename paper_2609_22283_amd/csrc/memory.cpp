@@ -88,10 +88,15 @@ extern "C" int sc_cache_weights_clear(const sc_cache* c, sc_node st, float* weig
                               static_cast<hipStream_t>(stream));
 }
 
+static int weigh_supported(const sc_cache* c) {
+  return c->d.dtype == SC_DTYPE_FP4 ? fail(SC_EUNSUPPORTED, "keys in 4 bits are not weighed") : SC_OK;
+}
+
 extern "C" size_t sc_attention_weigh_workspace_bytes(const sc_plan* p, const sc_cache* c) {
   size_t need = 0;
   guarded([&]() -> int {
-    if (!p || !c || p->cache != c || p->nodes.empty() || attention_check(p, c) != SC_OK) return SC_EINVAL;
+    if (!p || !c || p->cache != c || p->nodes.empty() || weigh_supported(c) != SC_OK || attention_check(p, c) != SC_OK)
+      return SC_EINVAL;
     need = weigh_attention_bytes(p, c);
     return SC_OK;
   });
@@ -101,9 +106,9 @@ extern "C" size_t sc_attention_weigh_workspace_bytes(const sc_plan* p, const sc_
 // What the weighing of a plan needs besides the attention itself.
 static int weigh_check(const sc_plan* p, const sc_cache* c, const float* weights, const void* ws, size_t ws_bytes) {
   if (!weights) return fail(SC_EINVAL, "null argument");
-  if (p->nodes.empty()) return SC_OK;
-  const int rc = attention_check(p, c);
-  if (rc != SC_OK) return rc;
+  int rc = weigh_supported(c);
+  if (rc != SC_OK || p->nodes.empty()) return rc;
+  if ((rc = attention_check(p, c)) != SC_OK) return rc;
   const size_t need = weigh_attention_bytes(p, c);
   if (!ws || ws_bytes < need) return fail(SC_EINVAL, "workspace of %zu bytes, need %zu", ws ? ws_bytes : 0, need);
   if (reinterpret_cast<uintptr_t>(ws) & 15) return fail(SC_EINVAL, "workspace must be 16-byte aligned");
@@ -150,6 +155,7 @@ extern "C" int sc_cache_condense(sc_cache* c, int32_t layer, int32_t n_layers, c
     if (layer < 0 || n_layers < 1 || n_layers > c->d.n_layers - layer)
       return fail(SC_EINVAL, "layers %d .. %d outside [0, %d)", layer, layer + n_layers - 1, c->d.n_layers);
     if (into.chunk < 0 || into.level < 0) return fail(SC_EINVAL, "bad state (%d,%d)", into.chunk, into.level);
+    if (c->d.dtype == SC_DTYPE_FP4) return fail(SC_EUNSUPPORTED, "states in 4 bits are not folded");
     int rc = condense_check(c, n);
     if (rc != SC_OK) return rc;
     const StateKey to(into.chunk, into.level);
