@@ -3,7 +3,10 @@
 // For every pack node i and head h: O = softmax(Q K^T * scale) V over the keys of node i's
 // pages, K and V the values that the codes stand for; q and o are bf16.
 #include <algorithm>
+#include <cfloat>
+#include <climits>
 #include <cmath>
+#include <cstdlib>
 #include <cstring>
 
 #include "fp4.h"
@@ -21,9 +24,15 @@ struct Fp4List {
 struct Fp4Geom {
   const char* layer_base;
   uint64_t slot_bytes;
-  int32_t heads, tpp, blocks, nq;
+  int32_t heads, nodes, tpp, blocks, nq, rows;
   DivMagic blocks_div, nq_div;
-  float scale_log2;
+  float unit;       // |scale| log2(e), no less than FLT_MIN
+  uint32_t q_flip;  // sign bits of a negative scale
+  // The items, first those of the prefix (none where the nodes read it by themselves, joined),
+  // then the nodes' own: row tiles fastest, then heads, then (own) nodes, then pieces of so many
+  // chunks.
+  int32_t joined, p_items, p_tiles, p_pieces, p_len, o_tiles, o_len;
+  float *part_o, *part_ml;  // [piece][head][row][128], [piece][head][row][2], or NULL: one piece
 };
 
 static void fp4_fill(const sc_plan* p, const sc_cache* c, int32_t layer, float scale, Fp4List& l, Fp4Geom& g) {
@@ -42,92 +51,430 @@ static void fp4_fill(const sc_plan* p, const sc_cache* c, int32_t layer, float s
   g.layer_base = c->pool + (size_t)layer * d.n_slots * c->slot_bytes;
   g.slot_bytes = c->slot_bytes;
   g.heads = d.n_heads;
+  g.nodes = n;
+  g.rows = n * p->nq;
   g.tpp = d.tokens_per_page;
   g.blocks = fp4_blocks(d.tokens_per_page);
   g.nq = p->nq;
   g.blocks_div = magic_div((uint32_t)g.blocks);
   g.nq_div = magic_div((uint32_t)p->nq);
-  g.scale_log2 = scale * 1.4426950408889634f;
+  g.unit = std::max(std::fabs(scale) * 1.4426950408889634f, FLT_MIN);
+  g.q_flip = std::signbit(scale) ? 0x80008000u : 0u;
 }
 
-__device__ __forceinline__ float fp4_value(uint32_t code) {  // of the code in the low bits
-  const float m[8] = {0.f, 0.5f, 1.f, 1.5f, 2.f, 3.f, 4.f, 6.f};
-  const float v = m[code & 7u];
-  return code & 8u ? -v : v;
-}
-__device__ __forceinline__ float fp4_power(uint32_t s) {
-  return s == 255u ? __uint_as_float(0x7fc00000u) : ldexpf(1.f, (int)s - 127);
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef short i16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int FA_NW = 4;      // waves of a work-group
+constexpr int FA_ROW = 132;   // floats of a row of partial outputs in LDS
+
+// c + A B over 128: A 16 rows of codes (a lane: row lane % 16, the 32 columns of group lane / 16)
+// whose scales are byte SA of the lanes' sa, B 16 columns of e4m3 (a lane: column lane % 16, rows 16 g ..
+// + 15 and 64 + 16 g .. + 15 with g = lane / 16), scaled by 2^(sb - 127).
+template <int SA>
+__device__ __forceinline__ f32x4 mx(const u32x4& a, const i32x8& b, const f32x4& c, uint32_t sa, uint32_t sb) {
+  const i32x8 a8 = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b, c, 4, 0, SA, (int)sa, 0, (int)sb);
 }
 
-// A wave per row and head: a lane takes half the channels of one key of a block, and
-// two channels of the output.
-__global__ __launch_bounds__(64) void fp4_attention_plain_kernel(const uint16_t* __restrict__ q, uint16_t* __restrict__ o,
-                                                                 Fp4Geom g, Fp4List list) {
-  __shared__ float qs[128], ps[32];
-  const int32_t lane = threadIdx.x, row = blockIdx.x, h = blockIdx.y;
-  const int32_t node = (int32_t)fast_div((uint32_t)row, g.nq_div);
-  const uint16_t* qr = q + ((size_t)row * g.heads + h) * 128;
-  qs[2 * lane] = bf16_to_f32(qr[2 * lane]);
-  qs[2 * lane + 1] = bf16_to_f32(qr[2 * lane + 1]);
+// The larger (or the sum) of the values of lanes l, l ^ 16, l ^ 32, l ^ 48.
+__device__ __forceinline__ float quarters_max(float x) {
+  u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+  x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float quarters_sum(float x) {
+  u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+  x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Four fp32 numbers of at most 448 as e4m3, and what that leaves of them, times `up`, in
+// e4m3 again: 8 significant bits together, which is all that bf16 has.
+__device__ __forceinline__ void split_e4m3(float a, float b, float c, float d, float up, int& hi, int& lo) {
+  int h = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  h = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, h, true);
+  const f32x2 ab = __builtin_amdgcn_cvt_pk_f32_fp8(h, false), cd = __builtin_amdgcn_cvt_pk_f32_fp8(h, true);
+  int l = __builtin_amdgcn_cvt_pk_fp8_f32((a - ab[0]) * up, (b - ab[1]) * up, 0, false);
+  l = __builtin_amdgcn_cvt_pk_fp8_f32((c - cd[0]) * up, (d - cd[1]) * up, l, true);
+  hi = h;
+  lo = l;
+}
+
+// 16 query rows as the B operand, in two parts with a scale each.
+struct Fp4Rows {
+  i32x8 hi, lo;
+  uint32_t s_hi, s_lo;
+};
+__device__ __forceinline__ Fp4Rows load_rows(const uint16_t* row, int32_t quarter, uint32_t flip) {
+  u32x4 v[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const u32x4*>(row + 64 * (i >> 1) + 16 * quarter + 8 * (i & 1));
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      top = umax(top, bf16x2_top(v[i][j]));
+      v[i][j] ^= flip;
+    }
+  top = umax(top, (uint32_t)__shfl_xor((int)top, 16));
+  top = umax(top, (uint32_t)__shfl_xor((int)top, 32));
+  const uint32_t e = top >> 23, s = e > 7u ? e - 7u : 0u;  // the largest becomes 2^7 .. 2^8
+  const float by = __uint_as_float((e > 7u ? 261u - e : 254u) << 23);
+  Fp4Rows r;
+  r.s_hi = e == 255u ? 255u : s;
+  r.s_lo = s > 4u ? s - 4u : 0u;
+  const float up = __uint_as_float((127u + s - r.s_lo) << 23);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t a = v[i >> 1][2 * (i & 1)], b = v[i >> 1][2 * (i & 1) + 1];
+    int h, l;
+    split_e4m3(__uint_as_float(a << 16) * by, __uint_as_float(a & 0xffff0000u) * by, __uint_as_float(b << 16) * by,
+               __uint_as_float(b & 0xffff0000u) * by, up, h, l);
+    r.hi[i] = e == 255u ? 0 : h;
+    r.lo[i] = e == 255u ? 0 : l;
+  }
+  return r;
+}
+
+// What a work-group does: rows [row0, row0 + rows) of a head over the chunks [c0, c1) of 128
+// keys (four blocks) of a list of pages; `slot` its place among the partials.
+struct Fp4Item {
+  int32_t head, row0, rows, node, pages, first, blocks, c0, c1, slot;
+};
+template <int R>
+__device__ __forceinline__ Fp4Item fp4_item(const Fp4Geom& g, const Fp4List& list, int32_t b) {
+  Fp4Item it;
+  const bool prefix = b < g.p_items;
+  const int32_t tiles = prefix ? g.p_tiles : g.o_tiles;
+  if (!prefix) b -= g.p_items;
+  const int32_t tile = b % tiles;
+  b /= tiles;
+  it.head = b % g.heads;
+  b /= g.heads;
+  it.node = prefix ? 0 : b % g.nodes;
+  const int32_t piece = prefix ? b : b / g.nodes, len = prefix ? g.p_len : g.o_len;
+  it.row0 = (prefix ? 0 : it.node * g.nq) + tile * 16 * R;
+  it.rows = min(16 * R, (prefix ? g.rows : g.nq) - tile * 16 * R);
+  it.first = prefix ? 0 : list.off[it.node];
+  it.pages = prefix ? list.shared : list.off[it.node + 1] - it.first + (g.joined ? list.shared : 0);
+  it.blocks = it.pages * g.blocks;
+  it.c0 = piece * len;
+  it.c1 = min(it.c0 + len, (it.blocks + 3) / 4);
+  it.slot = prefix ? piece : g.p_pieces + piece;
+  return it;
+}
+
+template <int R>
+__global__ __launch_bounds__(64 * FA_NW, 2) void fp4_attention_kernel(const uint16_t* __restrict__ q, uint16_t* __restrict__ o,
+                                                                      Fp4Geom g, Fp4List list) {
+  __shared__ __attribute__((aligned(16))) float part[FA_NW][16 * FA_ROW];
+  __shared__ float ml[FA_NW][2][16];
+  __shared__ uint64_t base[kFp4Pages];
+  const int32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const Fp4Item it = fp4_item<R>(g, list, (int32_t)xcd_remap(blockIdx.x, gridDim.x));
+  if (it.c0 >= it.c1) return;
+  const int32_t j0 = 4 * it.c0 / g.blocks, j1 = min(it.pages, (4 * it.c1 + g.blocks - 1) / g.blocks);
+  for (int32_t j = j0 + (int32_t)threadIdx.x; j < j1; j += 64 * FA_NW) {
+    const int32_t s = !g.joined ? it.first + j : j < list.shared ? j : it.first + j - list.shared;
+    base[j - j0] = (uint64_t)list.slot[s] * g.slot_bytes + (uint64_t)it.head * g.blocks * kFp4Block;
+  }
+  Fp4Rows rows[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    rows[r] = load_rows(q + ((size_t)(it.row0 + min(16 * r + (lane & 15), it.rows - 1)) * g.heads + it.head) * 128, lane >> 4, g.q_flip);
   __syncthreads();
-  const int32_t own = list.off[node], pages = list.shared + list.off[node + 1] - own;
-  float m = -INFINITY, sum = 0.f, acc[2] = {0.f, 0.f};
-  const int32_t t = lane & 31, half = lane >> 5;
-  for (int32_t j = 0; j < pages; ++j) {
-    const char* page = g.layer_base + (uint64_t)list.slot[j < list.shared ? j : own + j - list.shared] * g.slot_bytes +
-                       (uint64_t)h * g.blocks * kFp4Block;
-    for (int32_t b = 0; b < g.blocks; ++b) {
-      const uint8_t* blk = reinterpret_cast<const uint8_t*>(page) + (uint64_t)b * kFp4Block;
-      float s = 0.f;
-      for (int32_t c = 64 * half; c < 64 * half + 64; c += 32) {
-        float d = 0.f;
-        for (int32_t e = 0; e < 32; ++e) d += qs[c + e] * fp4_value(blk[t * 64 + (c + e) / 2] >> (4 * (e & 1)));
-        s += d * fp4_power(blk[kFp4KScale + (t >> 4) * 64 + (t & 3) * 16 + (c >> 5) * 4 + (t >> 2 & 3)]);
+  const auto block_at = [&](int32_t b) {
+    b = min(b, it.blocks - 1);
+    const int32_t j = (int32_t)fast_div((uint32_t)b, g.blocks_div);
+    return g.layer_base + base[j - j0] + (uint32_t)(b - j * g.blocks) * kFp4Block;
+  };
+  const auto tokens_of = [&](int32_t b) {  // keys of a block
+    const int32_t j = (int32_t)fast_div((uint32_t)min(b, it.blocks - 1), g.blocks_div);
+    return b < it.blocks ? g.tpp - (b - j * g.blocks) * kFp4Tokens : 0;
+  };
+  // K rows: row 4 x + i of product b is token 16 (x % 2) + 4 (b % 4) + i of the chunk's block
+  // 2 (b / 4) + x / 2, so that the rows a lane gets of S^T (x = lane / 16) are the columns it
+  // has to give of P^T
+  const uint32_t k_at = (16 * (lane >> 2 & 1) + (lane & 3)) * 64 + (lane >> 4) * 16;
+  const uint32_t ks_at = kFp4KScale + (lane >> 2 & 1) * 64 + (lane & 3) * 16 + (lane >> 4) * 4;
+  const uint32_t v_at = kFp4V + (lane & 15) * 16, vs_at = kFp4VScale + (lane & 15) * 8;
+  const bool ragged = (g.tpp & 31) != 0 || (it.blocks & 3) != 0;
+
+  f32x4 acc[R][8];
+  float m[R], sum[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    m[r] = -INFINITY;
+    sum[r] = 0.f;
+#pragma unroll
+    for (int n = 0; n < 8; ++n) acc[r][n] = f32x4{};
+  }
+  u32x4 k[8];
+  uint32_t ks[2];
+  const auto load_k = [&](int32_t c) __attribute__((always_inline)) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const char* p = block_at(4 * c + 2 * h + (lane >> 3 & 1));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) k[4 * h + i] = *reinterpret_cast<const u32x4*>(p + k_at + 256 * i);
+      ks[h] = *reinterpret_cast<const uint32_t*>(p + ks_at);
+    }
+  };
+  if (it.c0 + wave < it.c1) load_k(it.c0 + wave);
+  for (int32_t c = it.c0 + wave; c < it.c1; c += FA_NW) {
+    u32x4 v[8];
+    const char* vp = block_at(4 * c + (lane >> 4));
+#pragma unroll
+    for (int n = 0; n < 8; ++n) v[n] = *reinterpret_cast<const u32x4*>(vp + v_at + 256 * n);
+    const u32x2 vs = *reinterpret_cast<const u32x2*>(vp + vs_at);
+    int32_t left[2];
+    if (ragged) {
+      left[0] = tokens_of(4 * c + (lane >> 5)) - 16 * (lane >> 4 & 1);
+      left[1] = tokens_of(4 * c + 2 + (lane >> 5)) - 16 * (lane >> 4 & 1);
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      f32x4 s[8];
+      const f32x4 zero = {};
+#define SC_QK(b) s[b] = mx<(b) & 3>(k[b], rows[r].lo, mx<(b) & 3>(k[b], rows[r].hi, zero, ks[(b) >> 2], rows[r].s_hi), ks[(b) >> 2], rows[r].s_lo)
+      SC_QK(0); SC_QK(1); SC_QK(2); SC_QK(3); SC_QK(4); SC_QK(5); SC_QK(6); SC_QK(7);
+#undef SC_QK
+      if (r == R - 1 && c + FA_NW < it.c1) load_k(c + FA_NW);
+      if (ragged) {
+#pragma unroll
+        for (int b = 0; b < 8; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (4 * (b & 3) + i >= left[b >> 2]) s[b][i] = -INFINITY;
       }
-      s = (s + __shfl_xor(s, 32)) * g.scale_log2;
-      if (t >= g.tpp - b * kFp4Tokens) s = -INFINITY;
-      float top = s;
-      for (int x = 1; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
-      const float to = fmaxf(m, top), keep = m == to ? 1.f : exp2f(m - to);
-      const float p = s == -INFINITY && t >= g.tpp - b * kFp4Tokens ? 0.f : exp2f(s - to);
-      m = to;
-      float all = p;
-      for (int x = 1; x < 32; x <<= 1) all += __shfl_xor(all, x);
-      sum = sum * keep + all;
-      __syncthreads();
-      if (half == 0) ps[t] = p;
-      __syncthreads();
-      for (int i = 0; i < 2; ++i) {
-        const int32_t c = 2 * lane + i;
-        float d = 0.f;
-        for (int32_t e = 0; e < 32; ++e) d += ps[e] * fp4_value(blk[kFp4V + c * 16 + e / 2] >> (4 * (e & 1)));
-        acc[i] = acc[i] * keep + d * fp4_power(blk[kFp4VScale + (c & 15) * 8 + (c >> 4)]);
+      float top = s[0][0];
+#pragma unroll
+      for (int b = 0; b < 8; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, s[b][i]);
+      // exponentials are relative to a power of two no less than the chunk's largest, 2^8
+      // of it: a row's power is then a change of the scale alone
+      const float e = fmaxf(ceilf(quarters_max(top) * g.unit), -1e30f), shift = 8.f - e;
+      const float to = fmaxf(m[r], e);
+      if (__any(to > m[r])) {
+        const float keep = __builtin_amdgcn_exp2f(m[r] - to);
+        sum[r] *= keep;
+#pragma unroll
+        for (int n = 0; n < 8; ++n) acc[r][n] *= keep;
+        m[r] = to;
+      }
+      const int32_t d = (int32_t)fmaxf(e - to, -300.f);
+      const uint32_t s_hi = (uint32_t)max(d + 119, 0), s_lo = (uint32_t)max(d + 115, 0);
+      i32x8 hi, lo;
+      float all = 0.f;
+#pragma unroll
+      for (int b = 0; b < 8; ++b) {
+        float p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          p[i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], g.unit, shift));
+          all += p[i];
+        }
+        int h, l;
+        split_e4m3(p[0], p[1], p[2], p[3], 16.f, h, l);
+        hi[b] = h;
+        lo[b] = l;
+      }
+      sum[r] += ldexpf(all, d - 8);
+#define SC_PV(n) acc[r][n] = mx<(n) & 3>(v[n], lo, mx<(n) & 3>(v[n], hi, acc[r][n], vs[(n) >> 2], s_hi), vs[(n) >> 2], s_lo)
+      SC_PV(0); SC_PV(1); SC_PV(2); SC_PV(3); SC_PV(4); SC_PV(5); SC_PV(6); SC_PV(7);
+#undef SC_PV
+    }
+  }
+  // the waves' parts of 16 rows at a time: thread t has eight channels of row t / 16
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    if (16 * r >= it.rows) break;
+    if (r) __syncthreads();
+    const float all = quarters_sum(sum[r]);
+#pragma unroll
+    for (int n = 0; n < 8; ++n)
+      *reinterpret_cast<f32x4*>(&part[wave][(lane & 15) * FA_ROW + 16 * n + 4 * (lane >> 4)]) = acc[r][n];
+    if (lane < 16) {
+      ml[wave][0][lane] = m[r];
+      ml[wave][1][lane] = all;
+    }
+    __syncthreads();
+    const int32_t x = threadIdx.x >> 4, ch = 8 * (threadIdx.x & 15), row = it.row0 + 16 * r + x;
+    if (16 * r + x < it.rows) {
+      float to = ml[0][0][x];
+#pragma unroll
+      for (int w = 1; w < FA_NW; ++w) to = fmaxf(to, ml[w][0][x]);
+      f32x4 y[2] = {};
+      float l = 0.f;
+#pragma unroll
+      for (int w = 0; w < FA_NW; ++w) {
+        const float keep = exp2f(ml[w][0][x] - to);
+        l += keep * ml[w][1][x];
+        y[0] += keep * *reinterpret_cast<const f32x4*>(&part[w][x * FA_ROW + ch]);
+        y[1] += keep * *reinterpret_cast<const f32x4*>(&part[w][x * FA_ROW + ch + 4]);
+      }
+      if (g.part_o) {
+        const size_t at = ((size_t)it.slot * g.heads + it.head) * g.rows + row;
+        *reinterpret_cast<f32x4*>(g.part_o + at * 128 + ch) = y[0];
+        *reinterpret_cast<f32x4*>(g.part_o + at * 128 + ch + 4) = y[1];
+        if (ch == 0) {
+          g.part_ml[2 * at] = to;
+          g.part_ml[2 * at + 1] = l;
+        }
+      } else {
+        const float by = 1.f / l;
+        u32x4 z;
+        z[0] = pack_bf16x2(y[0][0] * by, y[0][1] * by);
+        z[1] = pack_bf16x2(y[0][2] * by, y[0][3] * by);
+        z[2] = pack_bf16x2(y[1][0] * by, y[1][1] * by);
+        z[3] = pack_bf16x2(y[1][2] * by, y[1][3] * by);
+        *reinterpret_cast<u32x4u*>(o + ((size_t)row * g.heads + it.head) * 128 + ch) = z;
       }
     }
   }
-  *reinterpret_cast<uint32_t*>(o + ((size_t)row * g.heads + h) * 128 + 2 * lane) = pack_bf16x2(acc[0] / sum, acc[1] / sum);
 }
 
-size_t fp4_attention_workspace_bytes(const sc_plan*, const sc_cache*) { return 0; }
+// A wave per row and head joins the pieces that its node has: the prefix's and its own.
+__global__ __launch_bounds__(256) void fp4_combine_kernel(uint16_t* __restrict__ o, Fp4Geom g, Fp4List list) {
+  const int32_t lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6), h = blockIdx.y;
+  if (row >= g.rows) return;
+  const int32_t node = (int32_t)fast_div((uint32_t)row, g.nq_div);
+  const int32_t blocks = (list.off[node + 1] - list.off[node] + (g.joined ? list.shared : 0)) * g.blocks;
+  const int32_t pieces = g.p_pieces + ((blocks + 3) / 4 + g.o_len - 1) / g.o_len;
+  const size_t step = (size_t)g.heads * g.rows, at = (size_t)h * g.rows + row;
+  float m = -INFINITY, l = 0.f, y[2] = {0.f, 0.f};
+  for (int32_t p = 0; p < pieces; ++p) {
+    const size_t i = p * step + at;
+    const f32x2 ml = *reinterpret_cast<const f32x2*>(g.part_ml + 2 * i);
+    const f32x2 x = *reinterpret_cast<const f32x2*>(g.part_o + i * 128 + 2 * lane);
+    const float to = fmaxf(m, ml[0]), keep = exp2f(m - to), by = exp2f(ml[0] - to);
+    m = to;
+    l = l * keep + ml[1] * by;
+    y[0] = y[0] * keep + x[0] * by;
+    y[1] = y[1] * keep + x[1] * by;
+  }
+  const float by = 1.f / l;
+  *reinterpret_cast<uint32_t*>(o + ((size_t)row * g.heads + h) * 128 + 2 * lane) = pack_bf16x2(y[0] * by, y[1] * by);
+}
+
+struct Fp4Schedule {
+  size_t room;
+  int32_t tile;      // rows of an item: 16, 32 or 64
+  int32_t joined, p_len, p_pieces, o_len, o_pieces;  // chunks of a piece, pieces (own: the most of a node)
+  size_t bytes;
+};
+
+static int64_t fp4_chunks(const sc_cache* c, int64_t pages) {
+  return (pages * fp4_blocks(c->d.tokens_per_page) + 3) / 4;
+}
+
+static Fp4Schedule find_fp4_schedule(const sc_plan* p, const sc_cache* c, size_t room) {
+  const int32_t n = (int32_t)p->nodes.size(), H = c->d.n_heads;
+  const int64_t rows = (int64_t)n * p->nq;
+  int64_t own_max = 0;
+  for (int32_t i = 0; i < n; ++i) own_max = std::max<int64_t>(own_max, p->page_off[i + 1] - p->page_off[i] - p->shared);
+  Fp4Schedule s{};
+  s.room = room;
+  const int64_t piece = rows * H * (128 + 2) * (int64_t)sizeof(float);
+  const int64_t most = piece ? std::min<int64_t>(room / piece, 1024) : 0;  // pieces that fit
+  const int64_t pc = fp4_chunks(c, p->shared), oc = fp4_chunks(c, own_max);
+  s.joined = p->shared == 0 || most < 2;
+  const int64_t tile_rows = s.joined ? p->nq : rows;
+  s.tile = tile_rows <= 16 ? 16 : 32;
+  if (const char* e = getenv("FP4_TILE")) s.tile = atoi(e);
+  const int64_t want = getenv("FP4_ITEMS") ? atoi(getenv("FP4_ITEMS")) : 512;
+  const int64_t ou = (int64_t)H * n * ((p->nq + s.tile - 1) / s.tile), pu = (int64_t)H * ((rows + s.tile - 1) / s.tile);
+  const int64_t len_min = getenv("FP4_MIN") ? atoi(getenv("FP4_MIN")) : 4;
+  if (s.joined) {
+    const int64_t all = fp4_chunks(c, own_max + p->shared);
+    int64_t pieces = std::max<int64_t>(1, std::min({want / ou, all / len_min, most}));
+    s.o_len = (int32_t)((all + pieces - 1) / pieces);
+    s.o_pieces = (int32_t)((all + s.o_len - 1) / s.o_len);
+    s.bytes = s.o_pieces > 1 ? (size_t)s.o_pieces * piece : 0;
+  } else {
+    const int64_t work = pc * pu + oc * ou;
+    int64_t len = std::max<int64_t>(len_min, work / want);
+    for (;; len += len / 8 + 1) {
+      s.p_len = (int32_t)std::min(len, pc);
+      s.o_len = (int32_t)std::min(len, oc);
+      s.p_pieces = (int32_t)((pc + s.p_len - 1) / s.p_len);
+      s.o_pieces = (int32_t)((oc + s.o_len - 1) / s.o_len);
+      if (s.p_pieces + s.o_pieces <= most) break;
+    }
+    s.bytes = (size_t)(s.p_pieces + s.o_pieces) * piece;
+  }
+  return s;
+}
+
+static const Fp4Schedule& fp4_schedule(const sc_plan* p, const sc_cache* c, size_t room) {
+  for (const auto& s : p->fp4)
+    if (s->room == room) return *s;
+  p->fp4.push_back(std::make_shared<Fp4Schedule>(find_fp4_schedule(p, c, room)));
+  return *p->fp4.back();
+}
+
+size_t fp4_attention_workspace_bytes(const sc_plan* p, const sc_cache* c) { return fp4_schedule(p, c, SIZE_MAX).bytes; }
+
+template <int R>
+static void launch_fp4_tiles(uint32_t items, const uint16_t* q, uint16_t* o, const Fp4Geom& g, const Fp4List& l, hipStream_t stream) {
+  hipLaunchKernelGGL(fp4_attention_kernel<R>, dim3(items), dim3(64 * FA_NW), 0, stream, q, o, g, l);
+}
 
 int launch_fp4_attention(const sc_plan* p, const sc_cache* c, int32_t layer, const void* q, void* o, float scale,
                          void* ws, size_t room, hipStream_t stream) {
   if (!std::isfinite(scale)) return fail(SC_EINVAL, "scale must be finite");
+  if (reinterpret_cast<uintptr_t>(q) & 15) return fail(SC_EINVAL, "q must be 16-byte aligned");
+  if (reinterpret_cast<uintptr_t>(ws) & 15) return fail(SC_EINVAL, "workspace must be 16-byte aligned");
   const int64_t rows = (int64_t)p->nodes.size() * p->nq;
   if (rows > INT32_MAX) return fail(SC_EUNSUPPORTED, "%lld query rows", (long long)rows);
+  const Fp4Schedule* s = &fp4_schedule(p, c, SIZE_MAX);
+  if (s->bytes > room) s = &fp4_schedule(p, c, room);
   Fp4List l;
   Fp4Geom g;
   fp4_fill(p, c, layer, scale, l, g);
+  g.joined = s->joined;
+  g.o_tiles = (p->nq + s->tile - 1) / s->tile;
+  g.o_len = s->o_len;
+  if (!s->joined) {
+    g.p_tiles = (g.rows + s->tile - 1) / s->tile;
+    g.p_pieces = s->p_pieces;
+    g.p_len = s->p_len;
+    g.p_items = g.p_tiles * g.heads * g.p_pieces;
+  }
+  const int64_t items = (int64_t)g.p_items + (int64_t)g.o_tiles * g.heads * g.nodes * s->o_pieces;
+  if (items > INT32_MAX) return fail(SC_EUNSUPPORTED, "%lld query tiles", (long long)items);
+  if (s->bytes) {
+    g.part_o = static_cast<float*>(ws);
+    g.part_ml = g.part_o + (size_t)(g.p_pieces + s->o_pieces) * g.heads * g.rows * 128;
+  }
+  const uint16_t* qb = static_cast<const uint16_t*>(q);
+  uint16_t* ob = static_cast<uint16_t*>(o);
   timer_begin(TK_ATTENTION, stream);
-  hipLaunchKernelGGL(fp4_attention_plain_kernel, dim3((uint32_t)rows, (uint32_t)g.heads), dim3(64), 0, stream,
-                     static_cast<const uint16_t*>(q), static_cast<uint16_t*>(o), g, l);
+  if (s->tile == 16)
+    launch_fp4_tiles<1>((uint32_t)items, qb, ob, g, l, stream);
+  else
+    launch_fp4_tiles<2>((uint32_t)items, qb, ob, g, l, stream);
   timer_end(TK_ATTENTION, stream);
+  if (s->bytes) {
+    timer_begin(TK_ATTN_COMBINE, stream);
+    hipLaunchKernelGGL(fp4_combine_kernel, dim3((uint32_t)(g.rows + 3) / 4, (uint32_t)g.heads), dim3(256), 0, stream, ob, g, l);
+    timer_end(TK_ATTN_COMBINE, stream);
+  }
   SC_HIP(hipGetLastError());
   return SC_OK;
 }
 
-int fp4_attention_form(const sc_plan*, const sc_cache*, int32_t* queries, int32_t* ring, int32_t* pieces) {
-  *queries = *ring = *pieces = 1;
+int fp4_attention_form(const sc_plan* p, const sc_cache* c, int32_t* queries, int32_t* ring, int32_t* pieces) {
+  const Fp4Schedule& s = fp4_schedule(p, c, SIZE_MAX);
+  *queries = s.tile;
+  *ring = 1;
+  *pieces = s.joined ? s.o_pieces : -s.p_pieces;
   return SC_OK;
 }
 
