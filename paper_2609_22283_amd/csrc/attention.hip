@@ -638,6 +638,20 @@ int launch_attention_lse(const sc_plan* p, const sc_cache* c, int32_t layer, con
   return launch_scheduled(p, c, layer, q, o, false, nullptr, scale, ws, ts, stream);
 }
 
+// A bf16 plan on the forms whose logits are products of q as it is, whether or not its nodes
+// share a prefix.
+double attention_exact_us(const sc_plan* p, const sc_cache* c) {
+  return share_schedule(p, c, attention_workspace_bound(), false).us;
+}
+size_t attention_exact_workspace_bytes(const sc_plan* p, const sc_cache* c) { return share_workspace_bytes(p, c, false); }
+int launch_attention_exact(const sc_plan* p, const sc_cache* c, int32_t layer, const void* q, void* o, float scale,
+                           void* ws, hipStream_t stream) {
+  const int rc = attention_check(p, c);
+  if (rc != SC_OK) return rc;
+  return launch_share(p, c, layer, q, o, nullptr, scale, ws, share_schedule(p, c, attention_workspace_bound(), false),
+                      nullptr, stream);
+}
+
 int launch_attention(const sc_plan* p, const sc_cache* c, int32_t layer, const void* q, void* o,
                      float scale, void* ws, size_t ws_bytes, hipStream_t stream) {
   if (const Weighing* w = Weighing::current; w && w->plan == p)

@@ -8,6 +8,8 @@
 #include <cmath>
 #include <cstdlib>
 #include <cstring>
+#include <map>
+#include <new>
 
 #include "fp4.h"
 
@@ -34,6 +36,8 @@ struct Fp4Geom {
   int32_t joined, p_items, p_tiles, p_pieces, p_len, o_tiles, o_len;
   float *part_o, *part_ml;  // [piece][head][row][128], [piece][head][row][2], or NULL: one piece
 };
+
+static size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
 
 static void fp4_fill(const sc_plan* p, const sc_cache* c, int32_t layer, float scale, Fp4List& l, Fp4Geom& g) {
   const sc_cache_desc& d = c->d;
@@ -67,47 +71,50 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef short i16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int FA_NW = 4;      // waves of a work-group
+constexpr float kFp4Rise = 40.f;  // sums of 2^31 keys in units of 2^m stay below 2^(40 + 31)
 constexpr int FA_ROW = 132;   // floats of a row of partial outputs in LDS
 
 // c + A B over 128: A 16 rows of codes (a lane: row lane % 16, the 32 columns of group lane / 16)
 // whose scales are byte SA of the lanes' sa, B 16 columns of e4m3 (a lane: column lane % 16, rows 16 g ..
-// + 15 and 64 + 16 g .. + 15 with g = lane / 16), scaled by 2^(sb - 127).
+// + 15 and 64 + 16 g .. + 15 with g = lane / 16), in two parts with their scales in the first two
+// bytes of sb.
 template <int SA>
-__device__ __forceinline__ f32x4 mx(const u32x4& a, const i32x8& b, const f32x4& c, uint32_t sa, uint32_t sb) {
+__device__ __forceinline__ f32x4 mx(const u32x4& a, const i32x8& hi, const i32x8& lo, const f32x4& c, uint32_t sa, uint32_t sb) {
   const i32x8 a8 = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b, c, 4, 0, SA, (int)sa, 0, (int)sb);
+  const f32x4 d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, hi, c, 4, 0, SA, (int)sa, 0, (int)sb);
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, lo, d, 4, 0, SA, (int)sa, 1, (int)sb);
 }
 
-// The larger (or the sum) of the values of lanes l, l ^ 16, l ^ 32, l ^ 48.
+__device__ __forceinline__ i32x8 join(const u32x4& a, const u32x4& b) {
+  return i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
+}
+
+// The largest of the values of lanes l, l ^ 16, l ^ 32, l ^ 48.
 __device__ __forceinline__ float quarters_max(float x) {
   u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false));
   x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
   r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
-__device__ __forceinline__ float quarters_sum(float x) {
-  u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false));
-  x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-  r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
-// Four fp32 numbers of at most 448 as e4m3, and what that leaves of them, times `up`, in
-// e4m3 again: 8 significant bits together, which is all that bf16 has.
-__device__ __forceinline__ void split_e4m3(float a, float b, float c, float d, float up, int& hi, int& lo) {
-  int h = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+// Four fp32 numbers of at most 448 as e4m3, and what that leaves of them, over `unit` (a power of
+// two), in e4m3 again: 8 significant bits together, which is all that bf16 has.
+// x, y: any two values that are not needed any more (the conversions write half a register at
+// a time, and would have one cleared first).
+__device__ __forceinline__ void split_e4m3(float a, float b, float c, float d, float unit, float x, float y, int& hi, int& lo) {
+  int h = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, (int)__float_as_uint(x), false);
   h = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, h, true);
   const f32x2 ab = __builtin_amdgcn_cvt_pk_f32_fp8(h, false), cd = __builtin_amdgcn_cvt_pk_f32_fp8(h, true);
-  int l = __builtin_amdgcn_cvt_pk_fp8_f32((a - ab[0]) * up, (b - ab[1]) * up, 0, false);
-  l = __builtin_amdgcn_cvt_pk_fp8_f32((c - cd[0]) * up, (d - cd[1]) * up, l, true);
+  i16x2 l = __builtin_bit_cast(i16x2, y);
+  l = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l, a - ab[0], b - ab[1], unit, false);
+  l = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l, c - cd[0], d - cd[1], unit, true);
   hi = h;
-  lo = l;
+  lo = __builtin_bit_cast(int, l);
 }
 
 // 16 query rows as the B operand, in two parts with a scale each.
 struct Fp4Rows {
   i32x8 hi, lo;
-  uint32_t s_hi, s_lo;
+  uint32_t scale;  // of hi, of lo << 8
 };
 __device__ __forceinline__ Fp4Rows load_rows(const uint16_t* row, int32_t quarter, uint32_t flip) {
   u32x4 v[4];
@@ -126,15 +133,15 @@ __device__ __forceinline__ Fp4Rows load_rows(const uint16_t* row, int32_t quarte
   const uint32_t e = top >> 23, s = e > 7u ? e - 7u : 0u;  // the largest becomes 2^7 .. 2^8
   const float by = __uint_as_float((e > 7u ? 261u - e : 254u) << 23);
   Fp4Rows r;
-  r.s_hi = e == 255u ? 255u : s;
-  r.s_lo = s > 4u ? s - 4u : 0u;
-  const float up = __uint_as_float((127u + s - r.s_lo) << 23);
+  const uint32_t s_lo = s > 4u ? s - 4u : 0u;
+  r.scale = (e == 255u ? 255u : s) | s_lo << 8;
+  const float unit = __uint_as_float((127u + s_lo - s) << 23);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const uint32_t a = v[i >> 1][2 * (i & 1)], b = v[i >> 1][2 * (i & 1) + 1];
     int h, l;
     split_e4m3(__uint_as_float(a << 16) * by, __uint_as_float(a & 0xffff0000u) * by, __uint_as_float(b << 16) * by,
-               __uint_as_float(b & 0xffff0000u) * by, up, h, l);
+               __uint_as_float(b & 0xffff0000u) * by, unit, 0.f, 0.f, h, l);
     r.hi[i] = e == 255u ? 0 : h;
     r.lo[i] = e == 255u ? 0 : l;
   }
@@ -170,11 +177,13 @@ __device__ __forceinline__ Fp4Item fp4_item(const Fp4Geom& g, const Fp4List& lis
 }
 
 template <int R>
-__global__ __launch_bounds__(64 * FA_NW, 2) void fp4_attention_kernel(const uint16_t* __restrict__ q, uint16_t* __restrict__ o,
+__global__ __launch_bounds__(64 * FA_NW, R == 1 ? 3 : 2) void fp4_attention_kernel(const uint16_t* __restrict__ q, uint16_t* __restrict__ o,
                                                                       Fp4Geom g, Fp4List list) {
   __shared__ __attribute__((aligned(16))) float part[FA_NW][16 * FA_ROW];
   __shared__ float ml[FA_NW][2][16];
   __shared__ uint64_t base[kFp4Pages];
+  __shared__ u32x4 qs[R][4][64];         // the queries' operands: halves of hi, halves of lo
+  __shared__ uint32_t q_scale[R][16];
   const int32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const Fp4Item it = fp4_item<R>(g, list, (int32_t)xcd_remap(blockIdx.x, gridDim.x));
   if (it.c0 >= it.c1) return;
@@ -183,10 +192,16 @@ __global__ __launch_bounds__(64 * FA_NW, 2) void fp4_attention_kernel(const uint
     const int32_t s = !g.joined ? it.first + j : j < list.shared ? j : it.first + j - list.shared;
     base[j - j0] = (uint64_t)list.slot[s] * g.slot_bytes + (uint64_t)it.head * g.blocks * kFp4Block;
   }
-  Fp4Rows rows[R];
+  if (wave < R) {
+    const Fp4Rows x = load_rows(q + ((size_t)(it.row0 + min(16 * wave + (lane & 15), it.rows - 1)) * g.heads + it.head) * 128,
+                                lane >> 4, g.q_flip);
 #pragma unroll
-  for (int r = 0; r < R; ++r)
-    rows[r] = load_rows(q + ((size_t)(it.row0 + min(16 * r + (lane & 15), it.rows - 1)) * g.heads + it.head) * 128, lane >> 4, g.q_flip);
+    for (int i = 0; i < 2; ++i) {
+      qs[wave][i][lane] = u32x4{(uint32_t)x.hi[4 * i], (uint32_t)x.hi[4 * i + 1], (uint32_t)x.hi[4 * i + 2], (uint32_t)x.hi[4 * i + 3]};
+      qs[wave][2 + i][lane] = u32x4{(uint32_t)x.lo[4 * i], (uint32_t)x.lo[4 * i + 1], (uint32_t)x.lo[4 * i + 2], (uint32_t)x.lo[4 * i + 3]};
+    }
+    if (lane < 16) q_scale[wave][lane] = x.scale;
+  }
   __syncthreads();
   const auto block_at = [&](int32_t b) {
     b = min(b, it.blocks - 1);
@@ -205,15 +220,18 @@ __global__ __launch_bounds__(64 * FA_NW, 2) void fp4_attention_kernel(const uint
   const uint32_t v_at = kFp4V + (lane & 15) * 16, vs_at = kFp4VScale + (lane & 15) * 8;
   const bool ragged = (g.tpp & 31) != 0 || (it.blocks & 3) != 0;
 
-  f32x4 acc[R][8];
-  float m[R], sum[R];
+  f32x4 acc[R][8], sum[R];  // sum: of a row's exponentials, as they enter the products
+  float m[R];
+  uint32_t qsc[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     m[r] = -INFINITY;
-    sum[r] = 0.f;
+    sum[r] = f32x4{};
+    qsc[r] = q_scale[r][lane & 15];
 #pragma unroll
     for (int n = 0; n < 8; ++n) acc[r][n] = f32x4{};
   }
+  const u32x4 ones = {0x22222222u, 0x22222222u, 0x22222222u, 0x22222222u};
   u32x4 k[8];
   uint32_t ks[2];
   const auto load_k = [&](int32_t c) __attribute__((always_inline)) {
@@ -227,25 +245,36 @@ __global__ __launch_bounds__(64 * FA_NW, 2) void fp4_attention_kernel(const uint
   };
   if (it.c0 + wave < it.c1) load_k(it.c0 + wave);
   for (int32_t c = it.c0 + wave; c < it.c1; c += FA_NW) {
-    u32x4 v[8];
-    const char* vp = block_at(4 * c + (lane >> 4));
-#pragma unroll
-    for (int n = 0; n < 8; ++n) v[n] = *reinterpret_cast<const u32x4*>(vp + v_at + 256 * n);
-    const u32x2 vs = *reinterpret_cast<const u32x2*>(vp + vs_at);
+    bool cut = false;  // a block of the chunk ends early, or is not there
     int32_t left[2];
     if (ragged) {
       left[0] = tokens_of(4 * c + (lane >> 5)) - 16 * (lane >> 4 & 1);
       left[1] = tokens_of(4 * c + 2 + (lane >> 5)) - 16 * (lane >> 4 & 1);
+      cut = __any(min(left[0], left[1]) < 16);
     }
+    i32x8 hi[R], lo[R];
+    uint32_t psc[R];
+    u32x4 v[8];
+    u32x2 vs;
+    const auto load_v = [&]() __attribute__((always_inline)) {
+      const char* vp = block_at(4 * c + (lane >> 4));
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      f32x4 s[8];
+      for (int n = 0; n < 8; ++n) v[n] = *reinterpret_cast<const u32x4*>(vp + v_at + 256 * n);
+      vs = *reinterpret_cast<const u32x2*>(vp + vs_at);
+    };
+    const auto logits = [&](int r, f32x4 (&s)[8]) __attribute__((always_inline)) {
       const f32x4 zero = {};
-#define SC_QK(b) s[b] = mx<(b) & 3>(k[b], rows[r].lo, mx<(b) & 3>(k[b], rows[r].hi, zero, ks[(b) >> 2], rows[r].s_hi), ks[(b) >> 2], rows[r].s_lo)
+      const i32x8 q_hi = join(qs[r][0][lane], qs[r][1][lane]), q_lo = join(qs[r][2][lane], qs[r][3][lane]);
+#define SC_QK(b) s[b] = mx<(b) & 3>(k[b], q_hi, q_lo, zero, ks[(b) >> 2], qsc[r])
       SC_QK(0); SC_QK(1); SC_QK(2); SC_QK(3); SC_QK(4); SC_QK(5); SC_QK(6); SC_QK(7);
 #undef SC_QK
-      if (r == R - 1 && c + FA_NW < it.c1) load_k(c + FA_NW);
-      if (ragged) {
+    };
+    // what the exponentials of a chunk are relative to: a power of two no less than its
+    // largest, 2^8 of it, which is a change of the scale of P alone.  The row's sums are
+    // in units of 2^m, m the first chunk's power until one is far above it (were m to follow
+    // every rise, some row of 16 would have its sums multiplied in most chunks).
+    const auto shift_of = [&](int r, f32x4 (&s)[8]) __attribute__((always_inline)) {
+      if (cut) {
 #pragma unroll
         for (int b = 0; b < 8; ++b)
 #pragma unroll
@@ -257,38 +286,77 @@ __global__ __launch_bounds__(64 * FA_NW, 2) void fp4_attention_kernel(const uint
       for (int b = 0; b < 8; ++b)
 #pragma unroll
         for (int i = 0; i < 4; ++i) top = fmaxf(top, s[b][i]);
-      // exponentials are relative to a power of two no less than the chunk's largest, 2^8
-      // of it: a row's power is then a change of the scale alone
-      const float e = fmaxf(ceilf(quarters_max(top) * g.unit), -1e30f), shift = 8.f - e;
-      const float to = fmaxf(m[r], e);
-      if (__any(to > m[r])) {
-        const float keep = __builtin_amdgcn_exp2f(m[r] - to);
+      const float e = fmaxf(ceilf(quarters_max(top) * g.unit), -1e30f);
+      if (__any(e > m[r] + kFp4Rise)) {
+        const float to = fmaxf(m[r], e), keep = __builtin_amdgcn_exp2f(m[r] - to);
         sum[r] *= keep;
 #pragma unroll
         for (int n = 0; n < 8; ++n) acc[r][n] *= keep;
         m[r] = to;
       }
-      const int32_t d = (int32_t)fmaxf(e - to, -300.f);
-      const uint32_t s_hi = (uint32_t)max(d + 119, 0), s_lo = (uint32_t)max(d + 115, 0);
-      i32x8 hi, lo;
-      float all = 0.f;
+      const int32_t d = (int32_t)fminf(fmaxf(e - m[r], -300.f), 100.f);
+      psc[r] = (uint32_t)max(d + 119, 0) | (uint32_t)max(d + 115, 0) << 8;
+      return 8.f - e;
+    };
+    const auto exponentials = [&](int r, f32x4 (&s)[8], float shift) __attribute__((always_inline)) {
 #pragma unroll
       for (int b = 0; b < 8; ++b) {
         float p[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          p[i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], g.unit, shift));
-          all += p[i];
-        }
+        for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], g.unit, shift));
         int h, l;
-        split_e4m3(p[0], p[1], p[2], p[3], 16.f, h, l);
-        hi[b] = h;
-        lo[b] = l;
+        split_e4m3(p[0], p[1], p[2], p[3], 0.0625f, s[b][0], s[b][1], h, l);
+        asm volatile("" : "+v"(h), "+v"(l));  // here, and not where the products need them
+        hi[r][b] = h;
+        lo[r][b] = l;
       }
-      sum[r] += ldexpf(all, d - 8);
-#define SC_PV(n) acc[r][n] = mx<(n) & 3>(v[n], lo, mx<(n) & 3>(v[n], hi, acc[r][n], vs[(n) >> 2], s_hi), vs[(n) >> 2], s_lo)
+    };
+    const auto products = [&](int r) __attribute__((always_inline)) {
+#define SC_PV(n) acc[r][n] = mx<(n) & 3>(v[n], hi[r], lo[r], acc[r][n], vs[(n) >> 2], psc[r])
       SC_PV(0); SC_PV(1); SC_PV(2); SC_PV(3); SC_PV(4); SC_PV(5); SC_PV(6); SC_PV(7);
 #undef SC_PV
+      sum[r] = mx<0>(ones, hi[r], lo[r], sum[r], 0x7f7f7f7fu, psc[r]);
+    };
+    const int32_t next = c + FA_NW < it.c1 ? c + FA_NW : c;  // at the end the same again: no branch
+    f32x4 s0[8];
+    logits(0, s0);
+    if constexpr (R == 1) {
+      __builtin_amdgcn_sched_barrier(0);  // V takes the registers of K, whose last product this was
+      load_v();
+      exponentials(0, s0, shift_of(0, s0));
+      __builtin_amdgcn_sched_barrier(0);
+      load_k(next);
+      __builtin_amdgcn_sched_barrier(0);
+      products(0);
+    } else {
+      // the products of one half of the rows run under the exponentials of the other
+      f32x4 s1[8];
+      float shift = shift_of(0, s0);
+      __builtin_amdgcn_sched_barrier(0);
+      logits(1, s1);
+      exponentials(0, s0, shift);
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 10, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      load_v();
+      shift = shift_of(1, s1);
+      __builtin_amdgcn_sched_barrier(0);
+      load_k(next);
+      exponentials(1, s1, shift);
+      products(0);
+      __builtin_amdgcn_sched_group_barrier(0x020, 10, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 40, 0);
+#pragma unroll
+      for (int i = 0; i < 18; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 8, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      products(1);
     }
   }
   // the waves' parts of 16 rows at a time: thread t has eight channels of row t / 16
@@ -296,13 +364,12 @@ __global__ __launch_bounds__(64 * FA_NW, 2) void fp4_attention_kernel(const uint
   for (int r = 0; r < R; ++r) {
     if (16 * r >= it.rows) break;
     if (r) __syncthreads();
-    const float all = quarters_sum(sum[r]);
 #pragma unroll
     for (int n = 0; n < 8; ++n)
       *reinterpret_cast<f32x4*>(&part[wave][(lane & 15) * FA_ROW + 16 * n + 4 * (lane >> 4)]) = acc[r][n];
     if (lane < 16) {
       ml[wave][0][lane] = m[r];
-      ml[wave][1][lane] = all;
+      ml[wave][1][lane] = sum[r][0];
     }
     __syncthreads();
     const int32_t x = threadIdx.x >> 4, ch = 8 * (threadIdx.x & 15), row = it.row0 + 16 * r + x;
@@ -363,15 +430,57 @@ __global__ __launch_bounds__(256) void fp4_combine_kernel(uint16_t* __restrict__
   *reinterpret_cast<uint32_t*>(o + ((size_t)row * g.heads + h) * 128 + 2 * lane) = pack_bf16x2(y[0] * by, y[1] * by);
 }
 
+// The same attention over bf16 pages: a plan over a cache of its distinct pages alone, which are
+// taken out of their 4 bits into the workspace first.
+struct Fp4Wide {
+  sc_cache cache;
+  sc_plan plan;
+  std::vector<int32_t> src, dst;  // slots that are taken out, and where to
+  size_t page_bytes = 0;
+};
+
+// How a plan runs within so many bytes of workspace.
 struct Fp4Schedule {
-  size_t room;
-  int32_t tile;      // rows of an item: 16, 32 or 64
-  int32_t joined, p_len, p_pieces, o_len, o_pieces;  // chunks of a piece, pieces (own: the most of a node)
-  size_t bytes;
+  size_t room = 0;
+  std::shared_ptr<Fp4Wide> wide;  // over bf16 pages; else by tiles of so many rows:
+  int32_t tile = 16;
+  int32_t joined = 1, p_len = 1, p_pieces = 0, o_len = 1, o_pieces = 1;  // chunks of a piece, pieces (own: the most of a node)
+  size_t bytes = 0;
+  double us = 1e30;
 };
 
 static int64_t fp4_chunks(const sc_cache* c, int64_t pages) {
   return (pages * fp4_blocks(c->d.tokens_per_page) + 3) / 4;
+}
+
+// NULL where the bf16 kernels do not take the plan.
+static std::shared_ptr<Fp4Wide> fp4_wide(const sc_plan* p, const sc_cache* c) {
+  auto w = std::make_shared<Fp4Wide>();
+  std::map<int32_t, int32_t> place;
+  for (int32_t s : p->page_slot)
+    if (place.emplace(s, (int32_t)place.size()).second) {
+      w->src.push_back(s);
+      w->dst.push_back((int32_t)w->dst.size());
+    }
+  w->cache.d = c->d;
+  w->cache.d.dtype = SC_DTYPE_BF16;
+  w->cache.d.n_layers = 1;
+  w->cache.d.n_slots = (int32_t)w->src.size();
+  w->cache.pool = nullptr;
+  w->cache.slot_bytes = 4ull * c->d.n_heads * c->d.tokens_per_page * 128;
+  w->cache.kv_half = w->cache.slot_bytes / 2;
+  w->page_bytes = w->src.size() * w->cache.slot_bytes;
+  w->plan.nodes = p->nodes;
+  w->plan.page_off = p->page_off;
+  w->plan.page_tokens = p->page_tokens;
+  w->plan.page_frame = p->page_frame;
+  w->plan.page_state = p->page_state;
+  w->plan.page_gen.assign(p->page_slot.size(), 0);
+  for (int32_t s : p->page_slot) w->plan.page_slot.push_back(place.at(s));
+  w->plan.cache = &w->cache;
+  w->plan.nq = p->nq;
+  w->plan.shared = p->shared;
+  return attention_check(&w->plan, &w->cache) == SC_OK ? w : nullptr;
 }
 
 static Fp4Schedule find_fp4_schedule(const sc_plan* p, const sc_cache* c, size_t room) {
@@ -409,21 +518,35 @@ static Fp4Schedule find_fp4_schedule(const sc_plan* p, const sc_cache* c, size_t
     }
     s.bytes = (size_t)(s.p_pieces + s.o_pieces) * piece;
   }
+  if (getenv("FP4_WIDE") && atoi(getenv("FP4_WIDE"))) {
+    auto w = fp4_wide(p, c);
+    if (w) {
+      const size_t bytes = align256(w->page_bytes) + attention_exact_workspace_bytes(&w->plan, &w->cache);
+      if (bytes <= room) {
+        s.wide = w;
+        s.bytes = bytes;
+      }
+      if (getenv("FP4_TELL")) fprintf(stderr, "wide us %.1f pages %.1f MB\n", attention_exact_us(&w->plan, &w->cache), w->page_bytes / 1e6);
+    }
+  }
   return s;
 }
 
-static const Fp4Schedule& fp4_schedule(const sc_plan* p, const sc_cache* c, size_t room) {
+// Found once per plan, for the few rooms that its calls ask for.
+static const Fp4Schedule* fp4_schedule(const sc_plan* p, const sc_cache* c, size_t room) {
   for (const auto& s : p->fp4)
-    if (s->room == room) return *s;
-  p->fp4.push_back(std::make_shared<Fp4Schedule>(find_fp4_schedule(p, c, room)));
-  return *p->fp4.back();
+    if (s->room == room) return s.get();
+  try {
+    p->fp4.push_back(std::make_shared<Fp4Schedule>(find_fp4_schedule(p, c, room)));
+  } catch (const std::bad_alloc&) {
+    return nullptr;
+  }
+  return p->fp4.back().get();
 }
 
-size_t fp4_attention_workspace_bytes(const sc_plan* p, const sc_cache* c) { return fp4_schedule(p, c, SIZE_MAX).bytes; }
-
-template <int R>
-static void launch_fp4_tiles(uint32_t items, const uint16_t* q, uint16_t* o, const Fp4Geom& g, const Fp4List& l, hipStream_t stream) {
-  hipLaunchKernelGGL(fp4_attention_kernel<R>, dim3(items), dim3(64 * FA_NW), 0, stream, q, o, g, l);
+size_t fp4_attention_workspace_bytes(const sc_plan* p, const sc_cache* c) {
+  const Fp4Schedule* s = fp4_schedule(p, c, SIZE_MAX);
+  return s ? s->bytes : 0;
 }
 
 int launch_fp4_attention(const sc_plan* p, const sc_cache* c, int32_t layer, const void* q, void* o, float scale,
@@ -433,8 +556,18 @@ int launch_fp4_attention(const sc_plan* p, const sc_cache* c, int32_t layer, con
   if (reinterpret_cast<uintptr_t>(ws) & 15) return fail(SC_EINVAL, "workspace must be 16-byte aligned");
   const int64_t rows = (int64_t)p->nodes.size() * p->nq;
   if (rows > INT32_MAX) return fail(SC_EUNSUPPORTED, "%lld query rows", (long long)rows);
-  const Fp4Schedule* s = &fp4_schedule(p, c, SIZE_MAX);
-  if (s->bytes > room) s = &fp4_schedule(p, c, room);
+  const Fp4Schedule* s = fp4_schedule(p, c, SIZE_MAX);
+  if (s && s->bytes > room) s = fp4_schedule(p, c, room);
+  if (!s) return fail(SC_EINVAL, "out of host memory");
+  if (s->wide) {
+    Fp4Wide& w = *s->wide;
+    w.cache.pool = static_cast<char*>(ws);
+    const PagePairs pairs{w.src.data(), w.dst.data(), (int32_t)w.src.size()};
+    const int rc = launch_page_convert(false, PoolView{c->pool + (size_t)layer * c->d.n_slots * c->slot_bytes, 0},
+                                       PoolView{w.cache.pool, 0}, c->d, pairs, 1, stream);
+    if (rc != SC_OK) return rc;
+    return launch_attention_exact(&w.plan, &w.cache, 0, q, o, scale, w.cache.pool + align256(w.page_bytes), stream);
+  }
   Fp4List l;
   Fp4Geom g;
   fp4_fill(p, c, layer, scale, l, g);
@@ -457,9 +590,9 @@ int launch_fp4_attention(const sc_plan* p, const sc_cache* c, int32_t layer, con
   uint16_t* ob = static_cast<uint16_t*>(o);
   timer_begin(TK_ATTENTION, stream);
   if (s->tile == 16)
-    launch_fp4_tiles<1>((uint32_t)items, qb, ob, g, l, stream);
+    hipLaunchKernelGGL(fp4_attention_kernel<1>, dim3((uint32_t)items), dim3(64 * FA_NW), 0, stream, qb, ob, g, l);
   else
-    launch_fp4_tiles<2>((uint32_t)items, qb, ob, g, l, stream);
+    hipLaunchKernelGGL(fp4_attention_kernel<2>, dim3((uint32_t)items), dim3(64 * FA_NW), 0, stream, qb, ob, g, l);
   timer_end(TK_ATTENTION, stream);
   if (s->bytes) {
     timer_begin(TK_ATTN_COMBINE, stream);
@@ -471,10 +604,11 @@ int launch_fp4_attention(const sc_plan* p, const sc_cache* c, int32_t layer, con
 }
 
 int fp4_attention_form(const sc_plan* p, const sc_cache* c, int32_t* queries, int32_t* ring, int32_t* pieces) {
-  const Fp4Schedule& s = fp4_schedule(p, c, SIZE_MAX);
-  *queries = s.tile;
+  const Fp4Schedule* s = fp4_schedule(p, c, SIZE_MAX);
+  if (!s) return fail(SC_EINVAL, "out of host memory");
+  *queries = s->wide ? 0 : s->tile;
   *ring = 1;
-  *pieces = s.joined ? s.o_pieces : -s.p_pieces;
+  *pieces = s->joined ? s->o_pieces : -s->p_pieces;
   return SC_OK;
 }
 

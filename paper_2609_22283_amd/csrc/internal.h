@@ -144,6 +144,12 @@ constexpr int32_t kAttnMinSplitTiles = 32;  // mean 64-key tiles per unit below 
 size_t attention_workspace_bytes(const sc_plan* plan, const sc_cache* cache);
 size_t attention_lse_workspace_bytes(const sc_plan* plan, const sc_cache* cache);  // with the logarithmic sums
 size_t attention_workspace_bound();
+// A bf16 plan with logits that are products of q as it is (attention_check has accepted it):
+// its estimated time in us, its workspace, its launches.
+double attention_exact_us(const sc_plan* plan, const sc_cache* cache);
+size_t attention_exact_workspace_bytes(const sc_plan* plan, const sc_cache* cache);
+int launch_attention_exact(const sc_plan* plan, const sc_cache* cache, int32_t layer, const void* q, void* o,
+                           float scale, void* ws, hipStream_t stream);
 int launch_append(const sc_cache* cache, int32_t layer, const int32_t* slots, int32_t chunk,
                   const void* k, const void* v, const sc_rope* rope, hipStream_t stream);
 int launch_rope_table(const sc_rope_desc* d, void* table, hipStream_t stream);
