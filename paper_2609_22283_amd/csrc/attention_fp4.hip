@@ -6,10 +6,10 @@
 #include <cfloat>
 #include <climits>
 #include <cmath>
-#include <cstdlib>
 #include <cstring>
 #include <map>
 #include <new>
+#include <vector>
 
 #include "fp4.h"
 
@@ -407,7 +407,9 @@ __global__ __launch_bounds__(64 * FA_NW, R == 1 ? 3 : 2) void fp4_attention_kern
   }
 }
 
-// A wave per row and head joins the pieces that its node has: the prefix's and its own.
+// A wave per row and head joins the pieces that its node has, the prefix's and its own, N at
+// a time, whose loads are independent.
+template <int N>
 __global__ __launch_bounds__(256) void fp4_combine_kernel(uint16_t* __restrict__ o, Fp4Geom g, Fp4List list) {
   const int32_t lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6), h = blockIdx.y;
   if (row >= g.rows) return;
@@ -416,15 +418,30 @@ __global__ __launch_bounds__(256) void fp4_combine_kernel(uint16_t* __restrict__
   const int32_t pieces = g.p_pieces + ((blocks + 3) / 4 + g.o_len - 1) / g.o_len;
   const size_t step = (size_t)g.heads * g.rows, at = (size_t)h * g.rows + row;
   float m = -INFINITY, l = 0.f, y[2] = {0.f, 0.f};
-  for (int32_t p = 0; p < pieces; ++p) {
-    const size_t i = p * step + at;
-    const f32x2 ml = *reinterpret_cast<const f32x2*>(g.part_ml + 2 * i);
-    const f32x2 x = *reinterpret_cast<const f32x2*>(g.part_o + i * 128 + 2 * lane);
-    const float to = fmaxf(m, ml[0]), keep = exp2f(m - to), by = exp2f(ml[0] - to);
+  for (int32_t p = 0; p < pieces; p += N) {
+    f32x2 x[N], ml[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const size_t from = (size_t)min(p + i, pieces - 1) * step + at;
+      ml[i] = *reinterpret_cast<const f32x2*>(g.part_ml + 2 * from);
+      x[i] = *reinterpret_cast<const f32x2*>(g.part_o + from * 128 + 2 * lane);
+    }
+    float to = m;
+#pragma unroll
+    for (int i = 0; i < N; ++i) to = fmaxf(to, ml[i][0]);  // past the end the last one again
+    const float keep = __builtin_amdgcn_exp2f(m - to);
     m = to;
-    l = l * keep + ml[1] * by;
-    y[0] = y[0] * keep + x[0] * by;
-    y[1] = y[1] * keep + x[1] * by;
+    l *= keep;
+    y[0] *= keep;
+    y[1] *= keep;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (p + i < pieces) {
+        const float by = __builtin_amdgcn_exp2f(ml[i][0] - to);
+        l = fmaf(by, ml[i][1], l);
+        y[0] = fmaf(by, x[i][0], y[0]);
+        y[1] = fmaf(by, x[i][1], y[1]);
+      }
   }
   const float by = 1.f / l;
   *reinterpret_cast<uint32_t*>(o + ((size_t)row * g.heads + h) * 128 + 2 * lane) = pack_bf16x2(y[0] * by, y[1] * by);
@@ -483,53 +500,114 @@ static std::shared_ptr<Fp4Wide> fp4_wide(const sc_plan* p, const sc_cache* c) {
   return attention_check(&w->plan, &w->cache) == SC_OK ? w : nullptr;
 }
 
+// The time in us at which `slots` work-groups at once have done items of the given number
+// and time each, dealt out in this order.
+struct Fp4Items {
+  double count, us;
+};
+static double fp4_makespan(double slots, const std::vector<Fp4Items>& items) {
+  std::vector<std::pair<double, double>> level{{0.0, slots}};  // from this time on, so many slots
+  double end = 0.0;
+  for (const Fp4Items& it : items)
+    for (double left = it.count; left > 0;) {
+      std::sort(level.begin(), level.end());
+      if (left >= 2 * slots && level.back().first - level.front().first <= it.us) {  // whole rounds move all alike
+        const double rounds = std::floor(left / slots) - 1;
+        for (auto& l : level) l.first += rounds * it.us;
+        left -= rounds * slots;
+      }
+      const double at = level.front().first + it.us, take = std::min(left, level.front().second);
+      end = std::max(end, at);
+      left -= take;
+      level.front().second -= take;
+      if (level.front().second <= 0) level.erase(level.begin());
+      auto same = std::find_if(level.begin(), level.end(), [&](const auto& l) { return std::fabs(l.first - at) < 1e-3; });
+      if (same != level.end())
+        same->second += take;
+      else
+        level.emplace_back(at, take);
+    }
+  return end;
+}
+
+// The cheapest way within `room` bytes, by estimated time in us.  Measured (2 .. 12 heads, 1 ..
+// 1024 rows a node, 512 .. 262144 keys, 700 ways of cutting them; what is chosen is within
+// 10 % of the best of them): four chunks, one to each wave of a work-group, take
+//   tiles of 16 rows  1.36 with one work-group to a CU, 2.0 with two, 3.0 with three
+//   tiles of 32 rows  2.3 with one, 3.8 with two
+// an item 1 more, a launch 3, no less than the pages take from HBM at 5.6 MB per us; joining
+// pieces 3.5, 0.13 per piece and the partials at 2.2 MB per us.  So nodes that fill their tiles
+// read a shared prefix each by itself (sixteen of 16 rows over 128 x 128 keys 38 us, 49 with
+// the rows of all nodes in one matrix; 32 of one row over 256 x 64 keys 26 against 20).
+// Over bf16 pages: the time of that attention, 8 and 0.17 per MB of them (four nodes of 4680
+// rows over 21 x 1560 keys 3.02 ms, 3.36 by tiles; four of 256 over 21 x 256 59 us, 41 by tiles).
 static Fp4Schedule find_fp4_schedule(const sc_plan* p, const sc_cache* c, size_t room) {
   const int32_t n = (int32_t)p->nodes.size(), H = c->d.n_heads;
   const int64_t rows = (int64_t)n * p->nq;
-  int64_t own_max = 0;
-  for (int32_t i = 0; i < n; ++i) own_max = std::max<int64_t>(own_max, p->page_off[i + 1] - p->page_off[i] - p->shared);
-  Fp4Schedule s{};
-  s.room = room;
+  std::map<int64_t, int32_t> own;  // pages of a node's own, and nodes with so many
+  int64_t own_all = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    const int64_t pages = p->page_off[i + 1] - p->page_off[i] - p->shared;
+    ++own[pages];
+    own_all += pages;
+  }
+  const int64_t own_max = own.rbegin()->first;
+  Fp4Schedule best;
+  best.room = room;
   const int64_t piece = rows * H * (128 + 2) * (int64_t)sizeof(float);
-  const int64_t most = piece ? std::min<int64_t>(room / piece, 1024) : 0;  // pieces that fit
-  const int64_t pc = fp4_chunks(c, p->shared), oc = fp4_chunks(c, own_max);
-  s.joined = p->shared == 0 || most < 2;
-  const int64_t tile_rows = s.joined ? p->nq : rows;
-  s.tile = tile_rows <= 16 ? 16 : 32;
-  if (const char* e = getenv("FP4_TILE")) s.tile = atoi(e);
-  const int64_t want = getenv("FP4_ITEMS") ? atoi(getenv("FP4_ITEMS")) : 512;
-  const int64_t ou = (int64_t)H * n * ((p->nq + s.tile - 1) / s.tile), pu = (int64_t)H * ((rows + s.tile - 1) / s.tile);
-  const int64_t len_min = getenv("FP4_MIN") ? atoi(getenv("FP4_MIN")) : 4;
-  if (s.joined) {
-    const int64_t all = fp4_chunks(c, own_max + p->shared);
-    int64_t pieces = std::max<int64_t>(1, std::min({want / ou, all / len_min, most}));
-    s.o_len = (int32_t)((all + pieces - 1) / pieces);
-    s.o_pieces = (int32_t)((all + s.o_len - 1) / s.o_len);
-    s.bytes = s.o_pieces > 1 ? (size_t)s.o_pieces * piece : 0;
-  } else {
-    const int64_t work = pc * pu + oc * ou;
-    int64_t len = std::max<int64_t>(len_min, work / want);
-    for (;; len += len / 8 + 1) {
-      s.p_len = (int32_t)std::min(len, pc);
-      s.o_len = (int32_t)std::min(len, oc);
-      s.p_pieces = (int32_t)((pc + s.p_len - 1) / s.p_len);
-      s.o_pieces = (int32_t)((oc + s.o_len - 1) / s.o_len);
-      if (s.p_pieces + s.o_pieces <= most) break;
-    }
-    s.bytes = (size_t)(s.p_pieces + s.o_pieces) * piece;
-  }
-  if (getenv("FP4_WIDE") && atoi(getenv("FP4_WIDE"))) {
-    auto w = fp4_wide(p, c);
-    if (w) {
-      const size_t bytes = align256(w->page_bytes) + attention_exact_workspace_bytes(&w->plan, &w->cache);
-      if (bytes <= room) {
-        s.wide = w;
-        s.bytes = bytes;
+  const double from_hbm = (double)(p->shared + own_all) * c->slot_bytes / 5.6e6;
+  const int64_t prefix = fp4_chunks(c, p->shared);
+  std::vector<Fp4Items> items;
+  for (const int32_t tile : {16, 32})
+    for (const int32_t joined : {1, 0}) {
+      if (!joined && !p->shared) continue;
+      const int64_t own_tiles = (int64_t)H * ((p->nq + tile - 1) / tile), p_tiles = (int64_t)H * ((rows + tile - 1) / tile);
+      const int64_t own_chunks = fp4_chunks(c, own_max + (joined ? p->shared : 0)), cut = std::max(own_chunks, joined ? 0 : prefix);
+      for (int64_t pieces = 1, last = 0; pieces <= std::min<int64_t>(cut, 256); pieces += 1 + pieces / 8) {
+        const int64_t len = (cut + pieces - 1) / pieces, o_len = std::min(len, own_chunks), p_len = joined ? 1 : std::min(len, prefix);
+        if (len == last) continue;
+        last = len;
+        Fp4Schedule s;
+        s.room = room;
+        s.tile = tile;
+        s.joined = joined;
+        s.o_len = (int32_t)o_len;
+        s.o_pieces = (int32_t)((own_chunks + o_len - 1) / o_len);
+        if (!joined) {
+          s.p_len = (int32_t)p_len;
+          s.p_pieces = (int32_t)((prefix + p_len - 1) / p_len);
+        }
+        const int64_t all = s.p_pieces + s.o_pieces;
+        if (all > 1 && (double)all * piece > (double)room) break;
+        s.bytes = all > 1 ? (size_t)(all * piece) : 0;
+        items.clear();
+        double total = 0;
+        const auto add = [&](double units, int64_t chunks, int64_t of) {
+          if (chunks >= of) items.push_back({units * (double)(chunks / of), (double)((of + 3) / 4)});
+          if (chunks % of) items.push_back({units, (double)((chunks % of + 3) / 4)});
+          total += units * (double)((chunks + of - 1) / of);
+        };
+        if (!joined) add((double)p_tiles, prefix, p_len);
+        for (const auto& o : own) add((double)own_tiles * o.second, fp4_chunks(c, o.first + (joined ? p->shared : 0)), o_len);
+        if (total > INT32_MAX / 2) continue;
+        const int32_t per = total <= kCUs ? 1 : total <= 2 * kCUs || tile == 32 ? 2 : 3;  // work-groups to a CU
+        const double step = tile == 16 ? (per == 1 ? 1.36 : per == 2 ? 2.0 : 3.0) : (per == 1 ? 2.3 : 3.8);
+        for (Fp4Items& i : items) i.us = i.us * step + 1.0;
+        s.us = std::max(fp4_makespan((double)kCUs * per, items), from_hbm) + 3.0;
+        if (s.bytes) s.us += 3.5 + 0.13 * (double)all + (double)s.bytes / 2.2e6;
+        if (s.us < best.us) best = s;
       }
-      if (getenv("FP4_TELL")) fprintf(stderr, "wide us %.1f pages %.1f MB\n", attention_exact_us(&w->plan, &w->cache), w->page_bytes / 1e6);
+    }
+  if (auto w = fp4_wide(p, c)) {
+    const size_t bytes = align256(w->page_bytes) + attention_exact_workspace_bytes(&w->plan, &w->cache);
+    const double us = attention_exact_us(&w->plan, &w->cache) + 8.0 + 0.17e-6 * (double)w->page_bytes;
+    if (bytes <= room && us < best.us) {
+      best.wide = w;
+      best.bytes = bytes;
+      best.us = us;
     }
   }
-  return s;
+  return best;
 }
 
 // Found once per plan, for the few rooms that its calls ask for.
@@ -596,7 +674,14 @@ int launch_fp4_attention(const sc_plan* p, const sc_cache* c, int32_t layer, con
   timer_end(TK_ATTENTION, stream);
   if (s->bytes) {
     timer_begin(TK_ATTN_COMBINE, stream);
-    hipLaunchKernelGGL(fp4_combine_kernel, dim3((uint32_t)(g.rows + 3) / 4, (uint32_t)g.heads), dim3(256), 0, stream, ob, g, l);
+    const dim3 grid((uint32_t)(g.rows + 3) / 4, (uint32_t)g.heads);
+    const int32_t most = g.p_pieces + s->o_pieces;
+    if (most <= 2)
+      hipLaunchKernelGGL(fp4_combine_kernel<2>, grid, dim3(256), 0, stream, ob, g, l);
+    else if (most <= 4)
+      hipLaunchKernelGGL(fp4_combine_kernel<4>, grid, dim3(256), 0, stream, ob, g, l);
+    else
+      hipLaunchKernelGGL(fp4_combine_kernel<8>, grid, dim3(256), 0, stream, ob, g, l);
     timer_end(TK_ATTN_COMBINE, stream);
   }
   SC_HIP(hipGetLastError());
