@@ -55,39 +55,128 @@ struct RotateArgs {
   int32_t rows, heads, half;  // half: pairs of all axes
   int32_t pairs_t, pairs_h, pairs_w, frames, grid_h, grid_w;
   int32_t rest;               // channels behind the rotated ones, copied (0 in place)
+  int32_t pair_units, units;  // of a row and head: runs of pairs, then runs of copied channels
   float sign;                 // of the sines
-  int32_t interleaved;
+  DivMagic units_div;
 };
 
-template <class T> __device__ __forceinline__ float rot_load(T x);
-template <> __device__ __forceinline__ float rot_load<uint16_t>(uint16_t x) { return bf16_to_f32(x); }
-template <> __device__ __forceinline__ float rot_load<float>(float x) { return x; }
-template <class T> __device__ __forceinline__ T rot_store(float x);
-template <> __device__ __forceinline__ uint16_t rot_store<uint16_t>(float x) { return f32_to_bf16(x); }
-template <> __device__ __forceinline__ float rot_store<float>(float x) { return x; }
+// 16 bytes of a tensor aligned to its elements, and its values as fp32.
+template <class T> struct RotRun;
+template <> struct RotRun<uint16_t> {
+  static constexpr int N = 8;
+  typedef uint32_t V __attribute__((ext_vector_type(4), aligned(2)));
+  static __device__ __forceinline__ float get(const V& v, int i) {
+    return __uint_as_float(i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16);
+  }
+  static __device__ __forceinline__ V make(const float (&f)[N]) {
+    return V{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
+  }
+  static __device__ __forceinline__ float one(uint16_t x) { return bf16_to_f32(x); }
+  static __device__ __forceinline__ uint16_t back(float x) { return f32_to_bf16(x); }
+};
+template <> struct RotRun<float> {
+  static constexpr int N = 4;
+  typedef float V __attribute__((ext_vector_type(4), aligned(4)));
+  static __device__ __forceinline__ float get(const V& v, int i) { return v[i]; }
+  static __device__ __forceinline__ V make(const float (&f)[N]) { return V{f[0], f[1], f[2], f[3]}; }
+  static __device__ __forceinline__ float one(float x) { return x; }
+  static __device__ __forceinline__ float back(float x) { return x; }
+};
 
-// A thread takes one pair of a row and head, or one channel that is copied.
-template <class T>
-__global__ __launch_bounds__(256) void rotate_plain_kernel(const T* x, T* y, RotateArgs g) {
-  const int32_t units = g.half + g.rest;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= (int64_t)g.rows * g.heads * units) return;
-  const int32_t u = (int32_t)(i % units), h = (int32_t)(i / units % g.heads), r = (int32_t)(i / units / g.heads);
-  const T* xr = x + r * g.x_row + h * g.x_head;
-  T* yr = y + r * g.y_row + h * g.y_head;
+// A thread takes a run of pairs (of 16 bytes of channels; HALF: 16 bytes of either half) of one
+// row in HP heads, or a run of copied channels.  The row's cosines and sines are read
+// once for the heads, whose loads are all out before the first is used.  Bound by memory
+// where there are many rows: four nodes of 4680 rows of 12 x 128 channels (115 MB) 26 us, 57
+// with a pair a thread; by latency at few.
+template <class T, bool HALF, int HP>
+__global__ __launch_bounds__(256) void rotate_kernel(const T* x, T* y, RotateArgs g) {
+  using Run = RotRun<T>;
+  using V = typename Run::V;
+  constexpr int N = Run::N, P = HALF ? N : N / 2;
+  const uint32_t i = blockIdx.x * 256u + threadIdx.x;
+  if (i >= (uint32_t)g.rows * (uint32_t)g.units) return;
+  const int32_t r = (int32_t)fast_div(i, g.units_div), u = (int32_t)i - r * g.units, h0 = blockIdx.y * HP;
   const int32_t t = g.pos[3 * (int64_t)r], ph = g.pos[3 * (int64_t)r + 1], pw = g.pos[3 * (int64_t)r + 2];
   if ((uint32_t)t >= (uint32_t)g.frames || (uint32_t)ph >= (uint32_t)g.grid_h || (uint32_t)pw >= (uint32_t)g.grid_w) return;
-  if (u >= g.half) {
-    yr[g.half + u] = xr[g.half + u];
+  const bool pairs = u < g.pair_units;
+  const int32_t p0 = u * P, c0 = pairs ? (HALF ? p0 : 2 * p0) : 2 * g.half + (u - g.pair_units) * N;
+  // elements of the run (of either half), all there but at the end
+  const int32_t n = pairs ? (HALF ? min(N, g.half - p0) : min(N, 2 * (g.half - p0))) : min(N, g.rest - (u - g.pair_units) * N);
+  const T* xr = x + r * g.x_row + c0;
+  T* yr = y + r * g.y_row + c0;
+  V a[HP], b[HP];
+  if (n == N)
+#pragma unroll
+    for (int j = 0; j < HP; ++j) {
+      const T* from = xr + min(h0 + j, g.heads - 1) * g.x_head;
+      a[j] = *reinterpret_cast<const V*>(from);
+      if (HALF && pairs) b[j] = *reinterpret_cast<const V*>(from + g.half);
+    }
+  if (!pairs) {
+#pragma unroll
+    for (int j = 0; j < HP; ++j) {
+      if (h0 + j >= g.heads) break;
+      T* to = yr + (h0 + j) * g.y_head;
+      if (n == N)
+        *reinterpret_cast<V*>(to) = a[j];
+      else
+        for (int e = 0; e < n; ++e) to[e] = xr[(h0 + j) * g.x_head + e];
+    }
     return;
   }
-  const float2 cs = u < g.pairs_t ? g.table[(int64_t)t * g.pairs_t + u]
-                    : u < g.pairs_t + g.pairs_h ? g.table[g.off_h + (int64_t)ph * g.pairs_h + u - g.pairs_t]
-                                                : g.table[g.off_w + (int64_t)pw * g.pairs_w + u - g.pairs_t - g.pairs_h];
-  const int32_t a = g.interleaved ? 2 * u : u, b = g.interleaved ? 2 * u + 1 : u + g.half;
-  const float x0 = rot_load<T>(xr[a]), x1 = rot_load<T>(xr[b]), s = g.sign * cs.y;
-  yr[a] = rot_store<T>(fmaf(x0, cs.x, -(x1 * s)));
-  yr[b] = rot_store<T>(fmaf(x0, s, x1 * cs.x));
+  float2 cs[P];
+#pragma unroll
+  for (int e = 0; e < P; ++e) {
+    const int32_t p = min(p0 + e, g.half - 1);
+    cs[e] = g.table[p < g.pairs_t ? (int64_t)t * g.pairs_t + p
+                    : p < g.pairs_t + g.pairs_h ? g.off_h + (int64_t)ph * g.pairs_h + p - g.pairs_t
+                                                : g.off_w + (int64_t)pw * g.pairs_w + p - g.pairs_t - g.pairs_h];
+    cs[e].y *= g.sign;
+  }
+#pragma unroll
+  for (int j = 0; j < HP; ++j) {
+    if (h0 + j >= g.heads) break;
+    T* to = yr + (h0 + j) * g.y_head;
+    if (n == N) {
+      float fa[N], fb[N];
+#pragma unroll
+      for (int e = 0; e < P; ++e) {
+        const float x0 = Run::get(a[j], HALF ? e : 2 * e), x1 = HALF ? Run::get(b[j], e) : Run::get(a[j], 2 * e + 1);
+        const float y0 = fmaf(x0, cs[e].x, -(x1 * cs[e].y)), y1 = fmaf(x0, cs[e].y, x1 * cs[e].x);
+        if constexpr (HALF) {
+          fa[e] = y0;
+          fb[e] = y1;
+        } else {
+          fa[2 * e] = y0;
+          fa[2 * e + 1] = y1;
+        }
+      }
+      *reinterpret_cast<V*>(to) = Run::make(fa);
+      if constexpr (HALF) *reinterpret_cast<V*>(to + g.half) = Run::make(fb);
+    } else {
+      const T* from = xr + (h0 + j) * g.x_head;
+#pragma unroll
+      for (int e = 0; e < P; ++e) {
+        if (p0 + e >= g.half) break;
+        const int32_t i0 = HALF ? e : 2 * e, i1 = HALF ? e + g.half : 2 * e + 1;
+        const float x0 = Run::one(from[i0]), x1 = Run::one(from[i1]);
+        to[i0] = Run::back(fmaf(x0, cs[e].x, -(x1 * cs[e].y)));
+        to[i1] = Run::back(fmaf(x0, cs[e].y, x1 * cs[e].x));
+      }
+    }
+  }
+}
+
+// Few rows: a head a thread, so that the work spreads over the CUs.
+template <class T, bool HALF>
+static void launch_rotate_t(const void* x, void* y, const RotateArgs& g, hipStream_t s) {
+  const uint32_t groups = (uint32_t)(((int64_t)g.rows * g.units + 255) / 256);
+  const T* xt = static_cast<const T*>(x);
+  T* yt = static_cast<T*>(y);
+  if ((int64_t)groups * ((g.heads + 3) / 4) < 4 * kCUs)
+    hipLaunchKernelGGL((rotate_kernel<T, HALF, 1>), dim3(groups, (uint32_t)g.heads), dim3(256), 0, s, xt, yt, g);
+  else
+    hipLaunchKernelGGL((rotate_kernel<T, HALF, 4>), dim3(groups, (uint32_t)(g.heads + 3) / 4), dim3(256), 0, s, xt, yt, g);
 }
 
 }  // namespace sc
@@ -160,7 +249,6 @@ extern "C" int sc_rope_rotate(const sc_rope* rope, const sc_rotate_desc* d, cons
   g.y_head = d->y_head;
   g.off_h = L.off_h;
   g.off_w = L.off_w;
-  g.rows = d->n_rows;
   g.heads = d->n_heads;
   g.half = (int32_t)(part / 2);
   g.pairs_t = L.pairs_t;
@@ -171,18 +259,30 @@ extern "C" int sc_rope_rotate(const sc_rope* rope, const sc_rotate_desc* d, cons
   g.grid_w = t.grid_w;
   g.rest = in_place ? 0 : (int32_t)(d->head_dim - part);
   g.sign = d->transpose ? -1.f : 1.f;
-  g.interleaved = d->layout == SC_ROPE_INTERLEAVED;
-  const int64_t threads = (int64_t)g.rows * g.heads * (g.half + g.rest), groups = (threads + 255) / 256;
-  if (groups > INT32_MAX) return fail(SC_EUNSUPPORTED, "%lld channel pairs in one call", (long long)threads);
+  const bool f32 = d->dtype == SC_DTYPE_F32, halves = d->layout == SC_ROPE_HALF;
+  const int32_t run = 16 / (int32_t)es, run_pairs = halves ? run : run / 2;
+  g.pair_units = (g.half + run_pairs - 1) / run_pairs;
+  g.units = g.pair_units + (g.rest + run - 1) / run;
+  g.units_div = magic_div((uint32_t)g.units);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  timer_begin(TK_ROTATE, s);
-  if (d->dtype == SC_DTYPE_F32)
-    hipLaunchKernelGGL(rotate_plain_kernel<float>, dim3((uint32_t)groups), dim3(256), 0, s, static_cast<const float*>(x),
-                       static_cast<float*>(y), g);
-  else
-    hipLaunchKernelGGL(rotate_plain_kernel<uint16_t>, dim3((uint32_t)groups), dim3(256), 0, s,
-                       static_cast<const uint16_t*>(x), static_cast<uint16_t*>(y), g);
-  timer_end(TK_ROTATE, s);
-  SC_HIP(hipGetLastError());
+  const int32_t most = INT32_MAX / g.units - 256;  // rows of a launch, whose threads are numbered in 31 bits
+  if (most < 1 || g.heads > 65535) return fail(SC_EUNSUPPORTED, "%d heads of %d channels", g.heads, d->head_dim);
+  for (int64_t row = 0; row < d->n_rows; row += most) {
+    g.rows = (int32_t)std::min<int64_t>(most, d->n_rows - row);
+    g.pos = positions + 3 * row;
+    const char* from = xb + row * d->x_row * (int64_t)es;
+    char* to = static_cast<char*>(y) + row * d->y_row * (int64_t)es;
+    timer_begin(TK_ROTATE, s);
+    if (f32 && halves)
+      launch_rotate_t<float, true>(from, to, g, s);
+    else if (f32)
+      launch_rotate_t<float, false>(from, to, g, s);
+    else if (halves)
+      launch_rotate_t<uint16_t, true>(from, to, g, s);
+    else
+      launch_rotate_t<uint16_t, false>(from, to, g, s);
+    timer_end(TK_ROTATE, s);
+    SC_HIP(hipGetLastError());
+  }
   return SC_OK;
 }
