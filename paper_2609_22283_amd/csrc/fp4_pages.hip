@@ -60,7 +60,7 @@ int launch_page_moves(const PoolView& from, const PoolView& to, uint64_t bytes, 
   });
 }
 
-// Where a wave's block lies: pages of both kinds.
+// Pages of both kinds, and the waves' items in a page: blocks, or pairs of them.
 struct ConvertGeom {
   const char* from;
   char* to;
@@ -69,71 +69,96 @@ struct ConvertGeom {
   DivMagic blocks_div;
 };
 
-// One wave per block; every access of a wave is of whole 256-byte runs of the block, and
-// of 16-byte runs of a row of the page.
-//   K: pass i takes the tokens 16 (i / 4) + 4 (i % 4) + lane / 16, eight channels a lane;
-//   V: pass n takes the channels 16 n + lane / 4, eight tokens a lane
-// so that four neighbouring lanes hold a group and a lane's passes fill its scales' words.
-template <bool PACK>
-__global__ __launch_bounds__(256) void page_convert_kernel(ConvertGeom g, PairList pairs) {
+// Lanes and passes over K of a block: pass i takes the tokens k_token(i) + lane / 16, eight
+// channels a lane, so that four neighbouring lanes hold a group and a lane's passes fill its
+// scales' words.
+__device__ __forceinline__ int k_token(int i) { return 16 * (i >> 2) + 4 * (i & 3); }
+__device__ __forceinline__ uint32_t k_scales_at(int32_t lane) { return kFp4KScale + (lane >> 4) * 16 + (lane >> 2 & 3) * 4; }
+__device__ __forceinline__ uint32_t group_scale(const u32x4& v) {
+  return fp4_scale(quad_max(umax(umax(bf16x2_top(v[0]), bf16x2_top(v[1])), umax(bf16x2_top(v[2]), bf16x2_top(v[3])))));
+}
+// Codes and scales of K of a block whose eight passes' values are given.
+__device__ __forceinline__ void pack_keys(const u32x4 (&k)[8], char* block, int32_t lane) {
+  uint32_t w[2] = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t s = group_scale(k[i]);
+    *reinterpret_cast<uint32_t*>(block + (k_token(i) + (lane >> 4)) * 64 + (lane & 15) * 4) = fp4_codes(k[i], s);
+    w[i >> 2] |= s << (8 * (i & 3));
+  }
+  if ((lane & 3) == 0) {
+    *reinterpret_cast<uint32_t*>(block + k_scales_at(lane)) = w[0];
+    *reinterpret_cast<uint32_t*>(block + k_scales_at(lane) + 64) = w[1];
+  }
+}
+
+// One wave per two blocks: of V, pass n takes the channels 8 n + lane / 8 of both, eight
+// tokens a lane, 128 bytes of a channel (a wave per block had pairs of waves wait for each
+// other's lines: 20 states of 64 tokens, 12 heads, 30 layers 78 us, 56 so).
+__global__ __launch_bounds__(256) void page_pack_kernel(ConvertGeom g, PairList pairs) {
   const int32_t lane = threadIdx.x & 63;
   const int32_t item = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (item >= g.heads * g.blocks) return;
-  const int32_t h = (int32_t)fast_div((uint32_t)item, g.blocks_div), b = item - h * g.blocks, t0 = b * kFp4Tokens;
-  const uint64_t half = (uint64_t)g.heads * g.tpp * 256;  // of a bf16 page
-  const int32_t src = pairs.src[blockIdx.y], dst = pairs.dst[blockIdx.y];
-  char* page = PACK ? const_cast<char*>(g.from) + blockIdx.z * g.from_layer + (uint64_t)src * g.from_slot
-                    : g.to + blockIdx.z * g.to_layer + (uint64_t)dst * g.to_slot;
-  char* block = (PACK ? g.to + blockIdx.z * g.to_layer + (uint64_t)dst * g.to_slot
-                      : const_cast<char*>(g.from) + blockIdx.z * g.from_layer + (uint64_t)src * g.from_slot) +
-                (uint64_t)item * kFp4Block;
-  char* krow = page + ((uint64_t)h * g.tpp + t0 + (lane >> 4)) * 256 + (lane & 15) * 16;
-  char* vrow = page + half + ((uint64_t)h * 128 + (lane >> 2)) * g.tpp * 2 + (t0 + 8 * (lane & 3)) * 2;
-  const int32_t left = g.tpp - t0;  // tokens of the page from t0 on
-  const auto k_token = [&](int i) { return 16 * (i >> 2) + 4 * (i & 3); };
-  char* ks = block + kFp4KScale + (lane >> 4) * 16 + (lane >> 2 & 3) * 4;
-  char* vs = block + kFp4VScale + (lane >> 2) * 8;
-  if constexpr (PACK) {
+  if (item >= g.heads * g.blocks) return;  // g.blocks: pairs of blocks of a page
+  const int32_t h = (int32_t)fast_div((uint32_t)item, g.blocks_div), b = 2 * (item - h * g.blocks), t0 = b * kFp4Tokens;
+  const int32_t all = (g.tpp + kFp4Tokens - 1) / kFp4Tokens, left = g.tpp - t0;  // blocks of a page; its tokens from t0 on
+  const char* page = g.from + blockIdx.z * g.from_layer + (uint64_t)pairs.src[blockIdx.y] * g.from_slot;
+  char* block = g.to + blockIdx.z * g.to_layer + (uint64_t)pairs.dst[blockIdx.y] * g.to_slot + ((uint64_t)h * all + b) * kFp4Block;
+  const char* krow = page + ((uint64_t)h * g.tpp + t0 + (lane >> 4)) * 256 + (lane & 15) * 16;
+  const char* vrow = page + (uint64_t)g.heads * g.tpp * 256 + ((uint64_t)h * 128 + (lane >> 3)) * g.tpp * 2 + (t0 + 8 * (lane & 7)) * 2;
+  const bool two = b + 1 < all, mine = two || (lane & 4) == 0;
+  char* vcodes = block + (lane >> 2 & 1) * kFp4Block + kFp4V + (lane >> 3) * 16 + (lane & 3) * 4;
+  u32x2 vw[2] = {};
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
     u32x4 k[8], v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       k[i] = v[i] = u32x4{};
-      if (k_token(i) + (lane >> 4) < left) k[i] = *reinterpret_cast<const u32x4u*>(krow + (uint64_t)k_token(i) * 256);
-      if (8 * (lane & 3) < left) v[i] = *reinterpret_cast<const u32x4u*>(vrow + (uint64_t)i * 16 * g.tpp * 2);
-    }
-    uint32_t kw[2] = {0, 0}, vw[2] = {0, 0};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t s = fp4_scale(quad_max(umax(umax(bf16x2_top(k[i][0]), bf16x2_top(k[i][1])),
-                                                 umax(bf16x2_top(k[i][2]), bf16x2_top(k[i][3])))));
-      *reinterpret_cast<uint32_t*>(block + (k_token(i) + (lane >> 4)) * 64 + (lane & 15) * 4) = fp4_codes(k[i], s);
-      kw[i >> 2] |= s << (8 * (i & 3));
-      const uint32_t w = fp4_scale(quad_max(umax(umax(bf16x2_top(v[i][0]), bf16x2_top(v[i][1])),
-                                                 umax(bf16x2_top(v[i][2]), bf16x2_top(v[i][3])))));
-      *reinterpret_cast<uint32_t*>(block + kFp4V + i * 256 + lane * 4) = fp4_codes(v[i], w);
-      vw[i >> 2] |= w << (8 * (i & 3));
-    }
-    if ((lane & 3) == 0) {
-      *reinterpret_cast<uint32_t*>(ks) = kw[0];
-      *reinterpret_cast<uint32_t*>(ks + 64) = kw[1];
-      *reinterpret_cast<u32x2*>(vs) = u32x2{vw[0], vw[1]};
-    }
-  } else {
-    uint32_t k[8], v[8];
-    const uint32_t kw[2] = {*reinterpret_cast<const uint32_t*>(ks), *reinterpret_cast<const uint32_t*>(ks + 64)};
-    const u32x2 vw = *reinterpret_cast<const u32x2*>(vs);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      k[i] = *reinterpret_cast<const uint32_t*>(block + (k_token(i) + (lane >> 4)) * 64 + (lane & 15) * 4);
-      v[i] = *reinterpret_cast<const uint32_t*>(block + kFp4V + i * 256 + lane * 4);
+      if (32 * half + k_token(i) + (lane >> 4) < left)
+        k[i] = *reinterpret_cast<const u32x4u*>(krow + (uint64_t)(32 * half + k_token(i)) * 256);
+      if (8 * (lane & 7) < left) v[i] = *reinterpret_cast<const u32x4u*>(vrow + (uint64_t)(8 * half + i) * 8 * g.tpp * 2);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (k_token(i) + (lane >> 4) < left)
-        *reinterpret_cast<u32x4u*>(krow + (uint64_t)k_token(i) * 256) = fp4_values(k[i], kw[i >> 2] >> (8 * (i & 3)) & 255u);
-      if (8 * (lane & 3) < left)
-        *reinterpret_cast<u32x4u*>(vrow + (uint64_t)i * 16 * g.tpp * 2) = fp4_values(v[i], vw[i >> 2] >> (8 * (i & 3)) & 255u);
+    for (int i = 0; i < 8; ++i) {  // channel 64 half + 8 i + lane / 8: byte 4 half + i / 2 of the scales of channel % 16
+      const uint32_t s = group_scale(v[i]);
+      if (mine) *reinterpret_cast<uint32_t*>(vcodes + (8 * half + i) * 128) = fp4_codes(v[i], s);
+      vw[i & 1][half] |= s << (8 * (i >> 1));
     }
+    if (half == 0 || two) pack_keys(k, block + half * kFp4Block, lane);
+  }
+  if ((lane & 3) == 0 && mine) {
+    char* vs = block + (lane >> 2 & 1) * kFp4Block + kFp4VScale + (lane >> 3) * 8;
+    *reinterpret_cast<u32x2*>(vs) = vw[0];
+    *reinterpret_cast<u32x2*>(vs + 64) = vw[1];
+  }
+}
+
+// One wave per block: of V, pass n takes the channels 16 n + lane / 4, eight tokens a lane.
+__global__ __launch_bounds__(256) void page_unpack_kernel(ConvertGeom g, PairList pairs) {
+  const int32_t lane = threadIdx.x & 63;
+  const int32_t item = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (item >= g.heads * g.blocks) return;
+  const int32_t h = (int32_t)fast_div((uint32_t)item, g.blocks_div), b = item - h * g.blocks, t0 = b * kFp4Tokens;
+  const int32_t left = g.tpp - t0;  // tokens of the page from t0 on
+  char* page = g.to + blockIdx.z * g.to_layer + (uint64_t)pairs.dst[blockIdx.y] * g.to_slot;
+  const char* block = g.from + blockIdx.z * g.from_layer + (uint64_t)pairs.src[blockIdx.y] * g.from_slot + (uint64_t)item * kFp4Block;
+  char* krow = page + ((uint64_t)h * g.tpp + t0 + (lane >> 4)) * 256 + (lane & 15) * 16;
+  char* vrow = page + (uint64_t)g.heads * g.tpp * 256 + ((uint64_t)h * 128 + (lane >> 2)) * g.tpp * 2 + (t0 + 8 * (lane & 3)) * 2;
+  const char* ks = block + k_scales_at(lane);
+  uint32_t k[8], v[8];
+  const uint32_t kw[2] = {*reinterpret_cast<const uint32_t*>(ks), *reinterpret_cast<const uint32_t*>(ks + 64)};
+  const u32x2 vw = *reinterpret_cast<const u32x2*>(block + kFp4VScale + (lane >> 2) * 8);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    k[i] = *reinterpret_cast<const uint32_t*>(block + (k_token(i) + (lane >> 4)) * 64 + (lane & 15) * 4);
+    v[i] = *reinterpret_cast<const uint32_t*>(block + kFp4V + i * 256 + lane * 4);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (k_token(i) + (lane >> 4) < left)
+      *reinterpret_cast<u32x4u*>(krow + (uint64_t)k_token(i) * 256) = fp4_values(k[i], kw[i >> 2] >> (8 * (i & 3)) & 255u);
+    if (8 * (lane & 3) < left)
+      *reinterpret_cast<u32x4u*>(vrow + (uint64_t)i * 16 * g.tpp * 2) = fp4_values(v[i], vw[i >> 2] >> (8 * (i & 3)) & 255u);
   }
 }
 
@@ -143,9 +168,9 @@ int launch_page_convert(bool pack, const PoolView& from, const PoolView& to, con
   std::memset(&g, 0, sizeof g);
   g.heads = d.n_heads;
   g.tpp = d.tokens_per_page;
-  g.blocks = fp4_blocks(g.tpp);
+  g.blocks = pack ? (fp4_blocks(g.tpp) + 1) / 2 : fp4_blocks(g.tpp);
   g.blocks_div = magic_div((uint32_t)g.blocks);
-  const uint64_t wide = 4ull * d.n_heads * d.tokens_per_page * 128, held = (uint64_t)d.n_heads * g.blocks * kFp4Block;
+  const uint64_t wide = 4ull * d.n_heads * d.tokens_per_page * 128, held = (uint64_t)d.n_heads * fp4_blocks(g.tpp) * kFp4Block;
   g.from_slot = pack ? wide : held;
   g.to_slot = pack ? held : wide;
   g.from_layer = from.layer_bytes;
@@ -155,9 +180,9 @@ int launch_page_convert(bool pack, const PoolView& from, const PoolView& to, con
     g.from = from.base + layer * from.layer_bytes;
     g.to = to.base + layer * to.layer_bytes;
     if (pack)
-      hipLaunchKernelGGL(page_convert_kernel<true>, dim3(groups, n, m), dim3(256), 0, stream, g, l);
+      hipLaunchKernelGGL(page_pack_kernel, dim3(groups, n, m), dim3(256), 0, stream, g, l);
     else
-      hipLaunchKernelGGL(page_convert_kernel<false>, dim3(groups, n, m), dim3(256), 0, stream, g, l);
+      hipLaunchKernelGGL(page_unpack_kernel, dim3(groups, n, m), dim3(256), 0, stream, g, l);
   });
 }
 
@@ -192,7 +217,7 @@ __global__ __launch_bounds__(256) void fp4_append_kernel(AppendArgs g, int32_t i
   u32x4 k[8], v[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int32_t tk = 16 * (i >> 2) + 4 * (i & 3) + (lane >> 4), tv = 8 * (lane >> 4) + i;
+    const int32_t tk = k_token(i) + (lane >> 4), tv = 8 * (lane >> 4) + i;
     k[i] = v[i] = u32x4{};
     if (tk < left) k[i] = *reinterpret_cast<const u32x4u*>(g.k + src + tk * row);
     if (tv < left) v[i] = *reinterpret_cast<const u32x4u*>(g.v + src + tv * row);
@@ -207,33 +232,33 @@ __global__ __launch_bounds__(256) void fp4_append_kernel(AppendArgs g, int32_t i
       base[j] = ax[j] == 0 ? (int64_t)(g.frame0 + page) * g.pairs_t + p
                 : ax[j] == 1 ? g.off_h + p - g.pairs_t : g.off_w + p - g.pairs_t - g.pairs_h;
     }
+    // four tokens' rotations at a time are out before the first is used
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int32_t tok = t0 + 16 * (i >> 2) + 4 * (i & 3) + (lane >> 4);
-      if (tok >= g.tpp) continue;
-      const int32_t hh = (int32_t)fast_div((uint32_t)tok, g.gw_div), ww = tok - hh * g.grid_w;
+    for (int i0 = 0; i0 < 8; i0 += 4) {
+      float2 cs[4][4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float2 cs = g.table[base[j] + (ax[j] == 0 ? 0 : ax[j] == 1 ? hh * g.pairs_h : ww * g.pairs_w)];
-        const float x0 = __uint_as_float(k[i][j] << 16), x1 = __uint_as_float(k[i][j] & 0xffff0000u);
-        // as the bf16 cache rotates and rounds them
-        k[i][j] = pack_bf16x2(fmaf(x0, cs.x, -(x1 * cs.y)), fmaf(x0, cs.y, x1 * cs.x));
+      for (int i = 0; i < 4; ++i) {
+        const int32_t tok = min(t0 + k_token(i0 + i) + (lane >> 4), g.tpp - 1);
+        const int32_t hh = (int32_t)fast_div((uint32_t)tok, g.gw_div), ww = tok - hh * g.grid_w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) cs[i][j] = g.table[base[j] + (ax[j] == 0 ? 0 : ax[j] == 1 ? hh * g.pairs_h : ww * g.pairs_w)];
       }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool there = k_token(i0 + i) + (lane >> 4) < left;  // behind the page's end zeros stay +0
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t w = k[i0 + i][j];
+          const float x0 = __uint_as_float(w << 16), x1 = __uint_as_float(w & 0xffff0000u);
+          // as the bf16 cache rotates and rounds them
+          const uint32_t y = pack_bf16x2(fmaf(x0, cs[i][j].x, -(x1 * cs[i][j].y)), fmaf(x0, cs[i][j].y, x1 * cs[i][j].x));
+          k[i0 + i][j] = there ? y : 0u;
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
-  uint32_t kw[2] = {0, 0};
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t s = fp4_scale(quad_max(umax(umax(bf16x2_top(k[i][0]), bf16x2_top(k[i][1])),
-                                               umax(bf16x2_top(k[i][2]), bf16x2_top(k[i][3])))));
-    *reinterpret_cast<uint32_t*>(block + (16 * (i >> 2) + 4 * (i & 3) + (lane >> 4)) * 64 + (lane & 15) * 4) = fp4_codes(k[i], s);
-    kw[i >> 2] |= s << (8 * (i & 3));
-  }
-  if ((lane & 3) == 0) {
-    char* ks = block + kFp4KScale + (lane >> 4) * 16 + (lane >> 2 & 3) * 4;
-    *reinterpret_cast<uint32_t*>(ks) = kw[0];
-    *reinterpret_cast<uint32_t*>(ks + 64) = kw[1];
-  }
+  pack_keys(k, block, lane);
   char* stage = lds[wave];
 #pragma unroll
   for (int j = 0; j < 8; ++j) {  // channel c = 8 (lane & 15) + j
@@ -246,8 +271,10 @@ __global__ __launch_bounds__(256) void fp4_append_kernel(AppendArgs g, int32_t i
       x[e] = sel ? (a >> 16) | (c & 0xffff0000u) : (a & 0xffffu) | (c << 16);
       top = umax(top, bf16x2_top(x[e]));
     }
-    top = umax(top, (uint32_t)__shfl_xor((int)top, 16));
-    top = umax(top, (uint32_t)__shfl_xor((int)top, 32));
+    u32x2 other = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(top, top, false, false));
+    top = umax(other[0], other[1]);
+    other = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(top, top, false, false));
+    top = umax(other[0], other[1]);
     const uint32_t s = fp4_scale(top), c = 8 * (lane & 15) + j;
     *reinterpret_cast<uint32_t*>(stage + c * 16 + 4 * (lane >> 4)) = fp4_codes(x, s);
     if (lane < 16) stage[2048 + (c & 15) * 8 + (c >> 4)] = (char)s;
