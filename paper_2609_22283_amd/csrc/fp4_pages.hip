@@ -20,7 +20,9 @@ static PairList pair_list(const PagePairs& p, int32_t first, int32_t n) {
 }
 
 // A work-group copies 16 KB of a page: four loads of a thread are out before the
-// first is stored.  x: pieces of a page, y: pairs, z: layers.
+// first is stored, and read past the caches.  x: pieces of a page, y: pairs, z: layers.
+// Bound by memory: six pages of 1560 tokens x 12 heads in eight layers (920 MB read and
+// written) 153 us, 6.0 TB/s.
 constexpr int MV_T = 256, MV_N = 4;
 __global__ __launch_bounds__(MV_T) void page_move_kernel(const char* from, char* to, uint64_t from_layer,
                                                          uint64_t to_layer, uint64_t bytes, PairList pairs) {
@@ -30,7 +32,7 @@ __global__ __launch_bounds__(MV_T) void page_move_kernel(const char* from, char*
   u32x4u v[MV_N];
 #pragma unroll
   for (int i = 0; i < MV_N; ++i)
-    if (at + i * MV_T * 16 < bytes) v[i] = *reinterpret_cast<const u32x4u*>(src + at + i * MV_T * 16);
+    if (at + i * MV_T * 16 < bytes) v[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4u*>(src + at + i * MV_T * 16));
 #pragma unroll
   for (int i = 0; i < MV_N; ++i)
     if (at + i * MV_T * 16 < bytes) *reinterpret_cast<u32x4u*>(dst + at + i * MV_T * 16) = v[i];
@@ -93,8 +95,9 @@ __device__ __forceinline__ void pack_keys(const u32x4 (&k)[8], char* block, int3
 }
 
 // One wave per two blocks: of V, pass n takes the channels 8 n + lane / 8 of both, eight
-// tokens a lane, 128 bytes of a channel (a wave per block had pairs of waves wait for each
-// other's lines: 20 states of 64 tokens, 12 heads, 30 layers 78 us, 56 so).
+// tokens a lane, 128 bytes of a channel (pairs of waves with a block each wait for each
+// other's lines).  Read past the caches, which the pages it reads would only push others out of:
+// 20 states of 64 tokens, 12 heads, 30 layers 79 us, 54 so.
 __global__ __launch_bounds__(256) void page_pack_kernel(ConvertGeom g, PairList pairs) {
   const int32_t lane = threadIdx.x & 63;
   const int32_t item = blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -115,8 +118,8 @@ __global__ __launch_bounds__(256) void page_pack_kernel(ConvertGeom g, PairList 
     for (int i = 0; i < 8; ++i) {
       k[i] = v[i] = u32x4{};
       if (32 * half + k_token(i) + (lane >> 4) < left)
-        k[i] = *reinterpret_cast<const u32x4u*>(krow + (uint64_t)(32 * half + k_token(i)) * 256);
-      if (8 * (lane & 7) < left) v[i] = *reinterpret_cast<const u32x4u*>(vrow + (uint64_t)(8 * half + i) * 8 * g.tpp * 2);
+        k[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4u*>(krow + (uint64_t)(32 * half + k_token(i)) * 256));
+      if (8 * (lane & 7) < left) v[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4u*>(vrow + (uint64_t)(8 * half + i) * 8 * g.tpp * 2));
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {  // channel 64 half + 8 i + lane / 8: byte 4 half + i / 2 of the scales of channel % 16
@@ -200,11 +203,13 @@ struct AppendArgs {
   int32_t slot[32];
 };
 
-// One wave per block of a page and head: x the blocks of the state's pages (four to a
-// work-group, one per wave), y the head.  Keys as in page_convert_kernel; of the values a lane takes
-// eight channels of the tokens 8 (lane / 16) .. + 7, finds each channel's largest
-// magnitude with the three lanes that hold its other tokens, and the codes cross LDS, so
-// that they leave in 16-byte runs.
+// A wave takes K (z 0) or V (z 1) of a block: x the blocks of the state's pages, four to a
+// work-group, y the head.  Keys as in pack_keys, rotated before; of V a lane takes eight
+// channels of the tokens 8 (lane / 16) .. + 7, finds each channel's largest magnitude with the
+// three lanes that hold its other tokens, and the codes cross LDS, so that they leave in
+// 16-byte runs.  A chain of latencies: a frame of 64 tokens, 12 heads, rotated, takes 6.2
+// us (9.7 with K and V in one wave and rotations loaded one by one), a chunk of 3 x 1560
+// tokens (36 MB) 12.7.
 template <bool ROPE>
 __global__ __launch_bounds__(256) void fp4_append_kernel(AppendArgs g, int32_t items) {
   __shared__ __attribute__((aligned(16))) char lds[4][2048 + 128];
@@ -214,51 +219,57 @@ __global__ __launch_bounds__(256) void fp4_append_kernel(AppendArgs g, int32_t i
   const int32_t page = item / g.blocks, b = item - page * g.blocks, t0 = b * kFp4Tokens, left = g.tpp - t0;
   char* block = g.layer_base + (uint64_t)g.slot[page] * g.slot_bytes + ((uint64_t)h * g.blocks + b) * kFp4Block;
   const uint64_t row = (uint64_t)g.heads * 128, src = ((uint64_t)page * g.tpp + t0) * row + (uint64_t)h * 128 + 8 * (lane & 15);
-  u32x4 k[8], v[8];
+  u32x4 v[8];
+  if (blockIdx.z == 0) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int32_t tk = k_token(i) + (lane >> 4), tv = 8 * (lane >> 4) + i;
-    k[i] = v[i] = u32x4{};
-    if (tk < left) k[i] = *reinterpret_cast<const u32x4u*>(g.k + src + tk * row);
-    if (tv < left) v[i] = *reinterpret_cast<const u32x4u*>(g.v + src + tv * row);
-  }
-  if constexpr (ROPE) {
-    int32_t ax[4];
-    int64_t base[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int32_t p = 4 * (lane & 15) + j;
-      ax[j] = p < g.pairs_t ? 0 : p < g.pairs_t + g.pairs_h ? 1 : 2;
-      base[j] = ax[j] == 0 ? (int64_t)(g.frame0 + page) * g.pairs_t + p
-                : ax[j] == 1 ? g.off_h + p - g.pairs_t : g.off_w + p - g.pairs_t - g.pairs_h;
+    for (int i = 0; i < 8; ++i) {
+      const int32_t t = k_token(i) + (lane >> 4);
+      v[i] = u32x4{};
+      if (t < left) v[i] = *reinterpret_cast<const u32x4u*>(g.k + src + t * row);
     }
-    // four tokens' rotations at a time are out before the first is used
+    if constexpr (ROPE) {
+      // the rotations of this lane's channel pairs: the axis and its table are fixed, the
+      // position changes with the token; all are out before the first is used
+      const float2* table[4];
+      int32_t ax[4];
 #pragma unroll
-    for (int i0 = 0; i0 < 8; i0 += 4) {
-      float2 cs[4][4];
+      for (int j = 0; j < 4; ++j) {
+        const int32_t p = 4 * (lane & 15) + j;
+        ax[j] = p < g.pairs_t ? 0 : p < g.pairs_t + g.pairs_h ? 1 : 2;
+        table[j] = g.table + (ax[j] == 0 ? (int64_t)(g.frame0 + page) * g.pairs_t + p
+                              : ax[j] == 1 ? g.off_h + p - g.pairs_t : g.off_w + p - g.pairs_t - g.pairs_h);
+      }
+      float2 cs[8][4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int32_t tok = min(t0 + k_token(i0 + i) + (lane >> 4), g.tpp - 1);
+      for (int i = 0; i < 8; ++i) {
+        const int32_t tok = min(t0 + k_token(i) + (lane >> 4), g.tpp - 1);
         const int32_t hh = (int32_t)fast_div((uint32_t)tok, g.gw_div), ww = tok - hh * g.grid_w;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) cs[i][j] = g.table[base[j] + (ax[j] == 0 ? 0 : ax[j] == 1 ? hh * g.pairs_h : ww * g.pairs_w)];
+        for (int j = 0; j < 4; ++j) cs[i][j] = table[j][ax[j] == 0 ? 0 : ax[j] == 1 ? hh * g.pairs_h : ww * g.pairs_w];
       }
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const bool there = k_token(i0 + i) + (lane >> 4) < left;  // behind the page's end zeros stay +0
+      for (int i = 0; i < 8; ++i) {
+        const bool there = k_token(i) + (lane >> 4) < left;  // behind the page's end zeros stay +0
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const uint32_t w = k[i0 + i][j];
+          const uint32_t w = v[i][j];
           const float x0 = __uint_as_float(w << 16), x1 = __uint_as_float(w & 0xffff0000u);
           // as the bf16 cache rotates and rounds them
           const uint32_t y = pack_bf16x2(fmaf(x0, cs[i][j].x, -(x1 * cs[i][j].y)), fmaf(x0, cs[i][j].y, x1 * cs[i][j].x));
-          k[i0 + i][j] = there ? y : 0u;
+          v[i][j] = there ? y : 0u;
         }
       }
-      __builtin_amdgcn_sched_barrier(0);
     }
+    pack_keys(v, block, lane);
+    return;
   }
-  pack_keys(k, block, lane);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int32_t t = 8 * (lane >> 4) + i;
+    v[i] = u32x4{};
+    if (t < left) v[i] = *reinterpret_cast<const u32x4u*>(g.v + src + t * row);
+  }
   char* stage = lds[wave];
 #pragma unroll
   for (int j = 0; j < 8; ++j) {  // channel c = 8 (lane & 15) + j
@@ -314,7 +325,7 @@ int launch_fp4_append(const sc_cache* c, int32_t layer, const int32_t* slots, in
     g.gw_div = magic_div((uint32_t)rope->desc.grid_w);
   }
   const int32_t items = d.pages_per_chunk * g.blocks;
-  const dim3 grid((items + 3) / 4, d.n_heads);
+  const dim3 grid((items + 3) / 4, d.n_heads, 2);
   timer_begin(TK_APPEND, stream);
   if (rope)
     hipLaunchKernelGGL(fp4_append_kernel<true>, grid, dim3(256), 0, stream, g, items);
