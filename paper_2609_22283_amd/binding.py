@@ -227,12 +227,18 @@ def _ptr(x) -> Optional[int]:
     return x.data_ptr()
 
 
+# torch's current stream of a device as an integer, without the stream object that
+# torch.cuda.current_stream() makes (4 us of a call of 8)
+_raw_stream = getattr(getattr(_torch, "_C", None), "_cuda_getCurrentRawStream", None)
+
+
 def _stream(s) -> Optional[int]:
     if s is None:
         try:
-            import torch
-            if torch.cuda.is_initialized():
-                return torch.cuda.current_stream().cuda_stream
+            if _torch.cuda.is_initialized():
+                if _raw_stream is not None:
+                    return _raw_stream(_torch.cuda.current_device())
+                return _torch.cuda.current_stream().cuda_stream
         except Exception:
             pass
         return None
@@ -453,21 +459,24 @@ def sc_rope_table_build(table, grid_h, grid_w, dims, max_frames, theta=10000.0, 
     return Rope(d, table)
 
 
+_ROTATED = {} if _torch is None else {_torch.bfloat16: SC_DTYPE_BF16, _torch.float32: SC_DTYPE_F32}
+
+
 def sc_rope_rotate(rope: Rope, x, y, positions, layout: str = "interleaved", transpose: bool = False,
                    stream=None) -> None:
     """Rotate the rows of ``x`` [rows, heads, head_dim] (bf16 or fp32, any strides between rows
     and heads) at ``positions`` (int32 [rows, 3]) into ``y``, of the same shape and dtype; ``y``
     may be ``x``."""
-    import torch
-    codes = {torch.bfloat16: SC_DTYPE_BF16, torch.float32: SC_DTYPE_F32}
-    if (x.dim() != 3 or y.shape != x.shape or x.dtype not in codes or y.dtype != x.dtype or
-            (x.numel() and (x.stride(2) != 1 or y.stride(2) != 1) and x.shape[2] != 1) or layout not in ROPE_LAYOUTS):
+    dtype = _ROTATED.get(x.dtype)
+    xs, ys, shape = x.stride(), y.stride(), x.shape
+    if (len(xs) != 3 or y.shape != shape or dtype is None or y.dtype != x.dtype or
+            (x.numel() and (xs[2] != 1 or ys[2] != 1) and shape[2] != 1) or layout not in ROPE_LAYOUTS):
         raise ScError(SC_EINVAL, "SC_EINVAL: x and y are [rows, heads, head_dim] of one dtype (bf16, fp32) with adjacent "
                                  f"channels, the layout one of {sorted(ROPE_LAYOUTS)}")
-    if tuple(positions.shape) != (x.shape[0], 3) or positions.dtype != torch.int32 or not positions.is_contiguous():
+    if tuple(positions.shape) != (shape[0], 3) or positions.dtype != _torch.int32 or not positions.is_contiguous():
         raise ScError(SC_EINVAL, "SC_EINVAL: positions are contiguous int32 [rows, 3]")
-    d = sc_rotate_desc(x.shape[0], x.shape[1], x.shape[2], codes[x.dtype], ROPE_LAYOUTS[layout], 1 if transpose else 0,
-                       x.stride(0), x.stride(1), y.stride(0), y.stride(1))
+    d = sc_rotate_desc(shape[0], shape[1], shape[2], dtype, ROPE_LAYOUTS[layout], 1 if transpose else 0,
+                       xs[0], xs[1], ys[0], ys[1])
     _check(lib.sc_rope_rotate(C.byref(rope.struct), C.byref(d), _ptr(x), _ptr(y), _ptr(positions), _stream(stream)))
 
 
