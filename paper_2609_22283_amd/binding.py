@@ -10,7 +10,6 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-import weakref
 from typing import List, Optional, Sequence, Tuple
 
 __all__ = [
@@ -342,8 +341,7 @@ class Cache:
     def __init__(self, handle, desc, pool):
         self._h = C.c_void_p(handle)
         self.desc = desc
-        self.pool = pool  # keeps the caller's buffer alive
-        self._family = weakref.WeakSet([self])  # the handles over this pool
+        self._held = [pool]  # keeps the caller's buffer alive; one list and one desc for a cache and its forks
 
     def __del__(self):
         if getattr(self, "_h", None) and self._h.value:
@@ -353,6 +351,10 @@ class Cache:
     @property
     def handle(self):
         return self._h
+
+    @property
+    def pool(self):
+        return self._held[0]
 
     def contains(self, state, layer: int = -1) -> bool:
         return bool(_check(lib.sc_cache_contains(self._h, sc_node(*state), layer)))
@@ -400,8 +402,7 @@ class Cache:
         out = C.c_void_p()
         _check(lib.sc_cache_fork(self._h, C.byref(out)))
         f = Cache(out.value, self.desc, self.pool)
-        f._family = self._family
-        self._family.add(f)
+        f._held = self._held
         return f
 
     def compact(self, weights=None, stream=None) -> None:
@@ -412,10 +413,8 @@ class Cache:
         """Move the pages of this cache and its forks to ``pool``, of ``n_slots`` slots, in the order
         of their slots (and the rows of ``weights`` to ``moved_weights``)."""
         _check(lib.sc_cache_move(self._h, _ptr(pool), n_slots, _ptr(weights), _ptr(moved_weights), _stream(stream)))
-        for c in self._family:
-            d = c.desc
-            c.pool = pool
-            c.desc = _desc(d.n_layers, d.n_heads, d.head_dim, d.tokens_per_page, d.pages_per_chunk, n_slots, d.dtype)
+        self._held[0] = pool
+        self.desc.n_slots = n_slots
 
 
 def sc_cache_create(pool, n_layers, n_heads, head_dim, tokens_per_page, pages_per_chunk, n_slots,
