@@ -28,7 +28,7 @@ struct Fp4Geom {
   uint64_t slot_bytes;
   int32_t heads, nodes, tpp, blocks, nq, rows;
   DivMagic blocks_div, nq_div;
-  float unit;       // |scale| log2(e), no less than FLT_MIN
+  float unit;       // |scale| log2(e), a normal number
   uint32_t q_flip;  // sign bits of a negative scale
   // The items, first those of the prefix (none where the nodes read it by themselves, joined),
   // then the nodes' own: row tiles fastest, then heads, then (own) nodes, then pieces of so many
@@ -62,7 +62,7 @@ static void fp4_fill(const sc_plan* p, const sc_cache* c, int32_t layer, float s
   g.nq = p->nq;
   g.blocks_div = magic_div((uint32_t)g.blocks);
   g.nq_div = magic_div((uint32_t)p->nq);
-  g.unit = std::max(std::fabs(scale) * 1.4426950408889634f, FLT_MIN);
+  g.unit = std::min(std::max(std::fabs(scale) * 1.4426950408889634f, FLT_MIN), FLT_MAX);
   g.q_flip = std::signbit(scale) ? 0x80008000u : 0u;
 }
 
@@ -610,7 +610,7 @@ static Fp4Schedule find_fp4_schedule(const sc_plan* p, const sc_cache* c, size_t
   return best;
 }
 
-// Found once per plan, for the few rooms that its calls ask for.
+// Found once per plan, for any room, the no-allocation call's and a block's.
 static const Fp4Schedule* fp4_schedule(const sc_plan* p, const sc_cache* c, size_t room) {
   for (const auto& s : p->fp4)
     if (s->room == room) return s.get();
