@@ -16,6 +16,7 @@
 namespace sc {
 
 constexpr int kFp4Nodes = 64, kFp4Pages = 800;  // of a plan (attention_check)
+constexpr int64_t kFp4Groups = UINT32_MAX / 256;  // work-groups of a launch (256 threads each, numbered in 32 bits)
 
 // A plan's pages: the prefix that all nodes read first, then the nodes' own.
 struct Fp4List {
@@ -470,8 +471,9 @@ static int64_t fp4_chunks(const sc_cache* c, int64_t pages) {
   return (pages * fp4_blocks(c->d.tokens_per_page) + 3) / 4;
 }
 
-// NULL where the bf16 kernels do not take the plan.
+// NULL where the bf16 kernels do not take the plan (their pages hold a key tile).
 static std::shared_ptr<Fp4Wide> fp4_wide(const sc_plan* p, const sc_cache* c) {
+  if (c->d.tokens_per_page < (p->shared || p->nq <= 64 ? 32 : 64)) return nullptr;
   auto w = std::make_shared<Fp4Wide>();
   std::map<int32_t, int32_t> place;
   for (int32_t s : p->page_slot)
@@ -578,7 +580,7 @@ static Fp4Schedule find_fp4_schedule(const sc_plan* p, const sc_cache* c, size_t
           s.p_pieces = (int32_t)((prefix + p_len - 1) / p_len);
         }
         const int64_t all = s.p_pieces + s.o_pieces;
-        if (all > 1 && (double)all * piece > (double)room) break;
+        if (all > 1 && ((double)all * piece > (double)room || rows > 4 * kFp4Groups)) break;
         s.bytes = all > 1 ? (size_t)(all * piece) : 0;
         items.clear();
         double total = 0;
@@ -589,7 +591,7 @@ static Fp4Schedule find_fp4_schedule(const sc_plan* p, const sc_cache* c, size_t
         };
         if (!joined) add((double)p_tiles, prefix, p_len);
         for (const auto& o : own) add((double)own_tiles * o.second, fp4_chunks(c, o.first + (joined ? p->shared : 0)), o_len);
-        if (total > INT32_MAX / 2) continue;
+        if (total > (double)kFp4Groups) continue;
         const int32_t per = total <= kCUs ? 1 : total <= 2 * kCUs || tile == 32 ? 2 : 3;  // work-groups to a CU
         const double step = tile == 16 ? (per == 1 ? 1.36 : per == 2 ? 2.0 : 3.0) : (per == 1 ? 2.3 : 3.8);
         for (Fp4Items& i : items) i.us = i.us * step + 1.0;
@@ -659,7 +661,7 @@ int launch_fp4_attention(const sc_plan* p, const sc_cache* c, int32_t layer, con
     g.p_items = g.p_tiles * g.heads * g.p_pieces;
   }
   const int64_t items = (int64_t)g.p_items + (int64_t)g.o_tiles * g.heads * g.nodes * s->o_pieces;
-  if (items > INT32_MAX) return fail(SC_EUNSUPPORTED, "%lld query tiles", (long long)items);
+  if (items > kFp4Groups) return fail(SC_EUNSUPPORTED, "%lld query tiles", (long long)items);
   if (s->bytes) {
     g.part_o = static_cast<float*>(ws);
     g.part_ml = g.part_o + (size_t)(g.p_pieces + s->o_pieces) * g.heads * g.rows * 128;

@@ -192,7 +192,8 @@ int launch_page_convert(bool pack, const PoolView& from, const PoolView& to, con
 int launch_fp4_append(const sc_cache* cache, int32_t layer, const int32_t* slots, int32_t chunk, const void* k,
                       const void* v, const sc_rope* rope, hipStream_t stream);
 
-// Launchers of attention_fp4.hip (their meaning as of those without the name, internal.h).
+// Launchers of attention_fp4.hip: the attention over 4-bit pages.  attention_check has accepted
+// the plan.
 size_t fp4_attention_workspace_bytes(const sc_plan* plan, const sc_cache* cache);
 // The cheapest way within `room` bytes at ws.
 int launch_fp4_attention(const sc_plan* plan, const sc_cache* cache, int32_t layer, const void* q, void* o, float scale,

@@ -85,9 +85,10 @@ template <> struct RotRun<float> {
 
 // A thread takes a run of pairs (of 16 bytes of channels; HALF: 16 bytes of either half) of one
 // row in HP heads, or a run of copied channels.  The row's cosines and sines are read
-// once for the heads, whose loads are all out before the first is used.  Bound by memory
-// where there are many rows: four nodes of 4680 rows of 12 x 128 channels (115 MB) 26 us, 57
-// with a pair a thread; by latency at few.
+// once for the heads, whose loads are all out before the first is used, and read past the
+// caches, which y gets.  Bound by memory where there are many rows: four nodes of 4680 rows of
+// 12 x 128 channels (115 MB) 24.6 us, 4.7 TB/s, as a plain copy runs (27.7 with loads that stay in the
+// caches, 25.7 with stores past them too, 57 with a pair a thread); by latency at few.
 template <class T, bool HALF, int HP>
 __global__ __launch_bounds__(256) void rotate_kernel(const T* x, T* y, RotateArgs g) {
   using Run = RotRun<T>;
@@ -109,8 +110,8 @@ __global__ __launch_bounds__(256) void rotate_kernel(const T* x, T* y, RotateArg
 #pragma unroll
     for (int j = 0; j < HP; ++j) {
       const T* from = xr + min(h0 + j, g.heads - 1) * g.x_head;
-      a[j] = *reinterpret_cast<const V*>(from);
-      if (HALF && pairs) b[j] = *reinterpret_cast<const V*>(from + g.half);
+      a[j] = __builtin_nontemporal_load(reinterpret_cast<const V*>(from));
+      if (HALF && pairs) b[j] = __builtin_nontemporal_load(reinterpret_cast<const V*>(from + g.half));
     }
   if (!pairs) {
 #pragma unroll
