@@ -300,8 +300,9 @@ int sc_plan_condition(sc_cache* cache, const sc_node* conditions, int32_t n, int
  * sc_attention_workspace_bytes(plan, cache) bytes (may be NULL when that is
  * 0, as for fp32 caches unless the nodes share a prefix); the bf16 kernel splits
  * long key ranges across work-groups and merges their partial softmax sums
- * there, and so does any that reads a shared prefix once.  Its contents are
- * undefined on return; calls sharing one workspace must be ordered on one
+ * there, and so does any that reads a shared prefix once; over a 4-bit cache long nodes have
+ * their distinct pages of the layer taken out there as bf16 and read by the bf16 forms.
+ * Its contents are undefined on return; calls sharing one workspace must be ordered on one
  * stream.  Errors: SC_ESTALE, SC_EUNAVAILABLE (a page's state not written at
  * this layer), SC_EINVAL (workspace too small or misaligned), SC_EUNSUPPORTED,
  * SC_EDEVICE. */

@@ -28,7 +28,8 @@ extern "C" {
  * (the projections of sc_condition_append), "row_scale" (no launch of its
  * own any more: always 0), "attention_weigh" (the keys' weights, after the
  * attention, and in small calls the merge of its partials), "condense" (the launches
- * of a fold).  A projection's time includes the launch that adds
+ * of a fold), "pages" (pages copied, moved, packed into 4 bits or taken out of them),
+ * "rotate" (sc_rope_rotate).  A projection's time includes the launch that adds
  * the parts of a split contraction.  Enabling clears earlier records.  Events
  * are created lazily and reused; the cost is two event records per launch. */
 int sc_timer_enable(int on);
@@ -39,7 +40,8 @@ int sc_timer_read(const char* kind, int32_t* launches, double* total_ms);
  * test or a benchmark can say which one it covers.
  * sc_attention_form: sc_attention with the plan's workspace.  *queries:
  * query rows per work-group (bf16: 32 with a node's keys split over the waves,
- * 64, 128 or 256 with a unit's keys in order; fp32: 16); *ring: K/V tiles in
+ * 64, 128 or 256 with a unit's keys in order; fp32: 16; 4-bit: 16 or 32, or 0 where the pages are first
+ * taken out as bf16, by whose forms the plan then runs); *ring: K/V tiles in
  * the LDS ring of a unit form, else 1; *pieces: key-range pieces that each
  * unit of the last round is cut into (1: none).  A plan of sc_plan_share that
  * reads its prefix once for all rows has minus the pieces of the prefix there.

@@ -2,6 +2,15 @@
 //
 // For every pack node i and head h: O = softmax(Q K^T * scale) V over the keys of node i's
 // pages, K and V the values that the codes stand for; q and o are bf16.
+//
+// The scaled matrix instructions take codes and their shared scales as a block holds them
+// (fp4.h), so K and V are never taken apart: S^T = K Q^T and O^T = V^T P^T have them as the A
+// operand, over 128 channels of four scales and over 128 keys of four blocks.  The other
+// operand comes in 8 bits at most.  A bf16 number has 8 significant bits, which are two e4m3
+// numbers of 4: q is split once per row, the exponentials of a chunk where they are made, and each
+// product is two instructions, which is what 128 channels of bf16 cost as well (64 cycles of
+// the matrix core), but without the codes' conversion, and over a quarter of the bytes in
+// cache and registers.
 #include <algorithm>
 #include <cfloat>
 #include <climits>
@@ -75,7 +84,7 @@ constexpr int FA_NW = 4;      // waves of a work-group
 constexpr float kFp4Rise = 40.f;  // sums of 2^31 keys in units of 2^m stay below 2^(40 + 31)
 constexpr int FA_ROW = 132;   // floats of a row of partial outputs in LDS
 
-// c + A B over 128: A 16 rows of codes (a lane: row lane % 16, the 32 columns of group lane / 16)
+// The scaled instruction's operands: c + A B over 128: A 16 rows of codes (a lane: row lane % 16, the 32 columns of group lane / 16)
 // whose scales are byte SA of the lanes' sa, B 16 columns of e4m3 (a lane: column lane % 16, rows 16 g ..
 // + 15 and 64 + 16 g .. + 15 with g = lane / 16), in two parts with their scales in the first two
 // bytes of sb.
@@ -98,7 +107,9 @@ __device__ __forceinline__ float quarters_max(float x) {
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 // Four fp32 numbers of at most 448 as e4m3, and what that leaves of them, over `unit` (a power of
-// two), in e4m3 again: 8 significant bits together, which is all that bf16 has.
+// two), in e4m3 again: 8 significant bits together, which is all that bf16 has, and half a step
+// 2^-9 of the number.  One e4m3 number alone (half a step 2^-4) would take half of the
+// products, and leave outputs with the error of a format that the caller did not choose.
 // x, y: any two values that are not needed any more (the conversions write half a register at
 // a time, and would have one cleared first).
 __device__ __forceinline__ void split_e4m3(float a, float b, float c, float d, float unit, float x, float y, int& hi, int& lo) {
@@ -177,6 +188,21 @@ __device__ __forceinline__ Fp4Item fp4_item(const Fp4Geom& g, const Fp4List& lis
   return it;
 }
 
+// A work-group has 16 R rows of a head; its four waves take every fourth chunk of 128 keys,
+// each with a softmax of its own (running power of two, sums, outputs), and join the four in
+// LDS at the end.  Nothing is shared between the waves' loops, so there is no barrier in them:
+// K and V go from the cache straight to the registers that the products read, K of the next
+// chunk under the exponentials of this one, V in K's registers.  The rows' sums come from one
+// more product, with ones, which has the exponentials as they were rounded.
+//
+// What bounds it: single tokens, reading the pages (16 x 16384 keys x 12 heads, 428 MB, 72.8
+// us, 5.9 TB/s); many rows, the vector unit, busy for 75 % of the time with 28 cycles for
+// each exponential and its two parts and 16 for each of the products' issue, the matrix core for
+// half of it (four nodes of 4680 rows over 21 x 1560 keys 3.32 ms, 1136 TFLOP/s, in tiles of 32 rows:
+// the products of one half of the rows stand between the exponentials of the other; 3.52 ms and
+// 1071 in tiles of 16, whose work-groups are three to a CU).  Tried on the same nodes: 32x32x64
+// products of 64 keys 3.66 ms, with their loads further ahead 3.71; the waves on rows of their own, 128 in all, over the same keys 3.25, but slower at
+// every shorter one (58 us become 144 at four nodes of 256 rows).
 template <int R>
 __global__ __launch_bounds__(64 * FA_NW, R == 1 ? 3 : 2) void fp4_attention_kernel(const uint16_t* __restrict__ q, uint16_t* __restrict__ o,
                                                                       Fp4Geom g, Fp4List list) {
@@ -409,7 +435,8 @@ __global__ __launch_bounds__(64 * FA_NW, R == 1 ? 3 : 2) void fp4_attention_kern
 }
 
 // A wave per row and head joins the pieces that its node has, the prefix's and its own, N at
-// a time, whose loads are independent.
+// a time, whose loads are independent.  Bound by latency, then by the partials: 4 us for 256
+// rows of 12 heads in four pieces (6.4 MB).
 template <int N>
 __global__ __launch_bounds__(256) void fp4_combine_kernel(uint16_t* __restrict__ o, Fp4Geom g, Fp4List list) {
   const int32_t lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6), h = blockIdx.y;
@@ -542,7 +569,8 @@ static double fp4_makespan(double slots, const std::vector<Fp4Items>& items) {
 // read a shared prefix each by itself (sixteen of 16 rows over 128 x 128 keys 38 us, 49 with
 // the rows of all nodes in one matrix; 32 of one row over 256 x 64 keys 26 against 20).
 // Over bf16 pages: the time of that attention, 8 and 0.17 per MB of them (four nodes of 4680
-// rows over 21 x 1560 keys 3.02 ms, 3.36 by tiles; four of 256 over 21 x 256 59 us, 41 by tiles).
+// rows over 21 x 1560 keys 2.94 to 3.07 ms, 3.32 by tiles; four of 256 over 21 x 256 59 us, 41 by
+// tiles): 32 rows read K and V from cache once, 256 of the bf16 form's eight waves.
 static Fp4Schedule find_fp4_schedule(const sc_plan* p, const sc_cache* c, size_t room) {
   const int32_t n = (int32_t)p->nodes.size(), H = c->d.n_heads;
   const int64_t rows = (int64_t)n * p->nq;
