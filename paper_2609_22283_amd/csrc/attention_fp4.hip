@@ -110,10 +110,11 @@ __device__ __forceinline__ float quarters_max(float x) {
 // two), in e4m3 again: 8 significant bits together, which is all that bf16 has, and half a step
 // 2^-9 of the number.  One e4m3 number alone (half a step 2^-4) would take half of the
 // products, and leave outputs with the error of a format that the caller did not choose.
-// x, y: any two values that are not needed any more (the conversions write half a register at
-// a time, and would have one cleared first).
-__device__ __forceinline__ void split_e4m3(float a, float b, float c, float d, float unit, float x, float y, int& hi, int& lo) {
-  int h = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, (int)__float_as_uint(x), false);
+__device__ __forceinline__ void split_e4m3(float a, float b, float c, float d, float unit, int& hi, int& lo) {
+  int h, y;  // the conversions write half a register at a time: whatever is in it first
+  asm volatile("" : "=v"(h));
+  asm volatile("" : "=v"(y));
+  h = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, h, false);
   h = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, h, true);
   const f32x2 ab = __builtin_amdgcn_cvt_pk_f32_fp8(h, false), cd = __builtin_amdgcn_cvt_pk_f32_fp8(h, true);
   i16x2 l = __builtin_bit_cast(i16x2, y);
@@ -153,7 +154,7 @@ __device__ __forceinline__ Fp4Rows load_rows(const uint16_t* row, int32_t quarte
     const uint32_t a = v[i >> 1][2 * (i & 1)], b = v[i >> 1][2 * (i & 1) + 1];
     int h, l;
     split_e4m3(__uint_as_float(a << 16) * by, __uint_as_float(a & 0xffff0000u) * by, __uint_as_float(b << 16) * by,
-               __uint_as_float(b & 0xffff0000u) * by, unit, 0.f, 0.f, h, l);
+               __uint_as_float(b & 0xffff0000u) * by, unit, h, l);
     r.hi[i] = e == 255u ? 0 : h;
     r.lo[i] = e == 255u ? 0 : l;
   }
@@ -332,7 +333,7 @@ __global__ __launch_bounds__(64 * FA_NW, R == 1 ? 3 : 2) void fp4_attention_kern
 #pragma unroll
         for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], g.unit, shift));
         int h, l;
-        split_e4m3(p[0], p[1], p[2], p[3], 0.0625f, s[b][0], s[b][1], h, l);
+        split_e4m3(p[0], p[1], p[2], p[3], 0.0625f, h, l);
         asm volatile("" : "+v"(h), "+v"(l));  // here, and not where the products need them
         hi[r][b] = h;
         lo[r][b] = l;
