@@ -45,8 +45,8 @@ T_SCHEDULE_K4 = (0.0, 5.0 / 8.0, 5.0 / 6.0, 15.0 / 16.0, 1.0)
 # FETCH_SIZE and WRITE_SIZE per dispatch, scaled by what the same counters
 # read for a plain 256 MiB copy (x2.0 fetch, x1.0 write).  Valid only for the
 # kernel sources it was measured on (hash below); otherwise reported as null.
-ATTN_TRAFFIC = {"sources_sha1": "316fc25169c6ec43e8d43aeecaa9218e064c2c59",
-                "fetch_bytes": 1.3477e+09, "write_bytes": 1.9880e+08}
+ATTN_TRAFFIC = {"sources_sha1": "6fc4ffa7bbe8f687bf4e67cfcd194b6b692e7e48",
+                "fetch_bytes": 1.3510e+09, "write_bytes": 1.9880e+08}
 
 
 def attn_traffic():
