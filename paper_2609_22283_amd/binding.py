@@ -412,7 +412,10 @@ class Cache:
     def move(self, pool, n_slots: int, weights=None, moved_weights=None, stream=None) -> None:
         """Move the pages of this cache and its forks to ``pool``, of ``n_slots`` slots, in the order
         of their slots (and the rows of ``weights`` to ``moved_weights``)."""
-        _check(lib.sc_cache_move(self._h, _ptr(pool), n_slots, _ptr(weights), _ptr(moved_weights), _stream(stream)))
+        on, old = _stream(stream), self._held[0]
+        _check(lib.sc_cache_move(self._h, _ptr(pool), n_slots, _ptr(weights), _ptr(moved_weights), on))
+        if on and hasattr(old, "record_stream"):  # it may go back to torch's allocator here
+            old.record_stream(_torch.cuda.ExternalStream(on, device=old.device))
         self._held[0] = pool
         self.desc.n_slots = n_slots
 

@@ -114,7 +114,6 @@ void forks() {
   sc_cache_free(nullptr);
 }
 
-// A block over a fork's plan reads flags of slots, of states that the handle has given up too.
 void copies() {
   const sc_cache_desc d = desc(8), q = desc(6, SC_DTYPE_FP4);
   Pool pool(d), held(q);

@@ -221,3 +221,29 @@ def test_compact_and_move_on_the_gpu():
         assert c.desc.n_slots == f.desc.n_slots == n and c.pool is to
         w = w2
         holds(to, w, n)
+
+
+@pytest.mark.parametrize("given", [True, False])
+def test_the_pool_left_behind_is_not_reused_early(given):
+    """Moved on a busy stream: the old pool, which nothing else holds, is handed out again only behind
+    the move."""
+    heads, tpp, n = 2, 64, 40
+    args = (1, heads, D, tpp, 1, n, sc.SC_DTYPE_FP4)
+    size = sc.sc_cache_pool_bytes(*args)
+    torch.cuda.empty_cache()
+    c = sc.sc_cache_create(torch.empty(size, dtype=torch.uint8, device="cuda"), *args)
+    kd, _ = bf16_dev(normal((tpp, heads, D), (8, TAG_K)))
+    for i in range(n):
+        c.append(0, (i, 0), kd, kd)
+    want, to = c.pool.clone(), torch.zeros(size, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(100_000_000)
+        if not given:
+            c.move(to, n)
+    if given:
+        c.move(to, n, stream=s)
+    other = torch.zeros(size, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    assert torch.equal(to, want) and not bool(other.any())
