@@ -199,9 +199,9 @@ __device__ __forceinline__ Fp4Item fp4_item(const Fp4Geom& g, const Fp4List& lis
 // What bounds it: single tokens, reading the pages (16 x 16384 keys x 12 heads, 428 MB, 72.8
 // us, 5.9 TB/s); many rows, the vector unit, busy for 75 % of the time with 28 cycles for
 // each exponential and its two parts and 16 for each of the products' issue, the matrix core for
-// half of it (four nodes of 4680 rows over 21 x 1560 keys 3.32 ms, 1136 TFLOP/s, in tiles of 32 rows:
-// the products of one half of the rows stand between the exponentials of the other; 3.52 ms and
-// 1071 in tiles of 16, whose work-groups are three to a CU).  Tried on the same nodes: 32x32x64
+// half of it (four nodes of 4680 rows over 21 x 1560 keys 3.28 ms, 1148 TFLOP/s, in tiles of 32 rows:
+// the products of one half of the rows stand between the exponentials of the other; 3.54 ms and
+// 1064 in tiles of 16, whose work-groups are three to a CU).  Tried on the same nodes: 32x32x64
 // products of 64 keys 3.66 ms, with their loads further ahead 3.71; the waves on rows of their own, 128 in all, over the same keys 3.25, but slower at
 // every shorter one (58 us become 144 at four nodes of 256 rows).
 template <int R>
@@ -570,7 +570,7 @@ static double fp4_makespan(double slots, const std::vector<Fp4Items>& items) {
 // read a shared prefix each by itself (sixteen of 16 rows over 128 x 128 keys 38 us, 49 with
 // the rows of all nodes in one matrix; 32 of one row over 256 x 64 keys 26 against 20).
 // Over bf16 pages: the time of that attention, 8 and 0.17 per MB of them (four nodes of 4680
-// rows over 21 x 1560 keys 2.94 to 3.07 ms, 3.32 by tiles; four of 256 over 21 x 256 59 us, 41 by
+// rows over 21 x 1560 keys 2.94 to 3.07 ms, 3.28 by tiles; four of 256 over 21 x 256 59 us, 41 by
 // tiles): 32 rows read K and V from cache once, 256 of the bf16 form's eight waves.
 static Fp4Schedule find_fp4_schedule(const sc_plan* p, const sc_cache* c, size_t room) {
   const int32_t n = (int32_t)p->nodes.size(), H = c->d.n_heads;
