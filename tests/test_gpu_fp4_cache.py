@@ -247,3 +247,23 @@ def test_the_pool_left_behind_is_not_reused_early(given):
     other = torch.zeros(size, dtype=torch.uint8, device="cuda")
     torch.cuda.synchronize()
     assert torch.equal(to, want) and not bool(other.any())
+
+
+def test_copies_of_a_pool_aligned_to_its_elements():
+    heads, tpp, frames = 3, 56, 2
+    args = (1, heads, D, tpp, frames, frames, sc.SC_DTYPE_BF16)
+    size = sc.sc_cache_pool_bytes(*args)
+    bufs = [torch.full((size + 16,), 0x5a, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    src, out = (sc.sc_cache_create(b[2:size + 2], *args) for b in bufs)
+    _, held = make_cache(sc.SC_DTYPE_FP4, heads, tpp, frames, frames)
+    kd, k = bf16_dev(normal((tpp * frames, heads, D), (9, TAG_K)))
+    vd, v = bf16_dev(normal((tpp * frames, heads, D), (9, TAG_V)))
+    src.append(0, (0, 0), kd, vd)
+    src.copy([(0, 0)], held, [(0, 0)], 0, 1)
+    held.copy([(0, 0)], out, [(0, 0)], 0, 1)
+    torch.cuda.synchronize()
+    got = bf16_pages(bufs[1][2:size + 2].clone(), heads, tpp, frames)
+    want = _values(k, v, heads, tpp, frames)
+    np.testing.assert_array_equal(got[0][0], want[0])
+    np.testing.assert_array_equal(got[1][0], want[1])
+    assert bool((bufs[1][:2] == 0x5a).all()) and bool((bufs[1][size + 2:] == 0x5a).all())
