@@ -253,8 +253,8 @@ int sc_cache_compact(sc_cache* cache, float* weights, sc_stream stream);
  * Errors (nothing has changed): SC_EINVAL (null argument, n_slots < 1, overlapping pools or
  * weights, one of the weights without the other), SC_ECAPACITY (more slots in use),
  * SC_EDEVICE. */
-int sc_cache_move(sc_cache* cache, void* dev_pool, int32_t n_slots, const float* weights, float* moved_weights,
-                  sc_stream stream);
+int sc_cache_move(sc_cache* cache, void* dev_pool, int32_t n_slots, const float* weights,
+                  float* moved_weights, sc_stream stream);
 
 /* ---- Plan: availability and page lists (Eq. 6, Eq. 8) ------------------
  * Resolves every segment of the selection to page slots and checks
@@ -294,16 +294,17 @@ int sc_plan_condition(sc_cache* cache, const sc_node* conditions, int32_t n, int
  * no per-round host-to-device copy is needed); larger plans fail with
  * SC_EUNSUPPORTED before anything is launched.  bf16 caches need head_dim
  * 128 and pages of at least one key tile: 32 tokens when Nq <= 64, 64
- * otherwise (else SC_EUNSUPPORTED).  4-bit caches: q and o are bf16, logits are products of q
- * as it is and of the values that the codes stand for; q 16-byte aligned, a finite scale
- * and at most 2^31 - 1 rows (else SC_EINVAL, SC_EUNSUPPORTED).  ws: device scratch, 16-byte aligned, of at least
+ * otherwise (else SC_EUNSUPPORTED).  4-bit caches: q and o are bf16, logits
+ * are products of q as it is and of the values that the codes stand for; q
+ * 16-byte aligned, a finite scale and at most 2^31 - 1 rows (else SC_EINVAL,
+ * SC_EUNSUPPORTED).  ws: device scratch, 16-byte aligned, of at least
  * sc_attention_workspace_bytes(plan, cache) bytes (may be NULL when that is
  * 0, as for fp32 caches unless the nodes share a prefix); the bf16 kernel splits
  * long key ranges across work-groups and merges their partial softmax sums
- * there, and so does any that reads a shared prefix once; over a 4-bit cache long nodes have
- * their distinct pages of the layer taken out there as bf16 and read by the bf16 forms.
- * Its contents are undefined on return; calls sharing one workspace must be ordered on one
- * stream.  Errors: SC_ESTALE, SC_EUNAVAILABLE (a page's state not written at
+ * there, and so does any that reads a shared prefix once; over a 4-bit cache
+ * long nodes have their distinct pages of the layer taken out there as bf16 and
+ * read by the bf16 forms.  Its contents are undefined on return; calls sharing
+ * one workspace must be ordered on one stream.  Errors: SC_ESTALE, SC_EUNAVAILABLE (a page's state not written at
  * this layer), SC_EINVAL (workspace too small or misaligned), SC_EUNSUPPORTED,
  * SC_EDEVICE. */
 size_t sc_attention_workspace_bytes(const sc_plan* plan, const sc_cache* cache);

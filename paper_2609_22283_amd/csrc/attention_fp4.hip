@@ -243,7 +243,7 @@ __global__ __launch_bounds__(64 * FA_NW, R == 1 ? 3 : 2) void fp4_attention_kern
   // K rows: row 4 x + i of product b is token 16 (x % 2) + 4 (b % 4) + i of the chunk's block
   // 2 (b / 4) + x / 2, so that the rows a lane gets of S^T (x = lane / 16) are the columns it
   // has to give of P^T
-  const uint32_t k_at = (16 * (lane >> 2 & 1) + (lane & 3)) * 64 + (lane >> 4) * 16;
+  const uint32_t k_at = (lane >> 2 & 1) * 256 + (lane >> 4) * 64 + (lane & 3) * 16;
   const uint32_t ks_at = kFp4KScale + (lane >> 2 & 1) * 64 + (lane & 3) * 16 + (lane >> 4) * 4;
   const uint32_t v_at = kFp4V + (lane & 15) * 16, vs_at = kFp4VScale + (lane & 15) * 8;
   const bool ragged = (g.tpp & 31) != 0 || (it.blocks & 3) != 0;
@@ -267,7 +267,7 @@ __global__ __launch_bounds__(64 * FA_NW, R == 1 ? 3 : 2) void fp4_attention_kern
     for (int h = 0; h < 2; ++h) {
       const char* p = block_at(4 * c + 2 * h + (lane >> 3 & 1));
 #pragma unroll
-      for (int i = 0; i < 4; ++i) k[4 * h + i] = *reinterpret_cast<const u32x4*>(p + k_at + 256 * i);
+      for (int i = 0; i < 4; ++i) k[4 * h + i] = *reinterpret_cast<const u32x4*>(p + k_at + 512 * i);
       ks[h] = *reinterpret_cast<const uint32_t*>(p + ks_at);
     }
   };

@@ -75,6 +75,9 @@ struct ConvertGeom {
 // channels a lane, so that four neighbouring lanes hold a group and a lane's passes fill its
 // scales' words.
 __device__ __forceinline__ int k_token(int i) { return 16 * (i >> 2) + 4 * (i & 3); }
+__device__ __forceinline__ uint32_t k_codes_at(int i, int32_t lane) {
+  return 512 * (i & 3) + 256 * (i >> 2) + (lane >> 2 & 3) * 64 + (lane >> 4) * 16 + (lane & 3) * 4;
+}
 __device__ __forceinline__ uint32_t k_scales_at(int32_t lane) { return kFp4KScale + (lane >> 4) * 16 + (lane >> 2 & 3) * 4; }
 __device__ __forceinline__ uint32_t group_scale(const u32x4& v) {
   return fp4_scale(quad_max(umax(umax(bf16x2_top(v[0]), bf16x2_top(v[1])), umax(bf16x2_top(v[2]), bf16x2_top(v[3])))));
@@ -85,7 +88,7 @@ __device__ __forceinline__ void pack_keys(const u32x4 (&k)[8], char* block, int3
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const uint32_t s = group_scale(k[i]);
-    *reinterpret_cast<uint32_t*>(block + (k_token(i) + (lane >> 4)) * 64 + (lane & 15) * 4) = fp4_codes(k[i], s);
+    *reinterpret_cast<uint32_t*>(block + k_codes_at(i, lane)) = fp4_codes(k[i], s);
     w[i >> 2] |= s << (8 * (i & 3));
   }
   if ((lane & 3) == 0) {
@@ -155,7 +158,7 @@ __global__ __launch_bounds__(256) void page_unpack_kernel(ConvertGeom g, PairLis
   const u32x2 vw = *reinterpret_cast<const u32x2*>(block + kFp4VScale + (lane >> 2) * 8);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    k[i] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(block + (k_token(i) + (lane >> 4)) * 64 + (lane & 15) * 4));
+    k[i] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(block + k_codes_at(i, lane)));
     v[i] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(block + kFp4V + i * 256 + lane * 4));
   }
 #pragma unroll
