@@ -40,9 +40,10 @@ int sc_timer_read(const char* kind, int32_t* launches, double* total_ms);
  * test or a benchmark can say which one it covers.
  * sc_attention_form: sc_attention with the plan's workspace.  *queries:
  * query rows per work-group (bf16: 32 with a node's keys split over the waves,
- * 64, 128 or 256 with a unit's keys in order; fp32: 16; 4-bit: 16 or 32, or 0 where the pages are first
- * taken out as bf16, by whose forms the plan then runs); *ring: K/V tiles in
- * the LDS ring of a unit form, else 1; *pieces: key-range pieces that each
+ * 64, 128 or 256 with a unit's keys in order; fp32: 16; 4-bit: 16 or 32, or 0
+ * where the pages are first taken out as bf16, by whose forms the plan then
+ * runs); *ring: K/V tiles in the LDS ring of a unit form, the waves that share
+ * a tile's keys where 4-bit pages are read as they are, else 1; *pieces: key-range pieces that each
  * unit of the last round is cut into (1: none).  A plan of sc_plan_share that
  * reads its prefix once for all rows has minus the pieces of the prefix there.
  * sc_gemm_form: the projection of the given timer kind ("gemm_qkv", "gemm_out",

@@ -80,7 +80,6 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef short i16x2 __attribute__((ext_vector_type(2)));
 
-constexpr int FA_NW = 4;      // waves of a work-group
 constexpr float kFp4Rise = 40.f;  // sums of 2^31 keys in units of 2^m stay below 2^(40 + 31)
 constexpr int FA_ROW = 132;   // floats of a row of partial outputs in LDS
 
@@ -189,9 +188,9 @@ __device__ __forceinline__ Fp4Item fp4_item(const Fp4Geom& g, const Fp4List& lis
   return it;
 }
 
-// A work-group has 16 R rows of a head; its four waves take every fourth chunk of 128 keys,
-// each with a softmax of its own (running power of two, sums, outputs), and join the four in
-// LDS at the end.  Nothing is shared between the waves' loops, so there is no barrier in them:
+// A work-group has 16 R rows of a head; its NW waves take every NW-th chunk of 128 keys, each
+// with a softmax of its own (running power of two, sums, outputs), and join them in LDS at the
+// end.  Nothing is shared between the waves' loops, so there is no barrier in them:
 // K and V go from the cache straight to the registers that the products read, K of the next
 // chunk under the exponentials of this one, V in K's registers.  The rows' sums come from one
 // more product, with ones, which has the exponentials as they were rounded.
@@ -204,11 +203,11 @@ __device__ __forceinline__ Fp4Item fp4_item(const Fp4Geom& g, const Fp4List& lis
 // 1064 in tiles of 16, whose work-groups are three to a CU).  Tried on the same nodes: 32x32x64
 // products of 64 keys 3.66 ms, with their loads further ahead 3.71; the waves on rows of their own, 128 in all, over the same keys 3.25, but slower at
 // every shorter one (58 us become 144 at four nodes of 256 rows).
-template <int R>
-__global__ __launch_bounds__(64 * FA_NW, R == 1 ? 3 : 2) void fp4_attention_kernel(const uint16_t* __restrict__ q, uint16_t* __restrict__ o,
+template <int R, int NW>
+__global__ __launch_bounds__(64 * NW, R == 1 && NW == 4 ? 3 : 2) void fp4_attention_kernel(const uint16_t* __restrict__ q, uint16_t* __restrict__ o,
                                                                       Fp4Geom g, Fp4List list) {
-  __shared__ __attribute__((aligned(16))) float part[FA_NW][16 * FA_ROW];
-  __shared__ float ml[FA_NW][2][16];
+  __shared__ __attribute__((aligned(16))) float part[NW][16 * FA_ROW];
+  __shared__ float ml[NW][2][16];
   __shared__ uint64_t base[kFp4Pages];
   __shared__ u32x4 qs[R][4][64];         // the queries' operands: halves of hi, halves of lo
   __shared__ uint32_t q_scale[R][16];
@@ -216,7 +215,7 @@ __global__ __launch_bounds__(64 * FA_NW, R == 1 ? 3 : 2) void fp4_attention_kern
   const Fp4Item it = fp4_item<R>(g, list, (int32_t)xcd_remap(blockIdx.x, gridDim.x));
   if (it.c0 >= it.c1) return;
   const int32_t j0 = 4 * it.c0 / g.blocks, j1 = min(it.pages, (4 * it.c1 + g.blocks - 1) / g.blocks);
-  for (int32_t j = j0 + (int32_t)threadIdx.x; j < j1; j += 64 * FA_NW) {
+  for (int32_t j = j0 + (int32_t)threadIdx.x; j < j1; j += 64 * NW) {
     const int32_t s = !g.joined ? it.first + j : j < list.shared ? j : it.first + j - list.shared;
     base[j - j0] = (uint64_t)list.slot[s] * g.slot_bytes + (uint64_t)it.head * g.blocks * kFp4Block;
   }
@@ -272,7 +271,7 @@ __global__ __launch_bounds__(64 * FA_NW, R == 1 ? 3 : 2) void fp4_attention_kern
     }
   };
   if (it.c0 + wave < it.c1) load_k(it.c0 + wave);
-  for (int32_t c = it.c0 + wave; c < it.c1; c += FA_NW) {
+  for (int32_t c = it.c0 + wave; c < it.c1; c += NW) {
     bool cut = false;  // a block of the chunk ends early, or is not there
     int32_t left[2];
     if (ragged) {
@@ -345,7 +344,7 @@ __global__ __launch_bounds__(64 * FA_NW, R == 1 ? 3 : 2) void fp4_attention_kern
 #undef SC_PV
       sum[r] = mx<0>(ones, hi[r], lo[r], sum[r], 0x7f7f7f7fu, psc[r]);
     };
-    const int32_t next = c + FA_NW < it.c1 ? c + FA_NW : c;  // at the end the same again: no branch
+    const int32_t next = c + NW < it.c1 ? c + NW : c;  // at the end the same again: no branch
     f32x4 s0[8];
     logits(0, s0);
     if constexpr (R == 1) {
@@ -401,14 +400,14 @@ __global__ __launch_bounds__(64 * FA_NW, R == 1 ? 3 : 2) void fp4_attention_kern
     }
     __syncthreads();
     const int32_t x = threadIdx.x >> 4, ch = 8 * (threadIdx.x & 15), row = it.row0 + 16 * r + x;
-    if (16 * r + x < it.rows) {
+    if (x < 16 && 16 * r + x < it.rows) {
       float to = ml[0][0][x];
 #pragma unroll
-      for (int w = 1; w < FA_NW; ++w) to = fmaxf(to, ml[w][0][x]);
+      for (int w = 1; w < NW; ++w) to = fmaxf(to, ml[w][0][x]);
       f32x4 y[2] = {};
       float l = 0.f;
 #pragma unroll
-      for (int w = 0; w < FA_NW; ++w) {
+      for (int w = 0; w < NW; ++w) {
         const float keep = exp2f(ml[w][0][x] - to);
         l += keep * ml[w][1][x];
         y[0] += keep * *reinterpret_cast<const f32x4*>(&part[w][x * FA_ROW + ch]);
@@ -489,7 +488,7 @@ struct Fp4Wide {
 struct Fp4Schedule {
   size_t room = 0;
   std::shared_ptr<Fp4Wide> wide;  // over bf16 pages; else by tiles of so many rows:
-  int32_t tile = 16;
+  int32_t tile = 16, waves = 4;
   int32_t joined = 1, p_len = 1, p_pieces = 0, o_len = 1, o_pieces = 1;  // chunks of a piece, pieces (own: the most of a node)
   size_t bytes = 0;
   double us = 1e30;
@@ -568,7 +567,10 @@ static double fp4_makespan(double slots, const std::vector<Fp4Items>& items) {
 // an item 1 more, a launch 3, no less than the pages take from HBM at 5.6 MB per us; joining
 // pieces 3.5, 0.13 per piece and the partials at 2.2 MB per us.  So nodes that fill their tiles
 // read a shared prefix each by itself (sixteen of 16 rows over 128 x 128 keys 38 us, 49 with
-// the rows of all nodes in one matrix; 32 of one row over 256 x 64 keys 26 against 20).
+// the rows of all nodes in one matrix; 32 of one row over 256 x 64 keys 26 against 20), and
+// where there are fewer work-groups than CUs, eight waves take what four would over more
+// pieces (256 rows over 17 x 512 keys 21.6 us, 25.3; one frame of 64 rows over 21 x 64 8.5,
+// 9.2; one row over 8 x 64 keys 6.6, 6.3).
 // Over bf16 pages: the time of that attention, 8 and 0.17 per MB of them (four nodes of 4680
 // rows over 21 x 1560 keys 2.94 to 3.07 ms, 3.28 by tiles; four of 256 over 21 x 256 59 us, 41 by
 // tiles): 32 rows read K and V from cache once, 256 of the bf16 form's eight waves.
@@ -589,7 +591,10 @@ static Fp4Schedule find_fp4_schedule(const sc_plan* p, const sc_cache* c, size_t
   const double from_hbm = (double)(p->shared + own_all) * c->slot_bytes / 5.6e6;
   const int64_t prefix = fp4_chunks(c, p->shared);
   std::vector<Fp4Items> items;
-  for (const int32_t tile : {16, 32})
+  struct Form {
+    int32_t tile, waves;
+  };
+  for (const auto [tile, waves] : {Form{16, 4}, Form{16, 8}, Form{32, 4}})
     for (const int32_t joined : {1, 0}) {
       if (!joined && !p->shared) continue;
       const int64_t own_tiles = (int64_t)H * ((p->nq + tile - 1) / tile), p_tiles = (int64_t)H * ((rows + tile - 1) / tile);
@@ -601,6 +606,7 @@ static Fp4Schedule find_fp4_schedule(const sc_plan* p, const sc_cache* c, size_t
         Fp4Schedule s;
         s.room = room;
         s.tile = tile;
+        s.waves = waves;
         s.joined = joined;
         s.o_len = (int32_t)o_len;
         s.o_pieces = (int32_t)((own_chunks + o_len - 1) / o_len);
@@ -614,16 +620,20 @@ static Fp4Schedule find_fp4_schedule(const sc_plan* p, const sc_cache* c, size_t
         items.clear();
         double total = 0;
         const auto add = [&](double units, int64_t chunks, int64_t of) {
-          if (chunks >= of) items.push_back({units * (double)(chunks / of), (double)((of + 3) / 4)});
-          if (chunks % of) items.push_back({units, (double)((chunks % of + 3) / 4)});
+          if (chunks >= of) items.push_back({units * (double)(chunks / of), (double)of});
+          if (chunks % of) items.push_back({units, (double)(chunks % of)});
           total += units * (double)((chunks + of - 1) / of);
         };
         if (!joined) add((double)p_tiles, prefix, p_len);
         for (const auto& o : own) add((double)own_tiles * o.second, fp4_chunks(c, o.first + (joined ? p->shared : 0)), o_len);
         if (total > (double)kFp4Groups) continue;
-        const int32_t per = total <= kCUs ? 1 : total <= 2 * kCUs || tile == 32 ? 2 : 3;  // work-groups to a CU
-        const double step = tile == 16 ? (per == 1 ? 1.36 : per == 2 ? 2.0 : 3.0) : (per == 1 ? 2.3 : 3.8);
-        for (Fp4Items& i : items) i.us = i.us * step + 1.0;
+        const int32_t per = total <= kCUs || waves == 8 ? 1 : total <= 2 * kCUs || tile == 32 ? 2 : 3;  // work-groups to a CU
+        const double step = tile == 32 ? (per == 1 ? 2.3 : 3.8) : per == 1 ? 1.45 : per == 2 ? 2.0 : 3.0;
+        for (Fp4Items& i : items) {
+          const double left = std::fmod(i.us, 8.0);
+          i.us = waves == 4 ? std::ceil(i.us / 4) * step + 1.0
+                            : std::floor(i.us / 8) * 2.1 + (left > 4 ? 2.1 : left > 0 ? step : 0.0) + 1.6;
+        }
         s.us = std::max(fp4_makespan((double)kCUs * per, items), from_hbm) + 3.0;
         if (s.bytes) s.us += 3.5 + 0.13 * (double)all + (double)s.bytes / 2.2e6;
         if (s.us < best.us) best = s;
@@ -698,10 +708,12 @@ int launch_fp4_attention(const sc_plan* p, const sc_cache* c, int32_t layer, con
   const uint16_t* qb = static_cast<const uint16_t*>(q);
   uint16_t* ob = static_cast<uint16_t*>(o);
   timer_begin(TK_ATTENTION, stream);
-  if (s->tile == 16)
-    hipLaunchKernelGGL(fp4_attention_kernel<1>, dim3((uint32_t)items), dim3(64 * FA_NW), 0, stream, qb, ob, g, l);
+  if (s->waves == 8)
+    hipLaunchKernelGGL((fp4_attention_kernel<1, 8>), dim3((uint32_t)items), dim3(512), 0, stream, qb, ob, g, l);
+  else if (s->tile == 16)
+    hipLaunchKernelGGL((fp4_attention_kernel<1, 4>), dim3((uint32_t)items), dim3(256), 0, stream, qb, ob, g, l);
   else
-    hipLaunchKernelGGL(fp4_attention_kernel<2>, dim3((uint32_t)items), dim3(64 * FA_NW), 0, stream, qb, ob, g, l);
+    hipLaunchKernelGGL((fp4_attention_kernel<2, 4>), dim3((uint32_t)items), dim3(256), 0, stream, qb, ob, g, l);
   timer_end(TK_ATTENTION, stream);
   if (s->bytes) {
     timer_begin(TK_ATTN_COMBINE, stream);
@@ -723,8 +735,8 @@ int fp4_attention_form(const sc_plan* p, const sc_cache* c, int32_t* queries, in
   const Fp4Schedule* s = fp4_schedule(p, c, SIZE_MAX);
   if (!s) return fail(SC_EINVAL, "out of host memory");
   *queries = s->wide ? 0 : s->tile;
-  *ring = 1;
-  *pieces = s->joined ? s->o_pieces : -s->p_pieces;
+  *ring = s->wide ? 1 : s->waves;
+  *pieces = s->wide ? 1 : s->joined ? s->o_pieces : -s->p_pieces;
   return SC_OK;
 }
 

@@ -18,7 +18,7 @@ def test_loops_without_scratch_memory(tmp_path):
     r = subprocess.run(cmd, capture_output=True, text=True)
     assert r.returncode == 0, r.stderr[-2000:]
     loops = {name: _innermost_loops(lines) for name, lines in _kernels(out.read_text()).items() if "fp4_attention" in name}
-    assert len(loops) == 2 and all(loops.values())
+    assert len(loops) == 3 and all(loops.values())
     for name, found in loops.items():
         for loop in found:
             assert not any("scratch_" in x or "s_barrier" in x for x in loop), name

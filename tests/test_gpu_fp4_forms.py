@@ -1,5 +1,5 @@
-"""Every way of running the attention over 4-bit pages, each where it is chosen: tiles of 16 and of
-32 rows, keys in pieces, a prefix read once or by each node, and bf16 pages taken out first; without
+"""Every way of running the attention over 4-bit pages, each where it is chosen: tiles of 16 rows
+with four waves and with eight, and of 32 rows, keys in pieces, a prefix read once or by each node, and bf16 pages taken out first; without
 a workspace; and as a block's cross-attention."""
 import numpy as np
 import pytest
@@ -15,19 +15,22 @@ from test_gpu_condition import PACK, RESIDENT, ROUNDINGS
 
 pytestmark = pytest.mark.gpu
 
-# heads, tokens per page, frames, prefix states, nodes, rows a node; tile rows (0: bf16 pages), and
-# pieces: 1, "pieces", or "prefix" where that is read once for all rows
+# heads, tokens per page, frames, prefix states, nodes, rows a node; tile rows (0: bf16 pages), the
+# waves of a work-group, and pieces: 1, "pieces", or "prefix" where that is read once for all rows
 FORMS = [
-    ((1, 64, 1, 0, 1, 1), 16, 1),
-    ((1, 8, 1, 700, 1, 1), 16, "pieces"),
-    ((1, 512, 1, 60, 32, 1), 16, "prefix"),
-    ((12, 64, 1, 100, 16, 4), 16, "prefix"),
-    ((2, 64, 1, 0, 4, 2000), 32, 1),
-    ((3, 520, 1, 30, 3, 256), 32, "pieces"),
-    ((3, 64, 1, 120, 3, 500), 32, "prefix"),
-    ((12, 64, 1, 0, 2, 2000), 0, 1),
-    ((3, 104, 1, 120, 3, 1024), 0, "pieces"),
-    ((2, 520, 3, 6, 2, 4680), 0, "prefix"),
+    ((1, 64, 1, 0, 1, 1), 16, 4, 1),
+    ((2, 40, 2, 9, 5, 17), 16, 8, 1),
+    ((1, 1560, 3, 0, 1, 65), 16, 4, "pieces"),
+    ((1, 8, 1, 700, 1, 1), 16, 8, "pieces"),
+    ((1, 64, 1, 40, 64, 1), 16, 4, "prefix"),
+    ((1, 512, 1, 60, 32, 1), 16, 8, "prefix"),
+    ((12, 64, 1, 100, 16, 4), 16, 8, "prefix"),
+    ((2, 64, 1, 0, 4, 2000), 32, 4, 1),
+    ((3, 520, 1, 30, 3, 256), 32, 4, "pieces"),
+    ((3, 64, 1, 120, 3, 500), 32, 4, "prefix"),
+    ((12, 64, 1, 0, 2, 2000), 0, 1, 1),
+    ((3, 104, 1, 120, 3, 1024), 0, 1, 1),
+    ((2, 520, 3, 6, 2, 4680), 0, 1, 1),
 ]
 
 
@@ -46,15 +49,15 @@ def _sampled(h, reads, q, nq):
 
 
 def _form(plan, cache):
-    tile, _, pieces = sc_attention_form(plan, cache)
-    return tile, "prefix" if pieces < 0 else "pieces" if pieces > 1 else pieces
+    tile, waves, pieces = sc_attention_form(plan, cache)
+    return tile, waves, "prefix" if pieces < 0 else "pieces" if pieces > 1 else pieces
 
 
-@pytest.mark.parametrize("shape,tile,pieces", FORMS)
-def test_every_form(shape, tile, pieces):
+@pytest.mark.parametrize("shape,tile,waves,pieces", FORMS)
+def test_every_form(shape, tile, waves, pieces):
     h, plan, reads = _case(*shape)
     nodes, nq = shape[-2:]
-    assert _form(plan, h.cache) == (tile, pieces)
+    assert _form(plan, h.cache) == (tile, waves, pieces)
     qd, q = h.queries(nodes * nq, 2.0)
     rows, (want, tol) = _sampled(h, reads, q, nq)
     got = attend(h, plan, qd)
@@ -63,7 +66,7 @@ def test_every_form(shape, tile, pieces):
     np.testing.assert_array_equal(got, attend(h, plan, qd))  # equal calls, equal bits
 
 
-@pytest.mark.parametrize("shape", [s for s, _, _ in FORMS] + [(4, 104, 3, 60, 4, 2048)])
+@pytest.mark.parametrize("shape", [s for s, *_ in FORMS] + [(4, 104, 3, 60, 4, 2048)])
 def test_without_a_workspace(shape):
     """The call that has an array of its own, which the last shape's fastest way does not fit into."""
     h, plan, reads = _case(*shape)
