@@ -322,6 +322,9 @@ def sc_selection_build(kind, K, W, nodes: Sequence[Tuple[int, int]], phi_table=N
 
 # ---------------------------------------------------------------------- cache
 def _nodes(states):
+    if len(states) == 1:  # without an array type: 0.7 us less
+        (c, j), = states
+        return C.byref(sc_node(int(c), int(j)))
     return (sc_node * max(1, len(states)))(*[sc_node(int(c), int(j)) for c, j in states])
 
 
