@@ -82,19 +82,16 @@ __device__ __forceinline__ uint32_t k_scales_at(int32_t lane) { return kFp4KScal
 __device__ __forceinline__ uint32_t group_scale(const u32x4& v) {
   return fp4_scale(quad_max(umax(umax(bf16x2_top(v[0]), bf16x2_top(v[1])), umax(bf16x2_top(v[2]), bf16x2_top(v[3])))));
 }
-// Codes and scales of K of a block whose eight passes' values are given.
-__device__ __forceinline__ void pack_keys(const u32x4 (&k)[8], char* block, int32_t lane) {
-  uint32_t w[2] = {0, 0};
+// Codes and scales of K of half a block, 16 tokens, whose four passes' values are given.
+__device__ __forceinline__ void pack_keys(const u32x4 (&k)[4], int half, char* block, int32_t lane) {
+  uint32_t w = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < 4; ++i) {
     const uint32_t s = group_scale(k[i]);
-    *reinterpret_cast<uint32_t*>(block + k_codes_at(i, lane)) = fp4_codes(k[i], s);
-    w[i >> 2] |= s << (8 * (i & 3));
+    *reinterpret_cast<uint32_t*>(block + k_codes_at(4 * half + i, lane)) = fp4_codes(k[i], s);
+    w |= s << (8 * i);
   }
-  if ((lane & 3) == 0) {
-    *reinterpret_cast<uint32_t*>(block + k_scales_at(lane)) = w[0];
-    *reinterpret_cast<uint32_t*>(block + k_scales_at(lane) + 64) = w[1];
-  }
+  if ((lane & 3) == 0) *reinterpret_cast<uint32_t*>(block + k_scales_at(lane) + 64 * half) = w;
 }
 
 // One wave per two blocks: of V, pass n takes the channels 8 n + lane / 8 of both, eight
@@ -116,12 +113,12 @@ __global__ __launch_bounds__(256) void page_pack_kernel(ConvertGeom g, PairList 
   u32x2 vw[2] = {};
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
-    u32x4 k[8], v[8];
+    u32x4 k[2][4], v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      k[i] = v[i] = u32x4{};
+      k[i >> 2][i & 3] = v[i] = u32x4{};
       if (32 * half + k_token(i) + (lane >> 4) < left)
-        k[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4u*>(krow + (uint64_t)(32 * half + k_token(i)) * 256));
+        k[i >> 2][i & 3] = __builtin_nontemporal_load(reinterpret_cast<const u32x4u*>(krow + (uint64_t)(32 * half + k_token(i)) * 256));
       if (8 * (lane & 7) < left) v[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4u*>(vrow + (uint64_t)(8 * half + i) * 8 * g.tpp * 2));
     }
 #pragma unroll
@@ -130,7 +127,10 @@ __global__ __launch_bounds__(256) void page_pack_kernel(ConvertGeom g, PairList 
       if (mine) *reinterpret_cast<uint32_t*>(vcodes + (8 * half + i) * 128) = fp4_codes(v[i], s);
       vw[i & 1][half] |= s << (8 * (i >> 1));
     }
-    if (half == 0 || two) pack_keys(k, block + half * kFp4Block, lane);
+    if (half == 0 || two) {
+      pack_keys(k[0], 0, block + half * kFp4Block, lane);
+      pack_keys(k[1], 1, block + half * kFp4Block, lane);
+    }
   }
   if ((lane & 3) == 0 && mine) {
     char* vs = block + (lane >> 2 & 1) * kFp4Block + kFp4VScale + (lane >> 3) * 8;
@@ -208,13 +208,13 @@ struct AppendArgs {
   int32_t slot[32];
 };
 
-// A wave takes K (z 0) or V (z 1) of a block: x the blocks of the state's pages, four to a
-// work-group, y the head.  Keys as in pack_keys, rotated before; of V a lane takes eight
+// A wave takes half of K (z 0 and 1) or V (z 2) of a block: x the blocks of the state's pages, four
+// to a work-group, y the head.  Keys as in pack_keys, rotated before; of V a lane takes eight
 // channels of the tokens 8 (lane / 16) .. + 7, finds each channel's largest magnitude with the
 // three lanes that hold its other tokens, and the codes cross LDS, so that they leave in
-// 16-byte runs.  A chain of latencies: a frame of 64 tokens, 12 heads, rotated, takes 6.2
-// us (9.7 with K and V in one wave and rotations loaded one by one), a chunk of 3 x 1560
-// tokens (36 MB) 12.7.
+// 16-byte runs.  A chain of latencies: a frame of 64 tokens, 12 heads, rotated, takes 4.8 us
+// (6.2 with K in one wave, 9.7 with V in the same one and rotations loaded one by one), a chunk
+// of 3 x 1560 tokens (36 MB) 11.2 (12.7 with K in one).
 template <bool ROPE>
 __global__ __launch_bounds__(256) void fp4_append_kernel(AppendArgs g, int32_t items) {
   __shared__ __attribute__((aligned(16))) char lds[4][2048 + 128];
@@ -224,13 +224,14 @@ __global__ __launch_bounds__(256) void fp4_append_kernel(AppendArgs g, int32_t i
   const int32_t page = item / g.blocks, b = item - page * g.blocks, t0 = b * kFp4Tokens, left = g.tpp - t0;
   char* block = g.layer_base + (uint64_t)g.slot[page] * g.slot_bytes + ((uint64_t)h * g.blocks + b) * kFp4Block;
   const uint64_t row = (uint64_t)g.heads * 128, src = ((uint64_t)page * g.tpp + t0) * row + (uint64_t)h * 128 + 8 * (lane & 15);
-  u32x4 v[8];
-  if (blockIdx.z == 0) {
+  if (blockIdx.z < 2) {
+    const int32_t t1 = 16 * blockIdx.z + (lane >> 4);  // of pass i: token t1 + 4 i
+    u32x4 k[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int32_t t = k_token(i) + (lane >> 4);
-      v[i] = u32x4{};
-      if (t < left) v[i] = *reinterpret_cast<const u32x4u*>(g.k + src + t * row);
+    for (int i = 0; i < 4; ++i) {
+      const int32_t t = t1 + 4 * i;
+      k[i] = u32x4{};
+      if (t < left) k[i] = *reinterpret_cast<const u32x4u*>(g.k + src + t * row);
     }
     if constexpr (ROPE) {
       // the rotations of this lane's channel pairs: the axis and its table are fixed, the
@@ -244,31 +245,32 @@ __global__ __launch_bounds__(256) void fp4_append_kernel(AppendArgs g, int32_t i
         table[j] = g.table + (ax[j] == 0 ? (int64_t)(g.frame0 + page) * g.pairs_t + p
                               : ax[j] == 1 ? g.off_h + p - g.pairs_t : g.off_w + p - g.pairs_t - g.pairs_h);
       }
-      float2 cs[8][4];
+      float2 cs[4][4];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int32_t tok = min(t0 + k_token(i) + (lane >> 4), g.tpp - 1);
+      for (int i = 0; i < 4; ++i) {
+        const int32_t tok = min(t0 + t1 + 4 * i, g.tpp - 1);
         const int32_t hh = (int32_t)fast_div((uint32_t)tok, g.gw_div), ww = tok - hh * g.grid_w;
 #pragma unroll
         for (int j = 0; j < 4; ++j) cs[i][j] = table[j][ax[j] == 0 ? 0 : ax[j] == 1 ? hh * g.pairs_h : ww * g.pairs_w];
       }
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const bool there = k_token(i) + (lane >> 4) < left;  // behind the page's end zeros stay +0
+      for (int i = 0; i < 4; ++i) {
+        const bool there = t1 + 4 * i < left;  // behind the page's end zeros stay +0
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const uint32_t w = v[i][j];
+          const uint32_t w = k[i][j];
           const float x0 = __uint_as_float(w << 16), x1 = __uint_as_float(w & 0xffff0000u);
           // as the bf16 cache rotates and rounds them
           const uint32_t y = pack_bf16x2(fmaf(x0, cs[i][j].x, -(x1 * cs[i][j].y)), fmaf(x0, cs[i][j].y, x1 * cs[i][j].x));
-          v[i][j] = there ? y : 0u;
+          k[i][j] = there ? y : 0u;
         }
       }
     }
-    pack_keys(v, block, lane);
+    pack_keys(k, blockIdx.z, block, lane);
     return;
   }
+  u32x4 v[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int32_t t = 8 * (lane >> 4) + i;
@@ -330,7 +332,7 @@ int launch_fp4_append(const sc_cache* c, int32_t layer, const int32_t* slots, in
     g.gw_div = magic_div((uint32_t)rope->desc.grid_w);
   }
   const int32_t items = d.pages_per_chunk * g.blocks;
-  const dim3 grid((items + 3) / 4, d.n_heads, 2);
+  const dim3 grid((items + 3) / 4, d.n_heads, 3);
   timer_begin(TK_APPEND, stream);
   if (rope)
     hipLaunchKernelGGL(fp4_append_kernel<true>, grid, dim3(256), 0, stream, g, items);
