@@ -502,12 +502,21 @@ static int64_t fp4_chunks(const sc_cache* c, int64_t pages) {
 static std::shared_ptr<Fp4Wide> fp4_wide(const sc_plan* p, const sc_cache* c) {
   if (c->d.tokens_per_page < (p->shared || p->nq <= 64 ? 32 : 64)) return nullptr;
   auto w = std::make_shared<Fp4Wide>();
-  std::map<int32_t, int32_t> place;
-  for (int32_t s : p->page_slot)
-    if (place.emplace(s, (int32_t)place.size()).second) {
+  std::vector<int32_t> place(c->d.n_slots, -1);
+  const auto put = [&](int32_t s) {
+    if (place[s] < 0) {
+      place[s] = (int32_t)w->src.size();
       w->src.push_back(s);
-      w->dst.push_back((int32_t)w->dst.size());
+      w->dst.push_back(place[s]);
     }
+    return place[s];
+  };
+  w->plan.page_slot.reserve(p->page_slot.size());
+  for (size_t i = 0; i + 1 < p->page_off.size(); ++i) {
+    size_t k = p->page_off[i];
+    for (int32_t s = 0; i && s < p->shared; ++s, ++k) w->plan.page_slot.push_back(w->plan.page_slot[s]);
+    for (; k < (size_t)p->page_off[i + 1]; ++k) w->plan.page_slot.push_back(put(p->page_slot[k]));
+  }
   w->cache.d = c->d;
   w->cache.d.dtype = SC_DTYPE_BF16;
   w->cache.d.n_layers = 1;
@@ -518,11 +527,7 @@ static std::shared_ptr<Fp4Wide> fp4_wide(const sc_plan* p, const sc_cache* c) {
   w->page_bytes = w->src.size() * w->cache.slot_bytes;
   w->plan.nodes = p->nodes;
   w->plan.page_off = p->page_off;
-  w->plan.page_tokens = p->page_tokens;
-  w->plan.page_frame = p->page_frame;
-  w->plan.page_state = p->page_state;
-  w->plan.page_gen.assign(p->page_slot.size(), 0);
-  for (int32_t s : p->page_slot) w->plan.page_slot.push_back(place.at(s));
+  if (p->page_slot.size() <= (size_t)kFp4Pages) w->plan.page_state = p->page_state;  // of lists that one launch reads whole
   w->plan.cache = &w->cache;
   w->plan.nq = p->nq;
   w->plan.shared = p->shared;
@@ -639,7 +644,11 @@ static Fp4Schedule find_fp4_schedule(const sc_plan* p, const sc_cache* c, size_t
         if (s.us < best.us) best = s;
       }
     }
-  if (auto w = fp4_wide(p, c)) {
+  // no less than the products at 1400 TFLOP/s and the longest list's pages taken out
+  double flops = 0;
+  for (const auto& o : own) flops += 512.0 * p->nq * H * (double)(o.first + p->shared) * c->d.tokens_per_page * o.second;
+  const double least = 8.0 + flops / 1.4e9 + 0.17e-6 * 512.0 * H * c->d.tokens_per_page * (double)(own_max + p->shared);
+  if (auto w = least < best.us ? fp4_wide(p, c) : nullptr) {
     const size_t bytes = align256(w->page_bytes) + attention_exact_workspace_bytes(&w->plan, &w->cache);
     const double us = attention_exact_us(&w->plan, &w->cache) + 8.0 + 0.17e-6 * (double)w->page_bytes;
     if (bytes <= room && us < best.us) {
