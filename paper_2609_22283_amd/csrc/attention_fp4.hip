@@ -435,8 +435,9 @@ __global__ __launch_bounds__(64 * NW, R == 1 && NW == 4 ? 3 : 2) void fp4_attent
 }
 
 // A wave per row and head joins the pieces that its node has, the prefix's and its own, N at
-// a time, whose loads are independent.  Bound by latency, then by the partials: 4 us for 256
-// rows of 12 heads in four pieces (6.4 MB).
+// a time, whose loads are independent: four, or eight of more pieces (one row over 16384 keys in
+// 12 pieces 11.1 us in all, 11.5 four at a time; 256 rows in four 37.8, 38.6 by eight).  Bound by
+// latency, then by the partials: 4 us for 256 rows of 12 heads in four pieces (6.4 MB).
 template <int N>
 __global__ __launch_bounds__(256) void fp4_combine_kernel(uint16_t* __restrict__ o, Fp4Geom g, Fp4List list) {
   const int32_t lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6), h = blockIdx.y;
@@ -727,10 +728,7 @@ int launch_fp4_attention(const sc_plan* p, const sc_cache* c, int32_t layer, con
   if (s->bytes) {
     timer_begin(TK_ATTN_COMBINE, stream);
     const dim3 grid((uint32_t)(g.rows + 3) / 4, (uint32_t)g.heads);
-    const int32_t most = g.p_pieces + s->o_pieces;
-    if (most <= 2)
-      hipLaunchKernelGGL(fp4_combine_kernel<2>, grid, dim3(256), 0, stream, ob, g, l);
-    else if (most <= 4)
+    if (g.p_pieces + s->o_pieces <= 4)
       hipLaunchKernelGGL(fp4_combine_kernel<4>, grid, dim3(256), 0, stream, ob, g, l);
     else
       hipLaunchKernelGGL(fp4_combine_kernel<8>, grid, dim3(256), 0, stream, ob, g, l);

@@ -168,13 +168,14 @@ __global__ __launch_bounds__(256) void rotate_kernel(const T* x, T* y, RotateArg
   }
 }
 
-// Few rows: a head a thread, so that the work spreads over the CUs.
+// Few rows: a head a thread, so that the work spreads over the CUs (12 heads of 128: 256 rows 2.7
+// us, 3.2 with four heads a thread; 1536 rows 3.9 either way, 4096 rows 6.9 against 5.8).
 template <class T, bool HALF>
 static void launch_rotate_t(const void* x, void* y, const RotateArgs& g, hipStream_t s) {
   const uint32_t groups = (uint32_t)(((int64_t)g.rows * g.units + 255) / 256);
   const T* xt = static_cast<const T*>(x);
   T* yt = static_cast<T*>(y);
-  if ((int64_t)groups * ((g.heads + 3) / 4) < 4 * kCUs)
+  if ((int64_t)groups * ((g.heads + 3) / 4) < 3 * kCUs / 2)
     hipLaunchKernelGGL((rotate_kernel<T, HALF, 1>), dim3(groups, (uint32_t)g.heads), dim3(256), 0, s, xt, yt, g);
   else
     hipLaunchKernelGGL((rotate_kernel<T, HALF, 4>), dim3(groups, (uint32_t)(g.heads + 3) / 4), dim3(256), 0, s, xt, yt, g);
