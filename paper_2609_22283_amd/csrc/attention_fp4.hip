@@ -198,14 +198,15 @@ __device__ __forceinline__ Fp4Item fp4_item(const Fp4Geom& g, const Fp4List& lis
 // What bounds it: single tokens, reading the pages (16 x 16384 keys x 12 heads, 428 MB, 72.8
 // us, 5.9 TB/s); many rows, the vector unit, busy for 75 % of the time with 28 cycles for
 // each exponential and its two parts and 16 for each of the products' issue, the matrix core for
-// half of it (four nodes of 4680 rows over 21 x 1560 keys 3.28 ms, 1148 TFLOP/s, in tiles of 32 rows:
-// the products of one half of the rows stand between the exponentials of the other; 3.54 ms and
+// half of it (four nodes of 4680 rows over 21 x 1560 keys 3.28 ms, 1148 TFLOP/s, in tiles of 32
+// rows: the products of one half of the rows stand between the exponentials of the other; 3.54 ms and
 // 1064 in tiles of 16, whose work-groups are three to a CU).  Tried on the same nodes: 32x32x64
-// products of 64 keys 3.66 ms, with their loads further ahead 3.71; the waves on rows of their own, 128 in all, over the same keys 3.25, but slower at
-// every shorter one (58 us become 144 at four nodes of 256 rows).
+// products of 64 keys 3.66 ms, with their loads further ahead 3.71; the waves on rows of their
+// own, 128 in all, over the same keys 3.25, but slower at every shorter one (58 us become 144 at
+// four nodes of 256 rows); the blocks' addresses on the scalar unit, no change.
 template <int R, int NW>
-__global__ __launch_bounds__(64 * NW, R == 1 && NW == 4 ? 3 : 2) void fp4_attention_kernel(const uint16_t* __restrict__ q, uint16_t* __restrict__ o,
-                                                                      Fp4Geom g, Fp4List list) {
+__global__ __launch_bounds__(64 * NW, R == 1 && NW == 4 ? 3 : 2) void fp4_attention_kernel(
+    const uint16_t* __restrict__ q, uint16_t* __restrict__ o, Fp4Geom g, Fp4List list) {
   __shared__ __attribute__((aligned(16))) float part[NW][16 * FA_ROW];
   __shared__ float ml[NW][2][16];
   __shared__ uint64_t base[kFp4Pages];
@@ -568,10 +569,12 @@ static double fp4_makespan(double slots, const std::vector<Fp4Items>& items) {
 // The cheapest way within `room` bytes, by estimated time in us.  Measured (2 .. 12 heads, 1 ..
 // 1024 rows a node, 512 .. 262144 keys, 700 ways of cutting them; what is chosen is within
 // 10 % of the best of them): four chunks, one to each wave of a work-group, take
-//   tiles of 16 rows  1.36 with one work-group to a CU, 2.0 with two, 3.0 with three
+//   tiles of 16 rows  1.45 with one work-group to a CU, 2.0 with two, 3.0 with three
 //   tiles of 32 rows  2.3 with one, 3.8 with two
-// an item 1 more, a launch 3, no less than the pages take from HBM at 5.6 MB per us; joining
-// pieces 3.5, 0.13 per piece and the partials at 2.2 MB per us.  So nodes that fill their tiles
+// and eight chunks, one to each of eight waves, of which a CU has room for one work-group, 2.1
+// (the last four or fewer 1.45).  An item is 1 more, 1.6 with eight waves, a launch 3, no less
+// than the pages take from HBM at 5.6 MB per us; joining pieces 3.5, 0.13 per piece and the
+// partials at 2.2 MB per us.  So nodes that fill their tiles
 // read a shared prefix each by itself (sixteen of 16 rows over 128 x 128 keys 38 us, 49 with
 // the rows of all nodes in one matrix; 32 of one row over 256 x 64 keys 26 against 20), and
 // where there are fewer work-groups than CUs, eight waves take what four would over more
@@ -635,7 +638,7 @@ static Fp4Schedule find_fp4_schedule(const sc_plan* p, const sc_cache* c, size_t
         if (total > (double)kFp4Groups) continue;
         const int32_t per = total <= kCUs || waves == 8 ? 1 : total <= 2 * kCUs || tile == 32 ? 2 : 3;  // work-groups to a CU
         const double step = tile == 32 ? (per == 1 ? 2.3 : 3.8) : per == 1 ? 1.45 : per == 2 ? 2.0 : 3.0;
-        for (Fp4Items& i : items) {
+        for (Fp4Items& i : items) {  // from chunks to us
           const double left = std::fmod(i.us, 8.0);
           i.us = waves == 4 ? std::ceil(i.us / 4) * step + 1.0
                             : std::floor(i.us / 8) * 2.1 + (left > 4 ? 2.1 : left > 0 ? step : 0.0) + 1.6;
