@@ -60,40 +60,53 @@ struct RotateArgs {
   DivMagic units_div;
 };
 
-// 16 bytes of a tensor aligned to its elements, and its values as fp32.
-template <class T> struct RotRun;
-template <> struct RotRun<uint16_t> {
-  static constexpr int N = 8;
-  typedef uint32_t V __attribute__((ext_vector_type(4), aligned(2)));
+// N elements of a tensor aligned to them, and their values as fp32.
+template <class T, int N> struct RotRun;
+template <int N> struct RotRun<uint16_t, N> {
+  typedef uint32_t V __attribute__((ext_vector_type(N / 2), aligned(2)));
   static __device__ __forceinline__ float get(const V& v, int i) {
     return __uint_as_float(i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16);
   }
   static __device__ __forceinline__ V make(const float (&f)[N]) {
-    return V{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
+    V v;
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) v[i] = pack_bf16x2(f[2 * i], f[2 * i + 1]);
+    return v;
   }
   static __device__ __forceinline__ float one(uint16_t x) { return bf16_to_f32(x); }
   static __device__ __forceinline__ uint16_t back(float x) { return f32_to_bf16(x); }
 };
-template <> struct RotRun<float> {
-  static constexpr int N = 4;
-  typedef float V __attribute__((ext_vector_type(4), aligned(4)));
+template <int N> struct RotRun<float, N> {
+  typedef float V __attribute__((ext_vector_type(N), aligned(4)));
   static __device__ __forceinline__ float get(const V& v, int i) { return v[i]; }
-  static __device__ __forceinline__ V make(const float (&f)[N]) { return V{f[0], f[1], f[2], f[3]}; }
+  static __device__ __forceinline__ V make(const float (&f)[N]) {
+    V v;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = f[i];
+    return v;
+  }
   static __device__ __forceinline__ float one(float x) { return x; }
   static __device__ __forceinline__ float back(float x) { return x; }
 };
+template <bool PAST, class V>
+__device__ __forceinline__ V rot_load(const V* p) {
+  if constexpr (PAST) return __builtin_nontemporal_load(p);
+  return *p;
+}
 
-// A thread takes a run of pairs (of 16 bytes of channels; HALF: 16 bytes of either half) of one
-// row in HP heads, or a run of copied channels.  The row's cosines and sines are read
-// once for the heads, whose loads are all out before the first is used, and read past the
-// caches, which y gets.  Bound by memory where there are many rows: four nodes of 4680 rows of
-// 12 x 128 channels (115 MB) 24.6 us, 4.7 TB/s, as a plain copy runs (27.7 with loads that stay in the
-// caches, 25.7 with stores past them too, 57 with a pair a thread); by latency at few.
-template <class T, bool HALF, int HP>
+// A thread takes a run of pairs (N channels; HALF: N of either half) of one row in HP heads, or a
+// run of copied channels.  The row's cosines and sines are read once for the heads, whose loads
+// are all out before the first is used.  Bound by memory where there are many rows: four nodes of
+// 4680 rows of 12 x 128 channels (115 MB) 24.6 us, 4.7 TB/s, as a plain copy runs (57 with a pair a
+// thread); by latency at few.
+// N: 16 bytes, but 8 of bf16 halves, of which a thread has two (12000 rows of 12 heads of 128 18.3
+// us, 21.7 with 16; of 40, whose halves 16 bytes do not divide, 9.0, 22.9).  PAST: read past the
+// caches, which y gets (the four nodes 27.7 us without, 25.7 with y's stores past them too).
+template <class T, bool HALF, int N, int HP, bool PAST>
 __global__ __launch_bounds__(256) void rotate_kernel(const T* x, T* y, RotateArgs g) {
-  using Run = RotRun<T>;
+  using Run = RotRun<T, N>;
   using V = typename Run::V;
-  constexpr int N = Run::N, P = HALF ? N : N / 2;
+  constexpr int P = HALF ? N : N / 2;
   const uint32_t i = blockIdx.x * 256u + threadIdx.x;
   if (i >= (uint32_t)g.rows * (uint32_t)g.units) return;
   const int32_t r = (int32_t)fast_div(i, g.units_div), u = (int32_t)i - r * g.units, h0 = blockIdx.y * HP;
@@ -110,8 +123,8 @@ __global__ __launch_bounds__(256) void rotate_kernel(const T* x, T* y, RotateArg
 #pragma unroll
     for (int j = 0; j < HP; ++j) {
       const T* from = xr + min(h0 + j, g.heads - 1) * g.x_head;
-      a[j] = __builtin_nontemporal_load(reinterpret_cast<const V*>(from));
-      if (HALF && pairs) b[j] = __builtin_nontemporal_load(reinterpret_cast<const V*>(from + g.half));
+      a[j] = rot_load<PAST>(reinterpret_cast<const V*>(from));
+      if (HALF && pairs) b[j] = rot_load<PAST>(reinterpret_cast<const V*>(from + g.half));
     }
   if (!pairs) {
 #pragma unroll
@@ -169,16 +182,21 @@ __global__ __launch_bounds__(256) void rotate_kernel(const T* x, T* y, RotateArg
 }
 
 // Few rows: a head a thread, so that the work spreads over the CUs (12 heads of 128: 256 rows 2.7
-// us, 3.2 with four heads a thread; 1536 rows 3.9 either way, 4096 rows 6.9 against 5.8).
-template <class T, bool HALF>
+// us, 3.2 with four heads a thread; 1536 rows 3.9 either way, 4096 rows 6.9 against 5.8).  Else
+// past the caches where a thread's neighbours read lines to their ends: runs of 128 bytes or of
+// 64-byte pieces (12000 rows of 12 heads of 40 in bf16, 80 bytes each, 9.4 us past them, 8.1 not;
+// of 80 in fp32 20.6 and 23.3).
+template <class T, bool HALF, int N>
 static void launch_rotate_t(const void* x, void* y, const RotateArgs& g, hipStream_t s) {
-  const uint32_t groups = (uint32_t)(((int64_t)g.rows * g.units + 255) / 256);
+  const uint32_t groups = (uint32_t)(((int64_t)g.rows * g.units + 255) / 256), fours = (uint32_t)(g.heads + 3) / 4;
   const T* xt = static_cast<const T*>(x);
   T* yt = static_cast<T*>(y);
-  if ((int64_t)groups * ((g.heads + 3) / 4) < 3 * kCUs / 2)
-    hipLaunchKernelGGL((rotate_kernel<T, HALF, 1>), dim3(groups, (uint32_t)g.heads), dim3(256), 0, s, xt, yt, g);
+  if ((int64_t)groups * fours < 3 * kCUs / 2)
+    hipLaunchKernelGGL((rotate_kernel<T, HALF, N, 1, false>), dim3(groups, (uint32_t)g.heads), dim3(256), 0, s, xt, yt, g);
+  else if (const size_t bytes = g.half * (HALF ? 1 : 2) * sizeof(T); bytes >= 128 || bytes % 64 == 0)
+    hipLaunchKernelGGL((rotate_kernel<T, HALF, N, 4, true>), dim3(groups, fours), dim3(256), 0, s, xt, yt, g);
   else
-    hipLaunchKernelGGL((rotate_kernel<T, HALF, 4>), dim3(groups, (uint32_t)(g.heads + 3) / 4), dim3(256), 0, s, xt, yt, g);
+    hipLaunchKernelGGL((rotate_kernel<T, HALF, N, 4, false>), dim3(groups, fours), dim3(256), 0, s, xt, yt, g);
 }
 
 }  // namespace sc
@@ -262,7 +280,7 @@ extern "C" int sc_rope_rotate(const sc_rope* rope, const sc_rotate_desc* d, cons
   g.rest = in_place ? 0 : (int32_t)(d->head_dim - part);
   g.sign = d->transpose ? -1.f : 1.f;
   const bool f32 = d->dtype == SC_DTYPE_F32, halves = d->layout == SC_ROPE_HALF;
-  const int32_t run = 16 / (int32_t)es, run_pairs = halves ? run : run / 2;
+  const int32_t run = f32 || halves ? 4 : 8, run_pairs = halves ? run : run / 2;
   g.pair_units = (g.half + run_pairs - 1) / run_pairs;
   g.units = g.pair_units + (g.rest + run - 1) / run;
   g.units_div = magic_div((uint32_t)g.units);
@@ -276,13 +294,13 @@ extern "C" int sc_rope_rotate(const sc_rope* rope, const sc_rotate_desc* d, cons
     char* to = static_cast<char*>(y) + row * d->y_row * (int64_t)es;
     timer_begin(TK_ROTATE, s);
     if (f32 && halves)
-      launch_rotate_t<float, true>(from, to, g, s);
+      launch_rotate_t<float, true, 4>(from, to, g, s);
     else if (f32)
-      launch_rotate_t<float, false>(from, to, g, s);
+      launch_rotate_t<float, false, 4>(from, to, g, s);
     else if (halves)
-      launch_rotate_t<uint16_t, true>(from, to, g, s);
+      launch_rotate_t<uint16_t, true, 4>(from, to, g, s);
     else
-      launch_rotate_t<uint16_t, false>(from, to, g, s);
+      launch_rotate_t<uint16_t, false, 8>(from, to, g, s);
     timer_end(TK_ROTATE, s);
     SC_HIP(hipGetLastError());
   }

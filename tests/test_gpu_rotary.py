@@ -162,6 +162,21 @@ def test_strides_padding_and_shared_rows(layout, dtype):
     assert torch.equal(x[pad].contiguous(), before[pad, 1:1 + heads * hd].unflatten(1, (heads, hd)))
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("layout", ["interleaved", "half"])
+@pytest.mark.parametrize("rows,heads,head_dim,dims", [
+    (9001, 5, 40, (14, 14, 12)), (9000, 6, 44, (10, 6, 6)), (9000, 9, 34, (26, 0, 0)), (9000, 4, 80, (28, 26, 26)), (9001, 7, 128, (64, 0, 0))])
+def test_rows_by_four_heads(rows, heads, head_dim, dims, layout, dtype):
+    """Many rows, whose threads take four heads each: odd numbers of heads, runs that end inside the
+    rotated part and inside the rest, reads that stay in the caches and that do not."""
+    x = torch.from_numpy(normal((rows, heads, head_dim), (3, heads)).astype(np.float32)).to(dtype).cuda()
+    pos, pd = _positions(rows, seed=heads)
+    y = torch.full_like(x, float("nan"))
+    sc.sc_rope_rotate(_rope(dims), x, y, pd, layout=layout)
+    torch.cuda.synchronize()
+    _check(y.cpu().double().numpy(), x.cpu().double().numpy(), pos, dims, layout, False, None, dtype)
+
+
 def test_many_rows_and_far_offsets():
     """More elements than 2^31 in the tensor that the rows are strided through."""
     rows, stride = 70000, 40000  # 2.8e9 elements between the first and the last row
