@@ -567,10 +567,10 @@ static double fp4_makespan(double slots, const std::vector<Fp4Items>& items) {
 }
 
 // The cheapest way within `room` bytes, by estimated time in us.  Measured (2 .. 12 heads, 1 ..
-// 1024 rows a node, 512 .. 262144 keys, 700 ways of cutting them; what is chosen is within
-// 10 % of the best of them): four chunks, one to each wave of a work-group, take
-//   tiles of 16 rows  1.45 with one work-group to a CU, 2.0 with two, 3.0 with three
-//   tiles of 32 rows  2.3 with one, 3.8 with two
+// 1024 rows a node, 512 .. 262144 keys, 2000 ways of cutting them; what is chosen is within
+// 6 % of the best of them): four chunks, one to each wave of a work-group, take
+//   tiles of 16 rows  1.45 with one work-group to a CU, 2.0 with two, 3.05 with three
+//   tiles of 32 rows  2.3 with one, 3.75 with two
 // and eight chunks, one to each of eight waves, of which a CU has room for one work-group, 2.1
 // (the last four or fewer 1.45).  An item is 1 more, 1.6 with eight waves, a launch 3, no less
 // than the pages take from HBM at 5.6 MB per us; joining pieces 3.5, 0.13 per piece and the
@@ -637,11 +637,19 @@ static Fp4Schedule find_fp4_schedule(const sc_plan* p, const sc_cache* c, size_t
         for (const auto& o : own) add((double)own_tiles * o.second, fp4_chunks(c, o.first + (joined ? p->shared : 0)), o_len);
         if (total > (double)kFp4Groups) continue;
         const int32_t per = total <= kCUs || waves == 8 ? 1 : total <= 2 * kCUs || tile == 32 ? 2 : 3;  // work-groups to a CU
-        const double step = tile == 32 ? (per == 1 ? 2.3 : 3.8) : per == 1 ? 1.45 : per == 2 ? 2.0 : 3.0;
-        for (Fp4Items& i : items) {  // from chunks to us
-          const double left = std::fmod(i.us, 8.0);
-          i.us = waves == 4 ? std::ceil(i.us / 4) * step + 1.0
-                            : std::floor(i.us / 8) * 2.1 + (left > 4 ? 2.1 : left > 0 ? step : 0.0) + 1.6;
+        const auto step = [&](int32_t k) { return tile == 32 ? (k == 1 ? 2.3 : 3.75) : k == 1 ? 1.45 : k == 2 ? 2.0 : 3.05; };
+        // items of a last round that leaves a CU fewer work-groups run as those do
+        const double rest = std::fmod(total, (double)kCUs * per);
+        const int32_t rest_per = std::max(1, (int32_t)std::ceil(rest / kCUs));
+        const size_t at_full = items.size();
+        if (rest > 0 && rest < total && rest_per < per) {
+          items.push_back({std::min(rest, items.back().count), items.back().us});
+          items[at_full - 1].count -= items.back().count;
+        }
+        for (size_t i = 0; i < items.size(); ++i) {  // from chunks to us
+          const double n = items[i].us, left = std::fmod(n, 8.0), one = step(i < at_full ? per : rest_per);
+          items[i].us = waves == 4 ? std::ceil(n / 4) * one + 1.0
+                                   : std::floor(n / 8) * 2.1 + (left > 4 ? 2.1 : left > 0 ? one : 0.0) + 1.6;
         }
         s.us = std::max(fp4_makespan((double)kCUs * per, items), from_hbm) + 3.0;
         if (s.bytes) s.us += 3.5 + 0.13 * (double)all + (double)s.bytes / 2.2e6;
