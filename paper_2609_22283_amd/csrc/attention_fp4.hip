@@ -81,6 +81,7 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef short i16x2 __attribute__((ext_vector_type(2)));
 
 constexpr float kFp4Rise = 40.f;  // sums of 2^31 keys in units of 2^m stay below 2^(40 + 31)
+constexpr float kFp4Far = 4194304.f;  // 2^22: steps of fp32 below it are a quarter at most
 constexpr int FA_ROW = 132;   // floats of a row of partial outputs in LDS
 
 // The scaled instruction's operands: c + A B over 128: A 16 rows of codes (a lane: row lane % 16, the 32 columns of group lane / 16)
@@ -314,17 +315,28 @@ __global__ __launch_bounds__(64 * NW, R == 1 && NW == 4 ? 3 : 2) void fp4_attent
       for (int b = 0; b < 8; ++b)
 #pragma unroll
         for (int i = 0; i < 4; ++i) top = fmaxf(top, s[b][i]);
-      const float e = fmaxf(ceilf(quarters_max(top) * g.unit), -1e30f);
-      if (__any(e > m[r] + kFp4Rise)) {
+      top = quarters_max(top);
+      const float t = top * g.unit, e = fmaxf(ceilf(t), -FLT_MAX);
+      float shift = 8.f - e;
+      if (__any(e - m[r] > kFp4Rise || fabsf(t) > kFp4Far)) {
         const float to = fmaxf(m[r], e), keep = __builtin_amdgcn_exp2f(m[r] - to);
         sum[r] *= keep;
 #pragma unroll
         for (int n = 0; n < 8; ++n) acc[r][n] *= keep;
         m[r] = to;
+        // From there on neither 8 - e nor how far t is below e is exact enough for exponentials of
+        // 2^8 at most: the logits' distances from the chunk's largest are (which counts as the
+        // fp32 number t, 2^-24 of it).  Without a number for t, above them all, the rows are NaN, and
+        // below them all the chunk has no weight.
+        const bool far = fabsf(t) > kFp4Far;
+        const float from = far && top > -INFINITY ? top : 0.f;
+        if (far) shift = 8.f - (e - t);
+#pragma unroll
+        for (int b = 0; b < 8; ++b) s[b] -= from;
       }
       const int32_t d = (int32_t)fminf(fmaxf(e - m[r], -300.f), 100.f);
       psc[r] = (uint32_t)max(d + 119, 0) | (uint32_t)max(d + 115, 0) << 8;
-      return 8.f - e;
+      return shift;
     };
     const auto exponentials = [&](int r, f32x4 (&s)[8], float shift) __attribute__((always_inline)) {
 #pragma unroll
