@@ -718,7 +718,9 @@ int launch_fp4_attention(const sc_plan* p, const sc_cache* c, int32_t layer, con
     const int rc = launch_page_convert(false, PoolView{c->pool + (size_t)layer * c->d.n_slots * c->slot_bytes, 0},
                                        PoolView{w.cache.pool, 0}, c->d, pairs, 1, stream);
     if (rc != SC_OK) return rc;
-    return launch_attention_exact(&w.plan, &w.cache, 0, q, o, scale, w.cache.pool + align256(w.page_bytes), stream);
+    // times log2(e) it has to be a number, or rows of zeros come out NaN
+    const float by = std::min(std::max(scale, -2.35e38f), 2.35e38f);
+    return launch_attention_exact(&w.plan, &w.cache, 0, q, o, by, w.cache.pool + align256(w.page_bytes), stream);
   }
   Fp4List l;
   Fp4Geom g;

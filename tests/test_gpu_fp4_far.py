@@ -125,3 +125,17 @@ def test_logits_that_fp32_does_not_hold(shape, tile, waves):
         want = v.mean(0)
         for r in (0, nq // 2, nq - 1):
             check(got[i * nq + r], want, 2.0 ** -8 * (np.abs(want) + np.abs(v).mean(0)), f"node {i}, row {r}")
+
+
+@pytest.mark.parametrize("shape,tile,waves", SHAPES)
+def test_rows_of_zeros_at_the_largest_scales(shape, tile, waves):
+    h, plan, reads = _case(shape, lambda st, n: np.where(np.arange(n) % 2 == 0, 0.0, -4.0))
+    nodes, nq = shape[-2:]
+    qd, _ = bf16_dev(np.zeros((nodes * nq, h.heads, D), np.float32))
+    for scale in (3e38, -3e38):
+        got = attend(h, plan, qd, scale)
+        for i, states in enumerate(reads):
+            v = np.concatenate([h.v[s] for s in states])
+            want = v.mean(0)
+            for r in (0, nq // 2, nq - 1):
+                check(got[i * nq + r], want, 2.0 ** -8 * (np.abs(want) + np.abs(v).mean(0)), f"node {i}, row {r}, scale {scale}")
