@@ -303,7 +303,8 @@ int sc_plan_condition(sc_cache* cache, const sc_node* conditions, int32_t n, int
  * long key ranges across work-groups and merges their partial softmax sums
  * there, and so does any that reads a shared prefix once; over a 4-bit cache
  * long nodes have their distinct pages of the layer taken out there as bf16 and
- * read by the bf16 forms.  Its contents are undefined on return; calls sharing
+ * read by the bf16 forms (for a plan over one that sc_attention would refuse as stale or
+ * unsupported the size is 0).  Its contents are undefined on return; calls sharing
  * one workspace must be ordered on one stream.  Errors: SC_ESTALE, SC_EUNAVAILABLE (a page's state not written at
  * this layer), SC_EINVAL (workspace too small or misaligned), SC_EUNSUPPORTED,
  * SC_EDEVICE. */

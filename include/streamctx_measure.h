@@ -52,7 +52,8 @@ int sc_timer_read(const char* kind, int32_t* launches, double* total_ms);
  * *tile_features, *tile_tokens: output tile per work-group; *ring: 64-k stages
  * in its LDS ring; *parts: work-groups that share a tile's contraction.
  * Errors: SC_EINVAL (null pointer, plan of another cache or without nodes,
- * unknown kind), SC_EUNSUPPORTED (shapes that the call refuses). */
+ * unknown kind), SC_EUNSUPPORTED (shapes that the call refuses), SC_ESTALE (a plan over
+ * 4-bit pages that have been released or moved). */
 int sc_attention_form(const sc_plan* plan, const sc_cache* cache, int32_t* queries, int32_t* ring,
                       int32_t* pieces);
 int sc_gemm_form(const char* kind, int32_t n_features, int32_t n_tokens, int32_t k,

@@ -516,7 +516,8 @@ static int64_t fp4_chunks(const sc_cache* c, int64_t pages) {
 static std::shared_ptr<Fp4Wide> fp4_wide(const sc_plan* p, const sc_cache* c) {
   if (c->d.tokens_per_page < (p->shared || p->nq <= 64 ? 32 : 64)) return nullptr;
   auto w = std::make_shared<Fp4Wide>();
-  std::vector<int32_t> place(c->d.n_slots, -1);
+  const auto last = std::max_element(p->page_slot.begin(), p->page_slot.end());
+  std::vector<int32_t> place(last == p->page_slot.end() ? 0 : *last + 1, -1);
   const auto put = [&](int32_t s) {
     if (place[s] < 0) {
       place[s] = (int32_t)w->src.size();
@@ -764,6 +765,8 @@ int launch_fp4_attention(const sc_plan* p, const sc_cache* c, int32_t layer, con
 }
 
 int fp4_attention_form(const sc_plan* p, const sc_cache* c, int32_t* queries, int32_t* ring, int32_t* pieces) {
+  const int rc = plan_current(p, c);
+  if (rc != SC_OK) return rc;
   const Fp4Schedule* s = fp4_schedule(p, c, SIZE_MAX);
   if (!s) return fail(SC_EINVAL, "out of host memory");
   *queries = s->wide ? 0 : s->tile;

@@ -27,23 +27,30 @@ int hip_fail(hipError_t e, const char* what) {
   return fail(SC_EDEVICE, "%s failed: %s", what, hipGetErrorString(e));
 }
 
-int plan_check(const sc_plan* plan, const sc_cache* cache, int32_t layer) {
-  if (plan->cache != cache) return fail(SC_EINVAL, "plan was built for another cache");
-  if (layer < 0 || layer >= cache->d.n_layers)
-    return fail(SC_EINVAL, "layer %d outside [0, %d)", layer, cache->d.n_layers);
-  // pages that every node's list starts with are looked at once
-  const int32_t n = (int32_t)plan->nodes.size();
-  const auto first = [&](int32_t i) { return (size_t)plan->page_off[i] + (i ? plan->shared : 0); };
-  for (int32_t i = 0; i < n; ++i)
-    for (size_t p = first(i); p < (size_t)plan->page_off[i + 1]; ++p) {
+// Where node i's pages start that need a look: those that every node's list starts with
+// are looked at once.
+static size_t first_page(const sc_plan* plan, int32_t i) { return (size_t)plan->page_off[i] + (i ? plan->shared : 0); }
+
+int plan_current(const sc_plan* plan, const sc_cache* cache) {
+  for (int32_t i = 0; i < (int32_t)plan->nodes.size(); ++i)
+    for (size_t p = first_page(plan, i); p < (size_t)plan->page_off[i + 1]; ++p) {
       int32_t s = plan->page_slot[p];
       if (!page_current(cache, s, plan->page_gen[p]))
         return fail(SC_ESTALE, "slot %d was released after the plan was built", s);
     }
+  return SC_OK;
+}
+
+int plan_check(const sc_plan* plan, const sc_cache* cache, int32_t layer) {
+  if (plan->cache != cache) return fail(SC_EINVAL, "plan was built for another cache");
+  if (layer < 0 || layer >= cache->d.n_layers)
+    return fail(SC_EINVAL, "layer %d outside [0, %d)", layer, cache->d.n_layers);
+  const int rc = plan_current(plan, cache);
+  if (rc != SC_OK) return rc;
   // every slot is still the one planned (above), so its flag is its state's
   const uint8_t* wr = cache->table->written.data() + (size_t)layer * cache->d.n_slots;
-  for (int32_t i = 0; i < n; ++i)
-    for (size_t p = first(i); p < (size_t)plan->page_off[i + 1]; ++p)
+  for (int32_t i = 0; i < (int32_t)plan->nodes.size(); ++i)
+    for (size_t p = first_page(plan, i); p < (size_t)plan->page_off[i + 1]; ++p)
       if (!wr[plan->page_slot[p]])
         return fail(SC_EUNAVAILABLE, "state (%d,%d) has no K/V at layer %d",
                     plan->page_state[p].first, plan->page_state[p].second, layer);
@@ -467,6 +474,8 @@ int sc_plan_condition(sc_cache* c, const sc_node* conds, int32_t n, int32_t nq, 
 
 size_t sc_attention_workspace_bytes(const sc_plan* p, const sc_cache* c) {
   if (!p || !c || p->cache != c) return 0;
+  // over 4-bit pages the size goes by which pages they are
+  if (c->d.dtype == SC_DTYPE_FP4 && (plan_current(p, c) != SC_OK || attention_check(p, c) != SC_OK)) return 0;
   return attention_workspace_bytes(p, c);
 }
 

@@ -99,6 +99,8 @@ namespace sc {
 // Validates a plan against the cache for reading `layer` (generations and
 // written flags).  Returns SC_OK or an error code with the message set.
 int plan_check(const sc_plan* plan, const sc_cache* cache, int32_t layer);
+// SC_ESTALE where one of a plan's pages has been released or moved since it was built.
+int plan_current(const sc_plan* plan, const sc_cache* cache);
 
 // The entry of a state about to be written at `layer`, its slots allocated if it
 // is new (*fresh: release it if the write fails).
@@ -193,7 +195,7 @@ int launch_fp4_append(const sc_cache* cache, int32_t layer, const int32_t* slots
                       const void* v, const sc_rope* rope, hipStream_t stream);
 
 // Launchers of attention_fp4.hip: the attention over 4-bit pages.  attention_check has accepted
-// the plan.
+// the plan, and its pages are current (fp4_attention_form looks for itself).
 size_t fp4_attention_workspace_bytes(const sc_plan* plan, const sc_cache* cache);
 // The cheapest way within `room` bytes at ws.
 int launch_fp4_attention(const sc_plan* plan, const sc_cache* cache, int32_t layer, const void* q, void* o, float scale,
