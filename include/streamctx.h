@@ -236,8 +236,10 @@ int sc_cache_copy(const sc_cache* from, const sc_node* states, int32_t n, sc_cac
  * branches: pages are shared, nothing is copied, and what either handle appends or releases
  * from then on is its own (a slot is free once no handle holds it).  Every state must be
  * written in every layer.  Plans belong to the handle that they were built with.  Handles
- * over one pool are used by one thread at a time, like one handle; weights kept beside the
- * cache go by slots, which the handles share.  Free it with sc_cache_free.
+ * over one pool are used by one thread at a time, like one handle, and what they launch on
+ * different streams is ordered by the caller: a slot that is free on the host, or a pool
+ * left behind by sc_cache_move, may still be read by work on another stream.  Weights kept
+ * beside the cache go by slots, which the handles share.  Free it with sc_cache_free.
  * Errors: SC_EINVAL, SC_EUNAVAILABLE (a state not written at some layer). */
 int sc_cache_fork(sc_cache* cache, sc_cache** out);
 /* Moves pages, in every layer, until the slots in use (of all handles over the pool) are the
@@ -248,7 +250,7 @@ int sc_cache_compact(sc_cache* cache, float* weights, sc_stream stream);
 /* Moves the pages to another pool, of n_slots slots (sc_cache_pool_bytes with that many), in
  * the order of their slots from slot 0 on; every handle over the old pool is over the new
  * one afterwards, and all plans are stale.  The old pool is read asynchronously on the
- * stream and not used after that.  weights, moved_weights: the array kept beside the cache
+ * stream, behind what the handles launched before, and not used after that.  weights, moved_weights: the array kept beside the cache
  * and the one that takes its place, or both NULL; rows of slots in use are moved.
  * Errors (nothing has changed): SC_EINVAL (null argument, n_slots < 1, overlapping pools or
  * weights, one of the weights without the other), SC_ECAPACITY (more slots in use),

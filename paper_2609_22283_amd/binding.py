@@ -321,6 +321,16 @@ def sc_selection_build(kind, K, W, nodes: Sequence[Tuple[int, int]], phi_table=N
 
 
 # ---------------------------------------------------------------------- cache
+_default_streams = {}
+
+
+def _default_stream(device):
+    """torch's default stream of a device, whose raw integer is 0."""
+    if device not in _default_streams:
+        _default_streams[device] = _torch.cuda.default_stream(device)
+    return _default_streams[device]
+
+
 def _nodes(states):
     if len(states) == 1:  # without an array type: 0.7 us less
         (c, j), = states
@@ -414,13 +424,16 @@ class Cache:
 
     def move(self, pool, n_slots: int, weights=None, moved_weights=None, stream=None) -> None:
         """Move the pages of this cache and its forks to ``pool``, of ``n_slots`` slots, in the order
-        of their slots (and the rows of ``weights`` to ``moved_weights``)."""
+        of their slots (and the rows of ``weights`` to ``moved_weights``).  The handles let go of the old
+        pool here, and torch's allocator hands its memory out again behind the work on ``stream``: what
+        reads it on other streams (the attention of a fork) has to be ordered before that, or the
+        caller holds the old pool until it is over."""
         on, old = _stream(stream), self._held[0]
         _check(lib.sc_cache_move(self._h, _ptr(pool), n_slots, _ptr(weights), _ptr(moved_weights), on))
-        if on and hasattr(old, "record_stream"):  # it may go back to torch's allocator here
-            old.record_stream(_torch.cuda.ExternalStream(on, device=old.device))
         self._held[0] = pool
         self.desc.n_slots = n_slots
+        if getattr(old, "is_cuda", False):  # its allocator knows the stream that it was allocated on alone
+            old.record_stream(_torch.cuda.ExternalStream(on, device=old.device) if on else _default_stream(old.device))
 
 
 def sc_cache_create(pool, n_layers, n_heads, head_dim, tokens_per_page, pages_per_chunk, n_slots,
