@@ -250,7 +250,7 @@ int sc_cache_compact(sc_cache* cache, float* weights, sc_stream stream);
 /* Moves the pages to another pool, of n_slots slots (sc_cache_pool_bytes with that many), in
  * the order of their slots from slot 0 on; every handle over the old pool is over the new
  * one afterwards, and all plans are stale.  The old pool is read asynchronously on the
- * stream, behind what the handles launched before, and not used after that.  weights, moved_weights: the array kept beside the cache
+ * stream and not used after that.  weights, moved_weights: the array kept beside the cache
  * and the one that takes its place, or both NULL; rows of slots in use are moved.
  * Errors (nothing has changed): SC_EINVAL (null argument, n_slots < 1, overlapping pools or
  * weights, one of the weights without the other), SC_ECAPACITY (more slots in use),

@@ -20,18 +20,19 @@
 #include <new>
 #include <vector>
 
+#include "attention_core.h"
 #include "fp4.h"
 
 namespace sc {
 
-constexpr int kFp4Nodes = 64, kFp4Pages = 800;  // of a plan (attention_check)
 constexpr int64_t kFp4Groups = UINT32_MAX / 256;  // work-groups of a launch (256 threads each, numbered in 32 bits)
 
-// A plan's pages: the prefix that all nodes read first, then the nodes' own.
+// A plan's pages (no more than attention_check lets through): the prefix that all nodes read first,
+// then the nodes' own.
 struct Fp4List {
   int32_t shared;
-  int32_t off[kFp4Nodes + 1];
-  int32_t slot[kFp4Pages];
+  int32_t off[kMaxNodes + 1];
+  int32_t slot[kMaxPages];
 };
 struct Fp4Geom {
   const char* layer_base;
@@ -61,7 +62,7 @@ static void fp4_fill(const sc_plan* p, const sc_cache* c, int32_t layer, float s
     l.off[i] = at;
     for (int32_t k = p->page_off[i] + p->shared; k < p->page_off[i + 1]; ++k) l.slot[at++] = p->page_slot[k];
   }
-  for (int32_t i = n; i <= kFp4Nodes; ++i) l.off[i] = at;
+  for (int32_t i = n; i <= kMaxNodes; ++i) l.off[i] = at;
   g.layer_base = c->pool + (size_t)layer * d.n_slots * c->slot_bytes;
   g.slot_bytes = c->slot_bytes;
   g.heads = d.n_heads;
@@ -210,7 +211,7 @@ __global__ __launch_bounds__(64 * NW, R == 1 && NW == 4 ? 3 : 2) void fp4_attent
     const uint16_t* __restrict__ q, uint16_t* __restrict__ o, Fp4Geom g, Fp4List list) {
   __shared__ __attribute__((aligned(16))) float part[NW][16 * FA_ROW];
   __shared__ float ml[NW][2][16];
-  __shared__ uint64_t base[kFp4Pages];
+  __shared__ uint64_t base[kMaxPages];
   __shared__ u32x4 qs[R][4][64];         // the queries' operands: halves of hi, halves of lo
   __shared__ uint32_t q_scale[R][16];
   const int32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -542,7 +543,7 @@ static std::shared_ptr<Fp4Wide> fp4_wide(const sc_plan* p, const sc_cache* c) {
   w->page_bytes = w->src.size() * w->cache.slot_bytes;
   w->plan.nodes = p->nodes;
   w->plan.page_off = p->page_off;
-  if (p->page_slot.size() <= (size_t)kFp4Pages) w->plan.page_state = p->page_state;  // of lists that one launch reads whole
+  if (p->page_slot.size() <= (size_t)kMaxPages) w->plan.page_state = p->page_state;  // of lists that one launch reads whole
   w->plan.cache = &w->cache;
   w->plan.nq = p->nq;
   w->plan.shared = p->shared;
