@@ -484,7 +484,7 @@ def sc_rope_rotate(rope: Rope, x, y, positions, layout: str = "interleaved", tra
                    stream=None) -> None:
     """Rotate the rows of ``x`` [rows, heads, head_dim] (bf16 or fp32, any strides between rows
     and heads) at ``positions`` (int32 [rows, 3]) into ``y``, of the same shape and dtype; ``y``
-    may be ``x``."""
+    may be ``x``.  All three are on one GPU, without ``stream`` the current one."""
     dtype = _ROTATED.get(x.dtype)
     xs, ys, shape = x.stride(), y.stride(), x.shape
     if (len(xs) != 3 or y.shape != shape or dtype is None or y.dtype != x.dtype or
@@ -493,6 +493,10 @@ def sc_rope_rotate(rope: Rope, x, y, positions, layout: str = "interleaved", tra
                                  f"channels, the layout one of {sorted(ROPE_LAYOUTS)}")
     if tuple(positions.shape) != (shape[0], 3) or positions.dtype != _torch.int32 or not positions.is_contiguous():
         raise ScError(SC_EINVAL, "SC_EINVAL: positions are contiguous int32 [rows, 3]")
+    on = x.get_device()  # -1 in host memory, which a kernel must not be given
+    if (on < 0 or y.get_device() != on or positions.get_device() != on or
+            (stream is None and on != _torch.cuda.current_device())):
+        raise ScError(SC_EINVAL, "SC_EINVAL: x, y and positions are tensors of one GPU, the current one unless a stream is given")
     d = sc_rotate_desc(shape[0], shape[1], shape[2], dtype, ROPE_LAYOUTS[layout], 1 if transpose else 0,
                        xs[0], xs[1], ys[0], ys[1])
     _check(lib.sc_rope_rotate(C.byref(rope.struct), C.byref(d), _ptr(x), _ptr(y), _ptr(positions), _stream(stream)))
