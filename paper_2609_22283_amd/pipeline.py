@@ -96,6 +96,7 @@ class StackPipeline:
         (a stack takes its layers' first RMSNorm factors from sums that the
         layer before stored)."""
         self._refuse_hooks(layer_hook)
+        self._refuse_other_weights()
         n = self.n_tok
         sel = sc.sc_selection_build(self.policy, self.K, self.W, nodes)
         plan = sc.sc_plan_build(sel, self.cache)
@@ -140,9 +141,15 @@ class StackPipeline:
         if self.weights is not None and any(h is not None for h in hooks):
             raise ValueError("layer hooks observe single blocks; a stack with a memory runs in one call")
 
+    def _refuse_other_weights(self) -> None:
+        if self.weights is not None and self.weights.shape[1] != self.cache.desc.n_slots:
+            raise ValueError(f"the weights are those of {self.weights.shape[1]} slots, the cache has {self.cache.desc.n_slots}: "
+                             "after Cache.move(..., weights, moved_weights) the pipeline's weights are the moved ones")
+
     def _fold_unread(self, future: Sequence[Tuple[int, int]]) -> None:
         """Release what no node of ``future`` selects, the clean states among it
         into the memory; the memory too once nothing is left to read it."""
+        self._refuse_other_weights()
         off, chunk, level, _ = sc.sc_selection_build(self.policy, self.K, self.W, future).tables()
         needed = {(chunk[s], level[s]) for i in range(len(future)) for s in range(off[i], off[i + 1] - 1)}
         unread = sorted(self.cached - needed)
