@@ -108,7 +108,7 @@ int sc::block_check(const sc_block_weights* w, const sc_cache* c, int32_t layer,
     if (it->second.written[layer])
       return fail(SC_EEXIST, "pack state (%d,%d) already written at layer %d", p->nodes[i].chunk,
                   p->nodes[i].level, layer);
-    if (rope && (p->nodes[i].chunk + 1) * d.pages_per_chunk > rope->desc.max_frames)
+    if (rope && ((int64_t)p->nodes[i].chunk + 1) * d.pages_per_chunk > rope->desc.max_frames)
       return fail(SC_EINVAL, "chunk %d beyond the rope table", p->nodes[i].chunk);
   }
   for (size_t q = 0; q < p->page_slot.size(); ++q) {

@@ -360,7 +360,7 @@ int sc_cache_append(sc_cache* c, int32_t layer, sc_node st, const void* k, const
     if (!rope->dev_table || r.grid_h * r.grid_w != c->d.tokens_per_page ||
         r.dim_t + r.dim_h + r.dim_w != c->d.head_dim || (r.dim_t | r.dim_h | r.dim_w) & 1)
       return fail(SC_EINVAL, "rope descriptor does not match the cache geometry");
-    if ((st.chunk + 1) * c->d.pages_per_chunk > r.max_frames)
+    if (((int64_t)st.chunk + 1) * c->d.pages_per_chunk > r.max_frames)
       return fail(SC_EINVAL, "chunk %d beyond the rope table's %d frames", st.chunk, r.max_frames);
   }
   StateEntry* e = nullptr;
