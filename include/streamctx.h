@@ -119,7 +119,7 @@ void sc_selection_free(sc_selection* sel);
  * tokens_per_page a positive multiple of 8, head_dim 64 or 128 (bf16: 128).
  * The pool must outlive the cache handle.
  *
- * SC_DTYPE_FP4 (head_dim 128, a 16-byte aligned pool) holds keys and values in 4 bits:
+ * SC_DTYPE_FP4 (head_dim 128, pages of at most 2^24 tokens, a 16-byte aligned pool) holds keys and values in 4 bits:
  * e2m1 codes (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) times a power of two
  * shared by 32 of them, 4.25 bits a value.  A group is 32 channels of a key, or a
  * channel of V over 32 tokens of its page (tokens 32 b .. 32 b + 31; fewer at the

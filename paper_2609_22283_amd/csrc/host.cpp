@@ -227,6 +227,8 @@ static int validate_desc(const sc_cache_desc* d) {
     return fail(SC_EUNSUPPORTED, "head_dim must be 64 or 128 (got %d)", d->head_dim);
   if (d->dtype == SC_DTYPE_FP4 && d->head_dim != 128)
     return fail(SC_EUNSUPPORTED, "4-bit caches need head_dim 128 (got %d)", d->head_dim);
+  if (d->dtype == SC_DTYPE_FP4 && d->tokens_per_page > kFp4PageTokens)
+    return fail(SC_EUNSUPPORTED, "4-bit pages hold at most %d tokens (got %d)", kFp4PageTokens, d->tokens_per_page);
   return SC_OK;
 }
 

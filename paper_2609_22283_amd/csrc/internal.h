@@ -55,6 +55,8 @@ inline size_t dtype_size(int32_t dtype) { return dtype == SC_DTYPE_F32 ? 4 : 2; 
 // padded; a slot is [head][block].
 constexpr int32_t kFp4Tokens = 32;    // tokens of a block
 constexpr int32_t kFp4Block = 4352;   // bytes of a block
+constexpr int32_t kFp4PageTokens = 1 << 24;  // of a page: the attention counts a head's bytes of it in 32 bits
+static_assert((uint64_t)kFp4PageTokens / kFp4Tokens * kFp4Block <= UINT32_MAX, "");
 inline int32_t fp4_blocks(int32_t tokens_per_page) { return (tokens_per_page + kFp4Tokens - 1) / kFp4Tokens; }
 
 }  // namespace sc

@@ -26,6 +26,18 @@ def test_what_is_planned(prefix, nodes, nq):
     assert e.value.code == sc.SC_EUNSUPPORTED and sc.sc_attention_workspace_bytes(plan, cache) == 0
 
 
+def test_pages_whose_bytes_32_bits_count():
+    """CPU only: a page of 2^25 tokens has more than 4 GiB a head, which the attention would read in the wrong places."""
+    def pool(tokens, dtype=sc.SC_DTYPE_FP4):
+        return sc.sc_cache_pool_bytes(1, 1, 128, tokens, 1, 1, dtype)
+    assert pool(1 << 24) == (1 << 24) // 32 * 4352 and pool(1 << 25, sc.SC_DTYPE_BF16) == 512 << 25
+    for tokens in ((1 << 24) + 8, 1 << 25, (1 << 31) - 8):
+        assert pool(tokens) == 0
+        with pytest.raises(sc.ScError) as e:
+            sc.sc_cache_create(1 << 20, 1, 1, 128, tokens, 1, 1, sc.SC_DTYPE_FP4)
+        assert e.value.code == sc.SC_EUNSUPPORTED
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("prefix,nodes", FULL)
 @pytest.mark.parametrize("nq", [1, 40])
