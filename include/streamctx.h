@@ -297,17 +297,19 @@ int sc_plan_condition(sc_cache* cache, const sc_node* conditions, int32_t n, int
  * SC_EUNSUPPORTED before anything is launched.  bf16 caches need head_dim
  * 128 and pages of at least one key tile: 32 tokens when Nq <= 64, 64
  * otherwise (else SC_EUNSUPPORTED).  4-bit caches: q and o are bf16, logits
- * are products of q as it is and of the values that the codes stand for; q
- * 16-byte aligned, a finite scale and at most 2^31 - 1 rows (else SC_EINVAL,
- * SC_EUNSUPPORTED).  ws: device scratch, 16-byte aligned, of at least
+ * are products of q and of the values that the codes stand for, each
+ * channel of q exact or to 2^-21 of its row's largest; q 16-byte aligned, a
+ * finite scale and at most 2^31 - 1 rows (else SC_EINVAL, SC_EUNSUPPORTED).
+ * ws: device scratch, 16-byte aligned, of at least
  * sc_attention_workspace_bytes(plan, cache) bytes (may be NULL when that is
  * 0, as for fp32 caches unless the nodes share a prefix); the bf16 kernel splits
  * long key ranges across work-groups and merges their partial softmax sums
  * there, and so does any that reads a shared prefix once; over a 4-bit cache
  * long nodes have their distinct pages of the layer taken out there as bf16 and
- * read by the bf16 forms (for a plan over one that sc_attention would refuse as stale or
- * unsupported the size is 0).  Its contents are undefined on return; calls sharing
- * one workspace must be ordered on one stream.  Errors: SC_ESTALE, SC_EUNAVAILABLE (a page's state not written at
+ * read by the bf16 forms (for a plan over one that sc_attention would refuse
+ * as stale or unsupported the size is 0).  Its contents are undefined on
+ * return; calls sharing one workspace must be ordered on one stream.
+ * Errors: SC_ESTALE, SC_EUNAVAILABLE (a page's state not written at
  * this layer), SC_EINVAL (workspace too small or misaligned), SC_EUNSUPPORTED,
  * SC_EDEVICE. */
 size_t sc_attention_workspace_bytes(const sc_plan* plan, const sc_cache* cache);

@@ -214,7 +214,7 @@ struct AppendArgs {
 // three lanes that hold its other tokens, and the codes cross LDS, so that they leave in
 // 16-byte runs.  A chain of latencies: a frame of 64 tokens, 12 heads, rotated, takes 4.8 us
 // (6.2 with K in one wave, 9.7 with V in the same one and rotations loaded one by one), a chunk
-// of 3 x 1560 tokens (36 MB) 11.2 (12.7 with K in one).
+// of 3 x 1560 tokens (36 MB) 11.2 (12.4 with K in one).
 template <bool ROPE>
 __global__ __launch_bounds__(256) void fp4_append_kernel(AppendArgs g, int32_t items) {
   __shared__ __attribute__((aligned(16))) char lds[4][2048 + 128];
