@@ -494,8 +494,8 @@ def sc_rope_rotate(rope: Rope, x, y, positions, layout: str = "interleaved", tra
     if tuple(positions.shape) != (shape[0], 3) or positions.dtype != _torch.int32 or not positions.is_contiguous():
         raise ScError(SC_EINVAL, "SC_EINVAL: positions are contiguous int32 [rows, 3]")
     on = x.get_device()  # -1 in host memory, which a kernel must not be given
-    if (on < 0 or y.get_device() != on or positions.get_device() != on or
-            (stream is None and on != _torch.cuda.current_device())):
+    if shape[0] and (on < 0 or y.get_device() != on or positions.get_device() != on or
+                     (stream is None and on != _torch.cuda.current_device())):
         raise ScError(SC_EINVAL, "SC_EINVAL: x, y and positions are tensors of one GPU, the current one unless a stream is given")
     d = sc_rotate_desc(shape[0], shape[1], shape[2], dtype, ROPE_LAYOUTS[layout], 1 if transpose else 0,
                        xs[0], xs[1], ys[0], ys[1])

@@ -25,6 +25,8 @@ def test_host_tensors(dtype):
         for out in (x, y):
             _refused(rope, x, out, pos)
             _refused(rope, x, out, pos, stream=0)
+    x, y, pos = _tensors("cpu", dtype)
+    sc.sc_rope_rotate(rope, x[:0], y[:0], pos[:0])  # of no rows nothing is read
 
 
 @pytest.mark.gpu
